@@ -309,6 +309,196 @@ ods_status ods_graph_launch(hipGraphExec_t exec, hipStream_t stream);
 /* Free a graph from ods_partition_graph (NULL is a no-op). */
 ods_status ods_graph_destroy(hipGraphExec_t exec);
 
+/* ---- Rotary positions ------------------------------------------------------
+ *
+ * A rotary embedding other than the whole-head, half-layout one the layer's
+ * `rope` operator applies. Pair i of rotary_dim / 2 turns by position *
+ * freqs[i]; the two values of a pair are dims i and i + rotary_dim / 2, or
+ * with interleaved != 0 dims 2 i and 2 i + 1. Dims from rotary_dim on pass
+ * through. The turned values are multiplied by `amplitude` (1: a plain
+ * rotation; a long-context model's attention factor goes here, as its square
+ * root of the score's factor).
+ *
+ * freqs: device table of rotary_dim / 2 doubles, which ods_rope_freqs() fills
+ * on the host from the other fields (angles of far positions need more than
+ * float: position 10^6 times a float's rounding is 0.06 of a radian). With
+ * f_i = theta^(-2 i / rotary_dim), `scaling` is
+ *   ODS_ROPE_PLAIN      f_i
+ *   ODS_ROPE_LINEAR     f_i / factor (position interpolation)
+ *   ODS_ROPE_BASE       f_i of theta * factor^(r / (r - 2)), r = rotary_dim (f_i for r = 2)
+ *   ODS_ROPE_ROTATIONS  f_i for pairs that turn turns_hi times or more over
+ *                       orig_ctx positions, f_i / factor for turns_lo or fewer,
+ *                       between them a blend linear in the number of turns
+ *   ODS_ROPE_INDEX      the same two ends, the blend linear in the pair's index
+ *                       between the indices of turns_hi (rounded down, at least
+ *                       0) and turns_lo (rounded up, at most r - 1)
+ * (interpolation by parts: Peng et al. 2023, arxiv 2309.00071). */
+typedef enum {
+  ODS_ROPE_PLAIN = 0, ODS_ROPE_LINEAR, ODS_ROPE_BASE, ODS_ROPE_ROTATIONS, ODS_ROPE_INDEX
+} ods_rope_scaling;
+
+typedef struct {
+  int32_t head_dim;     /* multiple of 8, 8 .. 256 */
+  int32_t rotary_dim;   /* even, 2 .. head_dim */
+  int32_t interleaved;  /* 0: half layout, 1: interleaved */
+  int32_t scaling;      /* ods_rope_scaling */
+  double theta, factor; /* > 0; theta != 1 for ODS_ROPE_INDEX */
+  double orig_ctx, turns_hi, turns_lo; /* ROTATIONS, INDEX: orig_ctx > 0, turns_hi > turns_lo > 0 */
+  float amplitude;
+  const double *freqs;  /* device [rotary_dim / 2] */
+} ods_rope;
+
+/* The table of `rope` (its freqs pointer is not read): rotary_dim / 2 doubles
+ * into caller memory on the host. ODS_EINVAL for null pointers, a field outside
+ * the ranges above or a value that is not finite; ODS_EUNSUPPORTED for a
+ * head_dim that is no multiple of 8 or past 256. */
+ods_status ods_rope_freqs(const ods_rope *rope, double *freqs_host);
+
+/* y = the heads of x rotated, bf16: row r's `heads` heads of head_dim values
+ * start at x + r * x_stride (in elements) and go to y + r * y_stride, turned
+ * to position pos[r] (device int32). A row with a negative position is left
+ * alone: its y is not written. x and y may be the same rows (in place) or
+ * rows that do not overlap; strides are multiples of 8 and at least
+ * heads * head_dim, so the q and k heads of qkv rows are one call.
+ * ODS_EINVAL for null or misaligned pointers, negative rows or heads, bad
+ * strides, a partial overlap, or rope fields ods_rope_freqs refuses; rows or
+ * heads of 0 return ODS_OK with nothing enqueued. */
+ods_status ods_rope_rows(const ods_rope *rope, const void *x, int64_t x_stride, void *y, int64_t y_stride,
+                         int32_t rows, int32_t heads, const int32_t *pos, hipStream_t stream);
+
+/* ---- Drafted rows: several tokens of a sequence in one step -----------------
+ *
+ * A step over a tree of drafted tokens per sequence (speculative decoding), a
+ * chunk of a prompt (a tree that is a chain) or one token (a tree of one).
+ * The operators are those of ods_run_partition, on rows instead of sequences:
+ * row_off[b] .. row_off[b + 1] - 1 of every live buffer are the drafted tokens
+ * of sequence b, and rope, kv_append and attn_core take their drafted form:
+ *   - batch->ctx_lens[b] counts the tokens already in the cache, none of the
+ *     drafted ones among them; 0 is a new sequence. A sequence with a negative
+ *     count is left alone by rope and kv_append, its attention output is zeros;
+ *   - drafted token j of a sequence lives in the cache slot of token position
+ *     ctx + j, whatever its place in the tree, and kv_append writes it there;
+ *   - its position for rope and sliding windows is ctx + depth[row]; depth is
+ *     0 for a token that follows the cached ones directly;
+ *   - it attends the cached tokens t < ctx (a sliding-window layer: those with
+ *     t > ctx + depth - window) and the drafted tokens j of its own sequence
+ *     with bit j of its mask set (bit j % 64 of word j / 64; in a
+ *     sliding-window layer only those less than `window` positions before it).
+ *     Its own bit is not implied: a row that may see nothing gets zeros. What
+ *     a row may not see does not reach it, infinities and NaN included.
+ * A chain of one token with its bit set is the decode step of context ctx + 1.
+ *
+ *   rows      rows of the live buffers (what ods_live_bytes and the GEMMs take
+ *             as the batch); rows from row_off[batch] on are padding, which
+ *             rope, kv_append and attn_core leave as they were
+ *   max_rows  most rows of one sequence, 1 .. ODS_DRAFT_MAX_ROWS; a sequence's
+ *             rows past it are treated as padding
+ *   row_off   device [batch + 1], ascending, row_off[0] >= 0
+ *   depth     device [rows], 0 .. max_rows - 1 (values outside are clamped)
+ *   mask      device [rows][(max_rows + 63) / 64]
+ *   rope      NULL: the layers' own rope_theta; or n_layers entries (host),
+ *             each with the layer's head_dim
+ * Slots past the page table (max_pages * 16 tokens) are neither written nor
+ * attended. A window-only ring must also hold the drafted tokens:
+ * ring_pages >= ceil((window + max_rows) / 16) + 1 (ODS_EINVAL otherwise).
+ * batch <= 4096 as for attn_core; rows * n_q < 2^31, and batch * n_kv * query
+ * tiles * window pages < 2^30 (ODS_EUNSUPPORTED otherwise). split_pages is not
+ * used. */
+#define ODS_DRAFT_MAX_ROWS 256
+typedef struct {
+  int32_t rows, max_rows;
+  const int32_t *row_off;
+  const int32_t *depth;
+  const uint64_t *mask;
+  const ods_rope *rope;
+} ods_draft;
+
+/* Minimum ods_state.ws_bytes for any operator range of this block, batch and
+ * draft (its pointers are not read); 0 on invalid arguments. */
+size_t ods_draft_workspace_bytes(const ods_block *blk, const ods_batch *batch, const ods_draft *draft);
+
+/* Enqueue operators [op_begin, op_end) of the block for drafted rows: the
+ * contract of ods_run_partition (fusion, checks before anything is enqueued,
+ * errors), with ods_draft_workspace_bytes() of workspace. batch->batch == 0 or
+ * draft->rows == 0 returns ODS_OK with nothing enqueued. */
+ods_status ods_run_draft(const ods_block *blk, int32_t op_begin, int32_t op_end, const ods_batch *batch,
+                         const ods_draft *draft, ods_state *state, hipStream_t stream);
+
+/* ods_partition_graph for drafted rows: the pointers of draft (the entries of
+ * draft->rope included) and rows, max_rows are held as of this call; row_off,
+ * depth, mask and freqs are read at each launch. */
+ods_status ods_draft_graph(const ods_block *blk, int32_t op_begin, int32_t op_end, const ods_batch *batch,
+                           const ods_draft *draft, ods_state *state, hipGraphExec_t *exec);
+
+/* ---- Pages of a cache: sharing, copying, compacting, freeing ----------------
+ *
+ * Host bookkeeping over caller memory, for page tables of full-attention
+ * layers (rings are not shared): who holds each page and which are free. No
+ * device work; the copies a call asks for are (src, dst) page pairs for
+ * ods_kv_copy_pages. One ods_pages serves all layers that share a table.
+ * Calls on one ods_pages are ordered by the caller. On a non-OK status nothing
+ * was changed. */
+typedef struct {
+  int64_t pool_pages;
+  int32_t *refs;      /* [pool_pages] holders of each page */
+  int32_t *free_ids;  /* [pool_pages]; the first n_free are the free pages, the next one taken last */
+  int64_t n_free;
+} ods_pages;
+
+/* Count the holders of every page in table [rows][max_pages] (NULL: none;
+ * entries < 0 hold nothing) and list the rest as free, lowest id taken first.
+ * ODS_ERANGE for an entry >= pool_pages. */
+ods_status ods_pages_init(ods_pages *pages, const int32_t *table, int32_t rows, int32_t max_pages);
+
+/* A sequence (its table row) goes from old_tokens to new_tokens tokens. Fewer:
+ * pages past the new count are given back. More: pages are taken, and if the
+ * page that holds position old_tokens is partly filled and shared, the
+ * sequence gets a page of its own for it: one pair (at most) is written to
+ * pair[2] and *n_pairs is 1, else 0; the caller copies it before the new
+ * tokens are written. ODS_ENOMEM without enough free pages, ODS_ERANGE when the
+ * row is too short, ODS_EINVAL for a row whose held pages are not exactly those
+ * of old_tokens. */
+ods_status ods_pages_resize(ods_pages *pages, int32_t *row, int32_t max_pages, int32_t old_tokens,
+                            int32_t new_tokens, int32_t pair[2], int32_t *n_pairs);
+
+/* dst_row (empty: every entry < 0) holds the pages of the `tokens` tokens of
+ * src_row too. Nothing is copied until either grows (ods_pages_resize). */
+ods_status ods_pages_fork(ods_pages *pages, const int32_t *src_row, int32_t *dst_row, int32_t max_pages,
+                          int32_t tokens);
+
+/* Give back every page of a row; its entries become -1. */
+ods_status ods_pages_release(ods_pages *pages, int32_t *row, int32_t max_pages);
+
+/* Move held pages with the highest ids into the lowest free ids, at most
+ * max_pairs of them, and rewrite the table: with max_pairs large enough the
+ * held pages become [0, pool_pages - n_free). Writes pairs [*n_pairs][2], no
+ * page twice in them. ODS_EINVAL unless the table's rows hold exactly what
+ * `refs` counts. */
+ods_status ods_pages_compact(ods_pages *pages, int32_t *table, int32_t rows, int32_t max_pages, int32_t *pairs,
+                             int32_t max_pairs, int32_t *n_pairs);
+
+/* Copy pages inside the pools of layers [layer_begin, layer_end): page
+ * pairs[i][0] to page pairs[i][1] (device int32 [n_pairs][2]), keys and values
+ * of every KV head. The copies have no order among each other: no page may be
+ * a dst twice, or both a src and a dst. Pairs with an id outside a layer's pool
+ * or with src == dst are skipped. ODS_ERANGE for a bad layer range. */
+ods_status ods_kv_copy_pages(const ods_block *blk, int32_t layer_begin, int32_t layer_end, const int32_t *pairs,
+                             int32_t n_pairs, hipStream_t stream);
+
+/* Keep one path of each sequence's drafted tokens: with path [batch][path_cols]
+ * and path_len [batch] (device), the cache slot of drafted token path[b][k]
+ * moves to that of token position ctx + k, for k < path_len[b], in every layer
+ * of [layer_begin, layer_end) (through the ring in ring layers), and
+ * ctx_out[b] = ctx + path_len[b] (device [batch]; NULL: not written; may be
+ * batch->ctx_lens itself). A path is strictly ascending and below the
+ * sequence's row count; the first entry that is not ends it there, and a
+ * length past path_cols is cut. The slots of a sequence being kept must lie on
+ * pages that no other sequence holds. draft: rows, max_rows and row_off are
+ * read. path_cols 1 .. ODS_DRAFT_MAX_ROWS. */
+ods_status ods_kv_accept(const ods_block *blk, int32_t layer_begin, int32_t layer_end, const ods_batch *batch,
+                         const ods_draft *draft, const int32_t *path, int32_t path_cols, const int32_t *path_len,
+                         int32_t *ctx_out, hipStream_t stream);
+
 /* Message for the last non-OK status returned on this thread ("" if none). */
 const char *ods_last_error(void);
 

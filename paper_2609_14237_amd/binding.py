@@ -19,6 +19,9 @@ PAGE_TOKENS = 16
 SCRATCH_BYTES = 64 << 20  # ODS_SCRATCH_BYTES
 ODS_WEIGHTS_ROWS, ODS_WEIGHTS_TILED = 0, 1
 
+ODS_ROPE_PLAIN, ODS_ROPE_LINEAR, ODS_ROPE_BASE, ODS_ROPE_ROTATIONS, ODS_ROPE_INDEX = 0, 1, 2, 3, 4
+DRAFT_MAX_ROWS = 256  # ODS_DRAFT_MAX_ROWS
+
 BUFFERS = ("resid", "xn", "qkv", "o", "hn", "gu", "act", "logits", "topk_w", "topk_ids", "perm",
            "slot_pos", "expert_off", "xp", "gu_p", "act_p", "yp")
 
@@ -56,6 +59,21 @@ class ods_state(C.Structure):
                 ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
 
 
+class ods_rope(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("scaling", C.c_int32),
+                ("theta", C.c_double), ("factor", C.c_double), ("orig_ctx", C.c_double), ("turns_hi", C.c_double),
+                ("turns_lo", C.c_double), ("amplitude", C.c_float), ("freqs", C.c_void_p)]
+
+
+class ods_draft(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("max_rows", C.c_int32), ("row_off", C.c_void_p), ("depth", C.c_void_p),
+                ("mask", C.c_void_p), ("rope", C.POINTER(ods_rope))]
+
+
+class ods_pages(C.Structure):
+    _fields_ = [("pool_pages", C.c_int64), ("refs", C.c_void_p), ("free_ids", C.c_void_p), ("n_free", C.c_int64)]
+
+
 # Every symbol include/ods.h declares, with its ctypes signature.
 SIGNATURES = {
     "ods_kv_alloc": (C.c_int, [C.c_int64, C.POINTER(C.c_int32), C.c_int32, C.c_uint64, C.c_int32,
@@ -81,6 +99,24 @@ SIGNATURES = {
     "ods_tiled_weight_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32, C.c_int32]),
     "ods_tile_weight": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                   C.c_void_p]),
+    "ods_rope_freqs": (C.c_int, [C.POINTER(ods_rope), C.c_void_p]),
+    "ods_rope_rows": (C.c_int, [C.POINTER(ods_rope), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32,
+                                C.c_void_p, C.c_void_p]),
+    "ods_draft_workspace_bytes": (C.c_size_t, [C.POINTER(ods_block), C.POINTER(ods_batch), C.POINTER(ods_draft)]),
+    "ods_run_draft": (C.c_int, [C.POINTER(ods_block), C.c_int32, C.c_int32, C.POINTER(ods_batch), C.POINTER(ods_draft),
+                                C.POINTER(ods_state), C.c_void_p]),
+    "ods_draft_graph": (C.c_int, [C.POINTER(ods_block), C.c_int32, C.c_int32, C.POINTER(ods_batch),
+                                  C.POINTER(ods_draft), C.POINTER(ods_state), C.POINTER(C.c_void_p)]),
+    "ods_pages_init": (C.c_int, [C.POINTER(ods_pages), C.c_void_p, C.c_int32, C.c_int32]),
+    "ods_pages_resize": (C.c_int, [C.POINTER(ods_pages), C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                                   C.c_void_p]),
+    "ods_pages_fork": (C.c_int, [C.POINTER(ods_pages), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32]),
+    "ods_pages_release": (C.c_int, [C.POINTER(ods_pages), C.c_void_p, C.c_int32]),
+    "ods_pages_compact": (C.c_int, [C.POINTER(ods_pages), C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
+                                    C.c_void_p]),
+    "ods_kv_copy_pages": (C.c_int, [C.POINTER(ods_block), C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]),
+    "ods_kv_accept": (C.c_int, [C.POINTER(ods_block), C.c_int32, C.c_int32, C.POINTER(ods_batch), C.POINTER(ods_draft),
+                                C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
 }
 
 
@@ -184,3 +220,73 @@ def ods_tiled_weight_bytes(out: int, in_: int, gated: int, groups: int) -> int:
 
 def ods_tile_weight(src: int, dst: int, out: int, in_: int, gated: int, groups: int, stream: int) -> int:
     return lib.ods_tile_weight(src, dst, out, in_, gated, groups, stream)
+
+
+def _np(a):
+    """Address of a C-contiguous int32 array (None: NULL)."""
+    return None if a is None else a.ctypes.data
+
+
+def ods_rope_freqs(rope: ods_rope, freqs_host) -> int:
+    """freqs_host: float64 numpy [rotary_dim / 2] (written)."""
+    return lib.ods_rope_freqs(C.byref(rope), _np(freqs_host))
+
+
+def ods_rope_rows(rope: ods_rope, x: int, x_stride: int, y: int, y_stride: int, rows: int, heads: int, pos: int,
+                  stream: int) -> int:
+    return lib.ods_rope_rows(C.byref(rope), x, x_stride, y, y_stride, rows, heads, pos, stream)
+
+
+def ods_draft_workspace_bytes(blk: ods_block, batch: ods_batch, draft: ods_draft) -> int:
+    return lib.ods_draft_workspace_bytes(C.byref(blk), C.byref(batch), C.byref(draft))
+
+
+def ods_run_draft(blk: ods_block, op_begin: int, op_end: int, batch: ods_batch, draft: ods_draft, state: ods_state,
+                  stream: int) -> int:
+    return lib.ods_run_draft(C.byref(blk), op_begin, op_end, C.byref(batch), C.byref(draft), C.byref(state), stream)
+
+
+def ods_draft_graph(blk: ods_block, op_begin: int, op_end: int, batch: ods_batch, draft: ods_draft, state: ods_state):
+    """(status, exec handle or None)."""
+    h = C.c_void_p()
+    st = lib.ods_draft_graph(C.byref(blk), op_begin, op_end, C.byref(batch), C.byref(draft), C.byref(state), C.byref(h))
+    return st, h.value
+
+
+def ods_pages_init(pages: ods_pages, table) -> int:
+    """table: int32 numpy [rows, max_pages] or None."""
+    rows, cols = (0, 0) if table is None else table.shape
+    return lib.ods_pages_init(C.byref(pages), _np(table), rows, cols)
+
+
+def ods_pages_resize(pages: ods_pages, row, old_tokens: int, new_tokens: int, pair):
+    """(status, n_pairs). row: int32 numpy [max_pages]; pair: int32 numpy [2] (written when n_pairs is 1)."""
+    n = C.c_int32(0)
+    st = lib.ods_pages_resize(C.byref(pages), _np(row), len(row), old_tokens, new_tokens, _np(pair), C.addressof(n))
+    return st, n.value
+
+
+def ods_pages_fork(pages: ods_pages, src_row, dst_row, tokens: int) -> int:
+    return lib.ods_pages_fork(C.byref(pages), _np(src_row), _np(dst_row), len(dst_row), tokens)
+
+
+def ods_pages_release(pages: ods_pages, row) -> int:
+    return lib.ods_pages_release(C.byref(pages), _np(row), len(row))
+
+
+def ods_pages_compact(pages: ods_pages, table, pairs):
+    """(status, n_pairs). table: int32 numpy [rows, max_pages]; pairs: int32 numpy [max_pairs, 2] (written)."""
+    n = C.c_int32(0)
+    st = lib.ods_pages_compact(C.byref(pages), _np(table), table.shape[0], table.shape[1], _np(pairs), len(pairs),
+                               C.addressof(n))
+    return st, n.value
+
+
+def ods_kv_copy_pages(blk: ods_block, layer_begin: int, layer_end: int, pairs: int, n_pairs: int, stream: int) -> int:
+    return lib.ods_kv_copy_pages(C.byref(blk), layer_begin, layer_end, pairs, n_pairs, stream)
+
+
+def ods_kv_accept(blk: ods_block, layer_begin: int, layer_end: int, batch: ods_batch, draft: ods_draft, path: int,
+                  path_cols: int, path_len: int, ctx_out, stream: int) -> int:
+    return lib.ods_kv_accept(C.byref(blk), layer_begin, layer_end, C.byref(batch), C.byref(draft), path, path_cols,
+                             path_len, ctx_out, stream)

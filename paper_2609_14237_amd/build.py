@@ -17,11 +17,12 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include")]
-SOURCES = ["k_gemm.hip", "k_gemm_stream.hip", "k_gemm_skinny.hip", "k_attn.hip", "k_elem.hip", "k_moe.hip", "ods_api.cpp"]
+SOURCES = ["k_gemm.hip", "k_gemm_stream.hip", "k_gemm_skinny.hip", "k_attn.hip", "k_elem.hip", "k_moe.hip",
+           "k_rope.hip", "k_tree.hip", "k_cache.hip", "ods_api.cpp"]
 # The HIP-free host part (validation, allocator, sizing, planning) builds with
-# the host compiler alone; tests/test_host_sanitize.py builds it again under
-# the CPU sanitizers.
-HOST_SOURCES = ["ods_host.cpp"]
+# the host compiler alone; tests/test_host_sanitize.py and
+# tests/test_draft_host.py build it again under the CPU sanitizers.
+HOST_SOURCES = ["ods_host.cpp", "ods_draft.cpp", "ods_pages.cpp"]
 HOST_CXX = os.environ.get("CXX", "g++")
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__", "-I", "/opt/rocm/include",
               "-I", os.path.join(ROOT, "include")]

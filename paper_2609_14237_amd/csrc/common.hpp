@@ -73,15 +73,18 @@ __device__ __forceinline__ float block_sum_256(float v, float *red) {
   return t;
 }
 
-// cos and sin of the RoPE angle of dimension pair i (of D / 2) at position p:
-// p * theta^(-2 i / D), reduced mod 2 pi in double before the fp32 functions.
-__device__ __forceinline__ void rope_angle(int p, int i, int D, float theta, float &cv, float &sv) {
+// cos and sin of an angle of many turns, reduced mod 2 pi in double before the fp32 functions.
+__device__ __forceinline__ void turn_by(double a, float &cv, float &sv) {
   const double two_pi_hi = 6.283185307179586, two_pi_lo = 2.4492935982947064e-16;
-  const double inv = exp2(-(2.0 * i / D) * log2((double)theta));
-  const double a = (double)p * inv;
   const double k = rint(a * (1.0 / two_pi_hi));
   const double r = fma(-k, two_pi_lo, fma(-k, two_pi_hi, a));
   sincosf((float)r, &sv, &cv);
+}
+
+// The same of the RoPE angle of dimension pair i (of D / 2) at position p: p * theta^(-2 i / D).
+__device__ __forceinline__ void rope_angle(int p, int i, int D, float theta, float &cv, float &sv) {
+  const double inv = exp2(-(2.0 * i / D) * log2((double)theta));
+  turn_by((double)p * inv, cv, sv);
 }
 
 // 8 bf16 values: their sum of squares, and their product with inv and a gain.

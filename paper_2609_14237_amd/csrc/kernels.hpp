@@ -67,4 +67,44 @@ hipError_t launch_gather_rows(const uint16_t *src, const int32_t *perm, const in
 hipError_t launch_moe_combine(const uint16_t *yp, const float *w, const int32_t *slot_pos, int B,
                               int k, int H, uint16_t *resid, hipStream_t s);
 
+// y = the rows' heads turned to their positions (arguments checked by check_rope_rows).
+hipError_t launch_rope_rows(const ods_rope &r, const uint16_t *x, int64_t xs, uint16_t *y, int64_t ys, int rows,
+                            int heads, const int32_t *pos, hipStream_t s);
+
+// Drafted rows of one layer: B sequences, `rows` rows of the buffers.
+struct DraftArgs {
+  uint16_t *qkv;
+  uint16_t *o;
+  int B, rows, max_rows, n_q, n_kv, D, window;
+  const int32_t *row_off, *depth, *ctx_lens, *table;
+  const uint64_t *mask;
+  int cols, ring;
+  uint16_t *pool;
+  int64_t pool_pages;
+  const double *freqs;  // null: the layer's own theta, whole head, half layout
+  int rdim, interleaved;
+  float amp, theta;
+};
+hipError_t launch_draft_rope_append(const DraftArgs &a, bool do_rope, bool do_append, hipStream_t s);
+hipError_t launch_tree_attention(const DraftArgs &a, hipStream_t s);
+
+// Pools of several layers, handed to one launch by value.
+constexpr int kPoolSet = 32;
+struct PoolRef {
+  uint16_t *pool;
+  int64_t pages, page_elems;  // page_elems = 2 n_kv 16 D
+  const int32_t *table;       // accept only
+  int cols, ring, n_kv, D;
+};
+struct PoolSet {
+  PoolRef p[kPoolSet];
+};
+struct AcceptArgs {
+  int B, rows, max_rows, path_cols;
+  const int32_t *row_off, *ctx_lens, *path, *path_len;
+};
+hipError_t launch_copy_pages(const PoolSet &pools, int n_pools, const int32_t *pairs, int n, hipStream_t s);
+hipError_t launch_accept(const AcceptArgs &a, const PoolSet &pools, int n_pools, int max_kv, hipStream_t s);
+hipError_t launch_accept_ctx(const AcceptArgs &a, int32_t *ctx_out, hipStream_t s);
+
 }  // namespace ods

@@ -107,6 +107,98 @@ ods_status scratch_ptr(void **out) {
   return ODS_OK;
 }
 
+// Enqueues a validated range.
+ods_status run_rows(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, const ods_state *st, int cus,
+                    bool trace, hipStream_t stream) {
+  for (int i = 0; i < op_end - op_begin;) {
+    Launch L;
+    plan_launch(blk, op_begin, op_end, i, batch, st, cus, &L);
+    const hipError_t e = execute(L, stream);
+    if (trace) fprintf(stderr, "[ods] layer %d %s B=%d -> %s\n", L.layer, L.what, batch->batch, hipGetErrorString(e));
+    if (e != hipSuccess)
+      return set_error(ODS_EHIP, "launch of %s (layer %d) failed: %s", L.what, L.layer, hipGetErrorString(e));
+    i += L.n_ops;
+  }
+  return ODS_OK;
+}
+
+// Captures what `enqueue` puts on a private stream as an instantiated graph.
+template <typename F>
+ods_status capture(hipGraphExec_t *exec, F enqueue) {
+  if (!exec) return set_error(ODS_EINVAL, "exec is null");
+  *exec = nullptr;
+  hipStream_t s = nullptr;
+  hipError_t e = hipStreamCreateWithFlags(&s, hipStreamNonBlocking);
+  if (e != hipSuccess) return set_error(ODS_EHIP, "hipStreamCreate: %s", hipGetErrorString(e));
+  e = hipStreamBeginCapture(s, hipStreamCaptureModeThreadLocal);
+  if (e != hipSuccess) {
+    hipStreamDestroy(s);
+    return set_error(ODS_EHIP, "hipStreamBeginCapture: %s", hipGetErrorString(e));
+  }
+  const ods_status rc = enqueue(s);
+  std::string msg = rc == ODS_OK ? "" : error_text();
+  hipGraph_t graph = nullptr;
+  e = hipStreamEndCapture(s, &graph);
+  hipStreamDestroy(s);
+  if (rc != ODS_OK) {
+    if (graph) hipGraphDestroy(graph);
+    return set_error(rc, "%s", msg.c_str());
+  }
+  if (e != hipSuccess || !graph) return set_error(ODS_EHIP, "hipStreamEndCapture: %s", hipGetErrorString(e));
+  e = hipGraphInstantiate(exec, graph, nullptr, nullptr, 0);
+  hipGraphDestroy(graph);
+  if (e != hipSuccess) {
+    *exec = nullptr;
+    return set_error(ODS_EHIP, "hipGraphInstantiate: %s", hipGetErrorString(e));
+  }
+  clear_error();
+  return ODS_OK;
+}
+
+DraftArgs draft_args(const ods_block *blk, int layer, const ods_batch *batch, const ods_draft *draft,
+                     const ods_state *st) {
+  const ods_layer &L = blk->layers[layer];
+  const ods_layer_cfg &c = L.cfg;
+  const KvMap m = kv_map(c, batch);
+  DraftArgs a{};
+  a.qkv = (uint16_t *)st->qkv;
+  a.o = (uint16_t *)st->o;
+  a.B = batch->batch; a.rows = draft->rows; a.max_rows = draft->max_rows;
+  a.n_q = c.n_q; a.n_kv = c.n_kv; a.D = c.head_dim; a.window = c.window;
+  a.row_off = draft->row_off; a.depth = draft->depth; a.ctx_lens = batch->ctx_lens; a.mask = draft->mask;
+  a.table = m.table; a.cols = m.cols; a.ring = m.ring;
+  a.pool = (uint16_t *)L.kv_pool; a.pool_pages = L.pool_pages;
+  a.theta = c.rope_theta;
+  if (draft->rope) {
+    const ods_rope &r = draft->rope[layer];
+    a.freqs = r.freqs; a.rdim = r.rotary_dim; a.interleaved = r.interleaved; a.amp = r.amplitude;
+  }
+  return a;
+}
+
+// Calls go(pools, n) for layers [begin, end), at most kPoolSet at a time.
+template <typename F>
+hipError_t each_pool_set(const ods_block *blk, int begin, int end, const ods_batch *batch, F go) {
+  for (int l0 = begin; l0 < end; l0 += kPoolSet) {
+    PoolSet set{};
+    const int n = end - l0 < kPoolSet ? end - l0 : kPoolSet;
+    for (int i = 0; i < n; ++i) {
+      const ods_layer &L = blk->layers[l0 + i];
+      PoolRef &r = set.p[i];
+      r.pool = (uint16_t *)L.kv_pool;
+      r.pages = L.pool_pages;
+      r.n_kv = L.cfg.n_kv;
+      r.D = L.cfg.head_dim;
+      r.page_elems = (int64_t)2 * r.n_kv * ODS_PAGE_TOKENS * r.D;
+      if (!batch) continue;
+      const KvMap m = kv_map(L.cfg, batch);
+      r.table = m.table; r.cols = m.cols; r.ring = m.ring;
+    }
+    if (const hipError_t e = go(set, n); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 }  // namespace
 
 extern "C" {
@@ -125,18 +217,9 @@ ods_status ods_run_partition(const ods_block *blk, int32_t op_begin, int32_t op_
     clear_error();
     return ODS_OK;
   }
-  const bool trace = trace_on();
-  for (int i = 0; i < op_end - op_begin;) {
-    Launch L;
-    plan_launch(blk, op_begin, op_end, i, batch, st, cus, &L);
-    const hipError_t e = execute(L, stream);
-    if (trace) fprintf(stderr, "[ods] layer %d %s B=%d -> %s\n", L.layer, L.what, batch->batch, hipGetErrorString(e));
-    if (e != hipSuccess)
-      return set_error(ODS_EHIP, "launch of %s (layer %d) failed: %s", L.what, L.layer, hipGetErrorString(e));
-    i += L.n_ops;
-  }
-  clear_error();
-  return ODS_OK;
+  const ods_status done = run_rows(blk, op_begin, op_end, batch, st, cus, trace_on(), stream);
+  if (done == ODS_OK) clear_error();
+  return done;
 }
 
 ods_status ods_run_partition_scratch(const ods_block *blk, int32_t op_begin, int32_t op_end,
@@ -198,34 +281,12 @@ ods_status ods_ffn_stage(const ods_block *blk, int32_t layer, const ods_batch *b
 
 ods_status ods_partition_graph(const ods_block *blk, int32_t op_begin, int32_t op_end, const ods_batch *batch,
                                ods_state *state, hipGraphExec_t *exec) {
-  if (!exec) return set_error(ODS_EINVAL, "exec is null");
-  *exec = nullptr;
-  hipStream_t s = nullptr;
-  hipError_t e = hipStreamCreateWithFlags(&s, hipStreamNonBlocking);
-  if (e != hipSuccess) return set_error(ODS_EHIP, "hipStreamCreate: %s", hipGetErrorString(e));
-  e = hipStreamBeginCapture(s, hipStreamCaptureModeThreadLocal);
-  if (e != hipSuccess) {
-    hipStreamDestroy(s);
-    return set_error(ODS_EHIP, "hipStreamBeginCapture: %s", hipGetErrorString(e));
-  }
-  const ods_status rc = ods_run_partition(blk, op_begin, op_end, batch, state, s);
-  std::string msg = rc == ODS_OK ? "" : error_text();
-  hipGraph_t graph = nullptr;
-  e = hipStreamEndCapture(s, &graph);
-  hipStreamDestroy(s);
-  if (rc != ODS_OK) {
-    if (graph) hipGraphDestroy(graph);
-    return set_error(rc, "%s", msg.c_str());
-  }
-  if (e != hipSuccess || !graph) return set_error(ODS_EHIP, "hipStreamEndCapture: %s", hipGetErrorString(e));
-  e = hipGraphInstantiate(exec, graph, nullptr, nullptr, 0);
-  hipGraphDestroy(graph);
-  if (e != hipSuccess) {
-    *exec = nullptr;
-    return set_error(ODS_EHIP, "hipGraphInstantiate: %s", hipGetErrorString(e));
-  }
-  clear_error();
-  return ODS_OK;
+  return capture(exec, [&](hipStream_t s) { return ods_run_partition(blk, op_begin, op_end, batch, state, s); });
+}
+
+ods_status ods_draft_graph(const ods_block *blk, int32_t op_begin, int32_t op_end, const ods_batch *batch,
+                           const ods_draft *draft, ods_state *state, hipGraphExec_t *exec) {
+  return capture(exec, [&](hipStream_t s) { return ods_run_draft(blk, op_begin, op_end, batch, draft, state, s); });
 }
 
 ods_status ods_graph_launch(hipGraphExec_t exec, hipStream_t stream) {
@@ -240,6 +301,90 @@ ods_status ods_graph_destroy(hipGraphExec_t exec) {
   if (!exec) return ODS_OK;
   const hipError_t e = hipGraphExecDestroy(exec);
   if (e != hipSuccess) return set_error(ODS_EHIP, "hipGraphExecDestroy: %s", hipGetErrorString(e));
+  clear_error();
+  return ODS_OK;
+}
+
+ods_status ods_rope_rows(const ods_rope *rope, const void *x, int64_t x_stride, void *y, int64_t y_stride,
+                         int32_t rows, int32_t heads, const int32_t *pos, hipStream_t stream) {
+  const ods_status rc = check_rope_rows(rope, x, x_stride, y, y_stride, rows, heads, pos);
+  if (rc != ODS_OK) return rc;
+  const hipError_t e = launch_rope_rows(*rope, (const uint16_t *)x, x_stride, (uint16_t *)y, y_stride, rows, heads, pos,
+                                        stream);
+  if (e != hipSuccess) return set_error(ODS_EHIP, "ods_rope_rows: %s", hipGetErrorString(e));
+  clear_error();
+  return ODS_OK;
+}
+
+size_t ods_draft_workspace_bytes(const ods_block *blk, const ods_batch *batch, const ods_draft *draft) {
+  if (check_block(blk) != ODS_OK || check_draft_sizes(blk, 0, num_ops(blk), batch, draft) != ODS_OK) return 0;
+  return draft_ws_bytes(blk, 0, num_ops(blk), batch, draft, num_cus());
+}
+
+ods_status ods_run_draft(const ods_block *blk, int32_t op_begin, int32_t op_end, const ods_batch *batch,
+                         const ods_draft *draft, ods_state *st, hipStream_t stream) {
+  const int cus = num_cus();
+  ods_status rc = validate_draft(blk, op_begin, op_end, batch, draft, st, cus);
+  if (rc != ODS_OK) return rc;
+  if (batch->batch == 0 || draft->rows == 0) {
+    clear_error();
+    return ODS_OK;
+  }
+  const bool trace = trace_on();
+  const ods_batch rb = row_batch(batch, draft);
+  for (int g = op_begin; g < op_end;) {
+    const DraftStep step = draft_step(blk, g, op_end);
+    g = step.end;
+    if (step.rows_only) {
+      if ((rc = run_rows(blk, step.begin, step.end, &rb, st, cus, trace, stream)) != ODS_OK) return rc;
+      continue;
+    }
+    const OpRef op = op_at(blk, step.begin);
+    const DraftArgs a = draft_args(blk, op.layer, batch, draft, st);
+    const hipError_t e = step.attn ? launch_tree_attention(a, stream)
+                                   : launch_draft_rope_append(a, step.rope, step.append, stream);
+    const char *what = step.rope && step.append ? "rope+kv_append" : op_kind_name(op.kind);
+    if (trace)
+      fprintf(stderr, "[ods] layer %d drafted %s B=%d rows=%d -> %s\n", op.layer, what, a.B, a.rows, hipGetErrorString(e));
+    if (e != hipSuccess)
+      return set_error(ODS_EHIP, "launch of drafted %s (layer %d) failed: %s", what, op.layer, hipGetErrorString(e));
+  }
+  clear_error();
+  return ODS_OK;
+}
+
+ods_status ods_kv_copy_pages(const ods_block *blk, int32_t layer_begin, int32_t layer_end, const int32_t *pairs,
+                             int32_t n_pairs, hipStream_t stream) {
+  const ods_status rc = check_pools(blk, layer_begin, layer_end, "ods_kv_copy_pages");
+  if (rc != ODS_OK) return rc;
+  if (n_pairs < 0) return set_error(ODS_EINVAL, "ods_kv_copy_pages: %d pairs", n_pairs);
+  if (n_pairs > 0) {
+    if (!pairs || !aligned16(pairs)) return set_error(ODS_EINVAL, "ods_kv_copy_pages: pairs is null or not 16-byte aligned");
+    const hipError_t e = each_pool_set(blk, layer_begin, layer_end, nullptr, [&](const PoolSet &set, int n) {
+      return launch_copy_pages(set, n, pairs, n_pairs, stream);
+    });
+    if (e != hipSuccess) return set_error(ODS_EHIP, "ods_kv_copy_pages: %s", hipGetErrorString(e));
+  }
+  clear_error();
+  return ODS_OK;
+}
+
+ods_status ods_kv_accept(const ods_block *blk, int32_t layer_begin, int32_t layer_end, const ods_batch *batch,
+                         const ods_draft *draft, const int32_t *path, int32_t path_cols, const int32_t *path_len,
+                         int32_t *ctx_out, hipStream_t stream) {
+  const ods_status rc = check_accept(blk, layer_begin, layer_end, batch, draft, path, path_cols, path_len, ctx_out);
+  if (rc != ODS_OK) return rc;
+  if (batch->batch > 0) {
+    AcceptArgs a{};
+    a.B = batch->batch; a.rows = draft->rows; a.max_rows = draft->max_rows; a.path_cols = path_cols;
+    a.row_off = draft->row_off; a.ctx_lens = batch->ctx_lens; a.path = path; a.path_len = path_len;
+    int max_kv = 0;
+    for (int l = layer_begin; l < layer_end; ++l) max_kv = blk->layers[l].cfg.n_kv > max_kv ? blk->layers[l].cfg.n_kv : max_kv;
+    hipError_t e = each_pool_set(blk, layer_begin, layer_end, batch,
+                                 [&](const PoolSet &set, int n) { return launch_accept(a, set, n, max_kv, stream); });
+    if (e == hipSuccess && ctx_out) e = launch_accept_ctx(a, ctx_out, stream);
+    if (e != hipSuccess) return set_error(ODS_EHIP, "ods_kv_accept: %s", hipGetErrorString(e));
+  }
   clear_error();
   return ODS_OK;
 }

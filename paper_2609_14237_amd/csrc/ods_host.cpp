@@ -58,28 +58,15 @@ ods_status check_cfg(const ods_layer_cfg &c, int layer) {
   return ODS_OK;
 }
 
-// Page table a layer's KV operators use: the window-only ring for a sliding-
-// window layer when the batch carries one, the full page table otherwise.
-struct KvMap {
-  const int32_t *table;
-  int cols;  // table columns
-  int ring;  // > 0: logical page lp lives in column lp % ring
-};
-
-KvMap kv_map(const ods_layer_cfg &c, const ods_batch *b) {
-  if (c.window > 0 && b->ring_pages > 0) return KvMap{b->ring_table, b->ring_pages, b->ring_pages};
-  return KvMap{b->page_table, b->max_pages, 0};
-}
-
 AttnPlan plan_for(const ods_layer_cfg &c, const ods_batch *b, int cus) {
   return attn_plan(b->batch, c.n_kv, c.head_dim, kv_map(c, b).cols, c.window, b->split_pages, cus);
 }
 
-size_t layer_ws_bytes(const ods_layer &L, const ods_batch *b, int cus) {
+size_t layer_ws_bytes(const ods_layer &L, const ods_batch *b, int cus, bool with_attn = true) {
   const ods_layer_cfg &c = L.cfg;
   const int B = b->batch;
   const bool t = tiled(L);
-  size_t w = align_up(attn_ws_bytes(B, c.n_q, c.n_kv, c.head_dim, plan_for(c, b, cus)));
+  size_t w = with_attn ? align_up(attn_ws_bytes(B, c.n_q, c.n_kv, c.head_dim, plan_for(c, b, cus))) : 0;
   // A batch of 65 to 128 rows also covers 64 and 80, whose split-K may be the
   // larger one (a SiLU-gated GEMM that runs unsplit past them).
   auto g = [&](int N, int K, int epi, bool bt) {
@@ -109,6 +96,11 @@ struct Need {
 };
 
 }  // namespace
+
+KvMap kv_map(const ods_layer_cfg &c, const ods_batch *b) {
+  if (c.window > 0 && b->ring_pages > 0) return KvMap{b->ring_table, b->ring_pages, b->ring_pages};
+  return KvMap{b->page_table, b->max_pages, 0};
+}
 
 // ---------------------------------------------------------------- error state
 
@@ -418,12 +410,13 @@ int layer_offset(const ods_block *blk, int layer) {
   return n;
 }
 
-size_t range_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, int cus) {
+size_t range_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, int cus,
+                      bool with_attn) {
   size_t w = 0;
   int last = -1;
   for (int g = op_begin; g < op_end; ++g) {
     const int l = op_at(blk, g).layer;
-    if (l != last) w = std::max(w, layer_ws_bytes(blk->layers[l], batch, cus));
+    if (l != last) w = std::max(w, layer_ws_bytes(blk->layers[l], batch, cus, with_attn));
     last = l;
   }
   return w;
@@ -493,7 +486,7 @@ bool gather_fused(const ods_block *blk, int g_permute, int op_end) {
 }  // namespace
 
 ods_status validate_range(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch,
-                          const ods_state *st, int cus) {
+                          const ods_state *st, int cus, bool with_attn) {
   ods_status rc = check_block(blk);
   if (rc != ODS_OK) return rc;
   if (!batch || !st) return set_error(ODS_EINVAL, "null batch or state");
@@ -598,7 +591,7 @@ ods_status validate_range(const ods_block *blk, int op_begin, int op_end, const 
     if (is_moe(c) && (int64_t)B * c.top_k > INT32_MAX / 2) return set_error(ODS_ERANGE, "batch * top_k too large");
   }
   if (need_ws) {
-    const size_t ws_need = range_ws_bytes(blk, op_begin, op_end, batch, cus);
+    const size_t ws_need = range_ws_bytes(blk, op_begin, op_end, batch, cus, with_attn);
     if (!st->ws) return set_error(ODS_EINVAL, "ws is null");
     if (!aligned16(st->ws)) return set_error(ODS_EINVAL, "ws is not 16-byte aligned");
     if (st->ws_bytes < ws_need)

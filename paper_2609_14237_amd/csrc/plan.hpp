@@ -127,9 +127,19 @@ OpRef op_at(const ods_block *blk, int g);       // global operator g
 int layer_offset(const ods_block *blk, int layer);
 int layer_num_ops(const ods_layer_cfg &c);
 
+// Page table a layer's KV operators use: the window-only ring for a sliding-
+// window layer when the batch carries one, the full page table otherwise.
+struct KvMap {
+  const int32_t *table;
+  int cols;  // table columns
+  int ring;  // > 0: logical page lp lives in column lp % ring
+};
+KvMap kv_map(const ods_layer_cfg &c, const ods_batch *b);
+
 // Workspace a range needs (the maximum over the layers it touches), for a
-// device with `cus` compute units.
-size_t range_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, int cus);
+// device with `cus` compute units. with_attn: attention's records included.
+size_t range_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, int cus,
+                      bool with_attn = true);
 size_t block_ws_bytes(const ods_block *blk, const ods_batch *batch, int cus);
 
 // Every check ods_run_partition makes before it enqueues anything: block,
@@ -137,7 +147,7 @@ size_t block_ws_bytes(const ods_block *blk, const ods_batch *batch, int cus);
 // (non-null, 16-byte aligned), shape limits, and the workspace size. ODS_OK
 // means the range can be planned and launched.
 ods_status validate_range(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch,
-                          const ods_state *st, int cus);
+                          const ods_state *st, int cus, bool with_attn = true);
 
 // One launch of a validated range.
 enum LaunchKind {
@@ -181,5 +191,37 @@ struct Launch {
 // be fused into it: out->n_ops says how many it covers.
 void plan_launch(const ods_block *blk, int op_begin, int op_end, int i, const ods_batch *batch, const ods_state *st,
                  int cus, Launch *out);
+
+// ---------------------------------------------------------------- rotary positions and drafted rows (ods_draft.cpp)
+// Fields of an ods_rope outside the documented ranges; `who` names it in the message. Its freqs pointer only
+// with need_freqs.
+ods_status check_rope(const ods_rope *r, const char *who, bool need_freqs);
+// Arguments of ods_rope_rows.
+ods_status check_rope_rows(const ods_rope *r, const void *x, int64_t xs, const void *y, int64_t ys, int rows, int heads,
+                           const int32_t *pos);
+
+inline bool is_kv_op(OpKind k) { return k == K_ROPE || k == K_KV_APPEND || k == K_ATTN_CORE; }
+// One step of a drafted range: a run [begin, end) of operators that only see rows (ods_run_partition on
+// row_batch()), or one of RoPE and/or append, or attention.
+struct DraftStep {
+  int begin, end;
+  bool rows_only, rope, append, attn;
+};
+DraftStep draft_step(const ods_block *blk, int begin, int op_end);
+// The batch the row-wise operators see: draft->rows rows.
+ods_batch row_batch(const ods_batch *batch, const ods_draft *draft);
+size_t draft_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, const ods_draft *draft,
+                      int cus);
+// Counts and shapes of a drafted range, no pointers.
+ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch,
+                             const ods_draft *draft);
+// Every check ods_run_draft makes before it enqueues anything.
+ods_status validate_draft(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, const ods_draft *draft,
+                          const ods_state *st, int cus);
+// Checks of the page operators (block, layer range, pools).
+ods_status check_pools(const ods_block *blk, int layer_begin, int layer_end, const char *who);
+ods_status check_accept(const ods_block *blk, int layer_begin, int layer_end, const ods_batch *batch,
+                        const ods_draft *draft, const int32_t *path, int path_cols, const int32_t *path_len,
+                        const int32_t *ctx_out);
 
 }  // namespace ods
