@@ -3,6 +3,8 @@
 // drafted ones its mask names.
 #include <math.h>
 
+#include <type_traits>
+
 #include "draft.hpp"
 #include "kernels.hpp"
 
@@ -53,64 +55,553 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
   }
 }
 
-// One wave per (drafted row, query head): lanes take a token each for the
-// scores, a dim each for the values; softmax sums and outputs in fp32. What a
-// row may not see is not read into its sums at all.
-__global__ __launch_bounds__(64) void tree_attention_kernel(DraftArgs a, float scale) {
-  __shared__ float sq[128], sp[64];
-  __shared__ int spage[64];
-  const int b = blockIdx.x, j = blockIdx.y, h = blockIdx.z, D = a.D, lane = threadIdx.x;
-  const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
-  if (j >= s.n) return;
-  const int64_t row = s.r0 + j;
-  const int g = h / (a.n_q / a.n_kv);
-  const uint16_t *q = a.qkv + row * (a.n_q + 2 * a.n_kv) * D + h * D;
-  for (int i = lane; i < D; i += 64) sq[i] = bf2f(q[i]);
-  const int depth = clamp_depth(a.depth[row], a.max_rows);
-  const int lo = a.window > 0 ? max(0, s.ctx + depth - a.window + 1) : 0;
-  const int words = (a.max_rows + 63) / 64;
-  const int64_t blk = (int64_t)kPage * D;
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-  const int first = a.window > 0 ? max(0, s.ctx - a.window + 1) / 64 * 64 : 0;
-  for (int t0 = first; t0 < s.end; t0 += 64) {
-    const int t = t0 + lane;
-    bool see = t < s.end && (t < s.ctx ? t >= lo : (a.mask[row * words + (t - s.ctx) / 64] >> ((t - s.ctx) % 64)) & 1);
-    if (see && t >= s.ctx && a.window > 0)
-      see = clamp_depth(a.depth[s.r0 + t - s.ctx], a.max_rows) > depth - a.window;
-    const int page = see ? page_of(a.table, b, t, a.cols, a.ring, a.pool_pages) : -1;
-    see = page >= 0;
-    float sc = -INFINITY;
-    if (see) {
-      const uint16_t *k = a.pool + (int64_t)page * 2 * a.n_kv * blk + g * blk + (t % kPage) * D;
-      float dot = 0.f;
-      for (int i = 0; i < D; ++i) dot += sq[i] * bf2f(k[i]);
-      sc = dot * scale;
+// ---------------------------------------------------------------- attention
+//
+// o = softmax(q k^T / sqrt(D)) v of each drafted row over the cached tokens in
+// its window and the drafted tokens of its mask. The query vectors of a
+// sequence that share a KV head (its drafted rows times the query heads of the
+// group) are columns of one problem, and up to QT of them (a query tile) share
+// every K/V byte read.
+//
+// Work split: the (sequence, KV head, query tile, 32-token tile) units of the
+// batch are numbered in that order and workgroup r takes the range [r S, (r +
+// 1) S), so ragged contexts and trees load every workgroup alike. Ranges may
+// end inside a task (sequence, KV head, query tile); such a task leaves a
+// record (sums, running maximum, running denominator) per range, and a second
+// kernel joins them.
+//
+// A workgroup is QW waves over one stream of tiles. The tiles (keys and values
+// of two pages) are fetched direct-to-LDS, two or three ahead; each wave holds NQ
+// of the tile's QT = QW * NQ columns in registers and reads every tile once:
+//   S = K Q^T      16x16x32: rows = 16 tokens, columns = 16 query vectors;
+//   softmax        a lane has 8 of the 32 scores of its column. The reference
+//                  point m is moved only when a score exceeds it by 2^8: a
+//                  probability then is at most 2^8 instead of 1, which no fp32
+//                  sum or bf16 rounding feels, and the cross-lane maximum and
+//                  the rescale of the sums are skipped for most tiles;
+//   O += V^T P     16x16x32 over both pages: the k index of lane quad r is
+//                  tokens 4 r .. 4 r + 3 of either page, which is how S leaves
+//                  P in registers and how 8-byte reads of the dim-major V find
+//                  its operand, so P never moves.
+// P is rounded to bf16 for the product (the values it multiplies are bf16); its
+// sum, the maximum and the outputs are fp32.
+//
+// Tiles with a drafted token, a window edge, the end of the sequence or a page
+// outside the pool are masked score by score. In these a value that is not
+// finite is taken out of the product (0 * NaN would reach rows that may not
+// see it) and added only to the columns that see it.
+
+constexpr int kTile = 32;   // tokens per tile: two pages
+constexpr float kSlack = 8.f;
+
+// Tiles of a sequence: [first, first + n). n = 0: nothing to do; the window of
+// a context past the page table may hold no token, one masked tile then.
+__device__ __forceinline__ void tiles_of(const DraftSeq &s, int window, int &first, int &n) {
+  first = n = 0;
+  if (s.end == 0) return;
+  const int last = (s.end - 1) / kTile;
+  if (window > 0) first = min(max(0, s.ctx - window + 1) / kTile, last);
+  n = last - first + 1;
+}
+
+__device__ __forceinline__ uint32_t bits_between(int lo, int hi) {  // bits [lo, hi) of 32
+  lo = max(lo, 0);
+  hi = min(hi, 32);
+  if (lo >= hi) return 0u;
+  return (hi == 32 ? 0xffffffffu : (1u << hi) - 1u) & ~((1u << lo) - 1u);
+}
+
+// Bits [j0, j0 + 32) of a row's mask (zeros before and after it).
+__device__ __forceinline__ uint32_t mask_window(const uint64_t *__restrict__ m, int words, int j0) {
+  if (j0 <= -32 || j0 >= words * 64) return 0u;
+  if (j0 < 0) return (uint32_t)(m[0] << -j0);
+  const int w = j0 / 64, sh = j0 % 64;
+  uint64_t v = m[w] >> sh;
+  if (sh > 32 && w + 1 < words) v |= m[w + 1] << (64 - sh);
+  return (uint32_t)v;
+}
+
+// The two bf16 halves of a dword as weights of what is not finite: 1 for +inf, 64 for -inf, 4096 for NaN, else 0.
+__device__ __forceinline__ uint32_t nonfinite_weight(uint32_t w) {
+  auto of = [](uint32_t h) {
+    return (h & 0x7f80u) != 0x7f80u ? 0u : (h & 0x7fu) ? 0x4580u : (h & 0x8000u) ? 0x4280u : 0x3f80u;
+  };
+  return of(w & 0xffffu) | of(w >> 16) << 16;
+}
+
+// Non-finite bf16 halves of a dword are cleared; true if there were any.
+__device__ __forceinline__ bool drop_nonfinite(uint32_t &w) {
+  const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
+  if (lo) w &= 0xffff0000u;
+  if (hi) w &= 0x0000ffffu;
+  return lo || hi;
+}
+
+template <int D, int NQ, int QW>
+struct TreeShape {
+  static constexpr int QT = NQ * QW;
+  static constexpr int kTileBytes = kTile * D * 2 * 2;
+  static constexpr int kSlots = QW == 1 ? 2 : QW == 2 ? 3 : 4;
+  // Tiles in flight. One wave alone refills the slot it has just read; several need a slot nobody reads.
+  static constexpr int kAhead = QW == 1 ? kSlots : kSlots - 1;
+  static constexpr int kChunks = kTileBytes / 1024;   // 1 KB direct-to-LDS loads of a tile
+  static constexpr int kPerWave = kChunks / QW;
+};
+
+template <int D, int NQ, int QW>
+__global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 64 ? 1 : 2))) void tree_attention_kernel(
+    const DraftArgs a, const int min_tiles, const float scale_log2, float *__restrict__ rec_acc,
+    float2 *__restrict__ rec_ml, int4 *__restrict__ desc) {
+  using Shape = TreeShape<D, NQ, QW>;
+  constexpr int KK = D / 32, NB = D / 16, CB = NQ / 16, QT = Shape::QT;
+  constexpr int NS = Shape::kSlots, AHEAD = Shape::kAhead, LPT = Shape::kPerWave, THREADS = 64 * QW;
+  constexpr int PB = kPage * D * 2;  // bytes of one page block of a head
+  extern __shared__ __align__(16) int smem[];
+  const int B = a.B, group = a.n_q / a.n_kv;
+  int *s_pre = smem, *s_first = smem + B + 1, *s_n = s_first + B;  // units before, first tile, tiles of a sequence
+  uint8_t *const slots = (uint8_t *)smem + ((3 * B + 1) * 4 + 15) / 16 * 16;
+  __shared__ int s_tot[QW];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hl = lane & 15, rq = lane >> 4;
+
+  {  // ---- units before each sequence
+    const int per = (B + THREADS - 1) / THREADS;
+    const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
+    int loc = 0;
+    for (int b = b0; b < b1; ++b) {
+      const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
+      int first, n;
+      tiles_of(s, a.window, first, n);
+      s_first[b] = first;
+      s_n[b] = n;
+      const int u = n * a.n_kv * ((s.n * group + QT - 1) / QT);
+      s_pre[b] = loc;
+      loc += u;
     }
-    const float m_new = fmaxf(m, wave_max(sc));
-    if (__ballot(see) == 0) continue;
-    const float base = m_new == -INFINITY ? 0.f : m_new;
-    const float p = see ? expf(sc - base) : 0.f;
-    const float alpha = expf(m - base);
-    l = l * alpha + wave_sum(p);
-    m = m_new;
-    sp[lane] = p;
-    spage[lane] = page;
+    int inc = loc;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(inc, d, kWave);
+      if (lane >= d) inc += y;
+    }
+    if (lane == 63) s_tot[wave] = inc;
     __syncthreads();
-    o0 *= alpha;
-    o1 *= alpha;
-    for (int i = 0; i < 64; ++i) {
-      if (spage[i] < 0) continue;
-      const uint16_t *v = a.pool + (int64_t)spage[i] * 2 * a.n_kv * blk + (a.n_kv + g) * blk + (t0 + i) % kPage;
-      o0 += sp[i] * bf2f(v[lane * kPage]);
-      if (D > 64) o1 += sp[i] * bf2f(v[(lane + 64) * kPage]);
-    }
+    int run = inc - loc;
+    for (int w = 0; w < wave; ++w) run += s_tot[w];
+    for (int b = b0; b < b1; ++b) s_pre[b] += run;
+    if (tid == THREADS - 1) s_pre[B] = run + loc;
     __syncthreads();
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint16_t *o = a.o + row * a.n_q * D + h * D;
-  o[lane] = f2bf(o0 * inv);
-  if (D > 64) o[lane + 64] = f2bf(o1 * inv);
+  const int total = __builtin_amdgcn_readfirstlane(s_pre[B]);
+  const int S = max(min_tiles, (total + (int)gridDim.x - 1) / (int)gridDim.x);
+  const int r = blockIdx.x;
+  if ((int64_t)r * S >= total) {
+    if (tid == 0) desc[r] = make_int4(0, 0, 0, 0);
+    return;
+  }
+  const int u0 = r * S, n_w = min(total - u0, S);
+
+  // last b with s_pre[b] <= u: a sequence with units when u < total
+  auto find_seq = [&](int u) {
+    int b = 0, hi = B;
+    while (hi - b > 1) {
+      const int mid = (b + hi) >> 1;
+      if (s_pre[mid] <= u) b = mid; else hi = mid;
+    }
+    return b;
+  };
+
+  // Pages and KV head of units [t0, t0 + 32) of the range: lane l has page l % 2 of unit t0 + l / 2 (-1: none).
+  auto gather = [&](int t0, int &page, int &head) {
+    const int t = t0 + (lane >> 1);
+    page = -1;
+    head = 0;
+    if (t >= n_w) return;
+    const int u = u0 + t, b = find_seq(u), n = s_n[b];
+    const int off = u - s_pre[b], task = off / n;
+    const int n_qt = (s_pre[b + 1] - s_pre[b]) / (n * a.n_kv);
+    head = task / n_qt;
+    const int lp = 2 * (s_first[b] + off % n) + (lane & 1);
+    if (a.ring <= 0 && lp >= a.cols) return;
+    page = a.table[(int64_t)b * a.cols + (a.ring > 0 ? lp % a.ring : lp)];
+    if (page >= a.pool_pages) page = -1;
+  };
+  int page_cur, head_cur, page_nxt, head_nxt;
+  gather(0, page_cur, head_cur);
+  gather(32, page_nxt, head_nxt);
+
+  const int64_t blk = (int64_t)kPage * D, page_stride = 2 * (int64_t)a.n_kv * blk;
+  const uint32_t key_off = (hl * D + rq * 8) * 2, val_off = lane * 16;
+  int it = 0, islot = 0;   // next unit to fetch, and its slot
+  uint32_t ok_bits = 0;    // two bits per fetched unit, the next one to be consumed lowest
+
+  // Fetches unit `it` (past the range: the first page of the pool, so that every call makes LPT loads and the waits can
+  // count them). Chunk c of the tile: keys of either page, then values; a wave takes LPT neighbouring ones. Keys: lane l
+  // brings the 16 bytes it reads as its fragment, K[l % 16][kk * 32 + l / 16 * 8 ..]; values: as they lie in the page.
+  auto fetch = [&](int age) {
+    if (it > 0 && (it & 31) == 0) {
+      page_cur = page_nxt;
+      head_cur = head_nxt;
+      gather(it + 32, page_nxt, head_nxt);
+    }
+    const int at = (it & 31) * 2;
+    const int p0 = __builtin_amdgcn_readlane(page_cur, at), p1 = __builtin_amdgcn_readlane(page_cur, at + 1);
+    const int g = __builtin_amdgcn_readlane(head_cur, at);
+    const bool live = it < n_w, ok0 = live && p0 >= 0, ok1 = live && p1 >= 0;
+    ok_bits |= ((ok0 ? 1u : 0u) | (ok1 ? 2u : 0u)) << (2 * age);
+    const uint8_t *base0 = (const uint8_t *)(a.pool + (int64_t)(ok0 ? p0 : 0) * page_stride + g * blk);
+    const uint8_t *base1 = ok1 ? (const uint8_t *)(a.pool + (int64_t)p1 * page_stride + g * blk) : base0;
+    uint8_t *const dst = slots + islot * Shape::kTileBytes;
+#pragma unroll
+    for (int i = 0; i < LPT; ++i) {
+      const int c = wave * LPT + i;             // 2 KK chunks of keys, then 2 KK of values
+      const int part = c / KK, kk = c % KK;     // 0, 1: keys of page 0, 1; 2, 3: values
+      const uint8_t *base = (part & 1 ? base1 : base0) + (part < 2 ? kk * 64 : a.n_kv * blk * 2 + kk * 1024);
+      __builtin_amdgcn_global_load_lds((const void *)(base + (part < 2 ? key_off : val_off)),
+                                       (__attribute__((address_space(3))) void *)(dst + c * 1024), 16, 0, 0);
+    }
+    ++it;
+    islot = islot + 1 == NS ? 0 : islot + 1;
+  };
+
+  // ---- the task being accumulated
+  int cb_seq = __builtin_amdgcn_readfirstlane(find_seq(u0)), ct, c_n, c_first, c_qts;  // sequence, task in it, its tiles
+  int tile;                                                                          // next tile of the task
+  DraftSeq seq;
+  int head, qt, seg_first;            // KV head, query tile, first tile of this range's piece
+  bool first_piece = true;
+  u32x4 q[CB][KK];
+  f32x4 acc[CB][NB];
+  float m[CB], l[CB];
+  int col_row[CB], col_lo[CB];        // drafted row (in the sequence) and first visible token of this lane's columns
+
+  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  auto load_seq = [&]() {
+    c_n = uniform(s_n[cb_seq]);
+    c_first = uniform(s_first[cb_seq]);
+    c_qts = uniform((s_pre[cb_seq + 1] - s_pre[cb_seq]) / (c_n * a.n_kv));
+    const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, cb_seq, a.rows, a.max_rows, a.cols, a.ring);
+    seq.r0 = uniform(s.r0);
+    seq.n = uniform(s.n);
+    seq.ctx = uniform(s.ctx);
+    seq.end = uniform(s.end);
+    seq.cap = s.cap;
+  };
+  auto open_task = [&]() {
+    head = ct / c_qts;
+    qt = ct % c_qts;
+    seg_first = tile;
+    const int cols = seq.n * group;
+    const int64_t row_elems = (int64_t)(a.n_q + 2 * a.n_kv) * D;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const int c = min(qt * QT + wave * NQ + cb * 16 + hl, cols - 1);  // columns past the last repeat it, unwritten
+      const int j = c / group;
+      const uint16_t *src = a.qkv + (seq.r0 + j) * row_elems + (head * group + c % group) * D + rq * 8;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) q[cb][kk] = *(const u32x4 *)(src + kk * 32);
+      col_row[cb] = j;
+      col_lo[cb] = a.window > 0 ? max(0, seq.ctx + clamp_depth(a.depth[seq.r0 + j], a.max_rows) - a.window + 1) : 0;
+      m[cb] = -INFINITY;
+      l[cb] = 0.f;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) acc[cb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // The q rows wait here, once per task: waited for at their first use, the compiler would drain the tiles in flight
+    // in every step.
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  };
+  // Output or record of the task's piece [seg_first, last tile so far]; `whole`: the piece is all of the task.
+  auto close_task = [&](bool whole) {
+    const int cols = seq.n * group;
+    const int rec = 2 * r + (first_piece ? 0 : 1);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      float sum = l[cb];
+      sum += __shfl_xor(sum, 16, kWave);
+      sum += __shfl_xor(sum, 32, kWave);
+      const int at = wave * NQ + cb * 16 + hl, c = qt * QT + at;
+      if (c >= cols) continue;
+      if (whole) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        uint16_t *dst = a.o + ((int64_t)(seq.r0 + c / group) * a.n_q + head * group + c % group) * D + rq * 4;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          u32x2 w;
+          w[0] = pack2(acc[cb][nb][0] * inv, acc[cb][nb][1] * inv);
+          w[1] = pack2(acc[cb][nb][2] * inv, acc[cb][nb][3] * inv);
+          *(u32x2 *)(dst + nb * 16) = w;
+        }
+      } else {
+        float *dst = rec_acc + ((int64_t)rec * QT + at) * D + rq * 4;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(dst + nb * 16) = acc[cb][nb];
+        if (rq == 0) rec_ml[(int64_t)rec * QT + at] = make_float2(m[cb], sum);
+      }
+    }
+  };
+
+  // One tile in LDS at src: tokens [t0, t0 + 32). EDGE: masked score by score.
+  auto step = [&](auto edge, const uint8_t *src, int t0, bool ok0, bool ok1) {
+    constexpr bool EDGE = decltype(edge)::value;
+    f32x4 s[CB][2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      u32x4 k[KK];
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) k[kk] = *(const u32x4 *)(src + half * PB + kk * 1024 + lane * 16);
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk)
+          x = mfma_16x16x32(__builtin_bit_cast(bf16x8, k[kk]), __builtin_bit_cast(bf16x8, q[cb][kk]), x);
+        s[cb][half] = x;
+      }
+    }
+    uint32_t vis[CB];
+    if (EDGE) {
+      __builtin_amdgcn_sched_barrier(0);
+      const int words = (a.max_rows + 63) / 64, seen_end = min(seq.ctx, seq.cap);
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        uint32_t v = mask_window(a.mask + (int64_t)(seq.r0 + col_row[cb]) * words, words, t0 - seq.ctx) &
+                     bits_between(seq.ctx - t0, seq.end - t0);
+        if (a.window > 0) {  // not the drafted tokens `window` positions or more before the row
+          uint32_t left = v;
+          while (left) {
+            const int i = __ffs(left) - 1;
+            left &= left - 1;
+            if (seq.ctx + clamp_depth(a.depth[seq.r0 + t0 + i - seq.ctx], a.max_rows) < col_lo[cb]) v &= ~(1u << i);
+          }
+        }
+        v |= bits_between(col_lo[cb] - t0, seen_end - t0);
+        v &= (ok0 ? 0x0000ffffu : 0u) | (ok1 ? 0xffff0000u : 0u);
+        vis[cb] = v;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!(v >> (half * 16 + rq * 4 + i) & 1)) s[cb][half][i] = -INFINITY;
+      }
+    }
+    float top[CB];
+    bool move = false;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const f32x4 x = s[cb][0], y = s[cb][1];
+      top[cb] = scale_log2 * fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+      move |= top[cb] > m[cb] + kSlack;
+    }
+    if (__any(move)) {  // move the reference points of whole columns
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        float to = fmaxf(m[cb], top[cb]);
+        to = fmaxf(to, __shfl_xor(to, 16, kWave));
+        to = fmaxf(to, __shfl_xor(to, 32, kWave));
+        const float alpha = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[cb] - to);
+        m[cb] = to;
+        l[cb] *= alpha;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) acc[cb][nb] *= alpha;
+      }
+    }
+    u32x4 p[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const float base = m[cb] == -INFINITY ? 0.f : m[cb];
+      float e[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(s[cb][0][i] * scale_log2 - base);
+        e[4 + i] = __builtin_amdgcn_exp2f(s[cb][1][i] * scale_log2 - base);
+      }
+      l[cb] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[cb][i] = pack2(e[2 * i], e[2 * i + 1]);
+    }
+    bool nonfinite = false;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const u32x2 v0 = *(const u32x2 *)(src + 2 * PB + (nb * 16 + hl) * 32 + rq * 8);
+      const u32x2 v1 = *(const u32x2 *)(src + 3 * PB + (nb * 16 + hl) * 32 + rq * 8);
+      u32x4 v = {v0[0], v0[1], v1[0], v1[1]};
+      if (EDGE) {
+        __builtin_amdgcn_sched_barrier(0);  // edge tiles are few: their registers count, not their overlap
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t w = v[i];
+          nonfinite |= drop_nonfinite(w);
+          v[i] = w;
+        }
+      }
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+        acc[cb][nb] = mfma_16x16x32(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p[cb]), acc[cb][nb]);
+    }
+    if (EDGE && __any(nonfinite)) {
+      // Rare. How many +inf, -inf and NaN of each dim a column sees, 32 at most of each, as one product: weights 1, 64
+      // and 4096 times the column's visible tokens. What it sees is added.
+      u32x4 see[CB];
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {  // dword i: tokens (i / 2) * 16 + rq * 4 + (i % 2) * 2 and the next
+          const uint32_t two = vis[cb] >> (i / 2 * 16 + rq * 4 + i % 2 * 2);
+          see[cb][i] = (two & 1 ? 0x3f80u : 0u) | (two & 2 ? 0x3f800000u : 0u);
+        }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const u32x2 v0 = *(const u32x2 *)(src + 2 * PB + (nb * 16 + hl) * 32 + rq * 8);
+        const u32x2 v1 = *(const u32x2 *)(src + 3 * PB + (nb * 16 + hl) * 32 + rq * 8);
+        const u32x4 v = {nonfinite_weight(v0[0]), nonfinite_weight(v0[1]), nonfinite_weight(v1[0]), nonfinite_weight(v1[1])};
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+          const f32x4 n = mfma_16x16x32(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, see[cb]), f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const int c = (int)n[d];
+            if (c & 63) acc[cb][nb][d] += INFINITY;
+            if (c & (63 << 6)) acc[cb][nb][d] -= INFINITY;
+            if (c >> 12) acc[cb][nb][d] = NAN;
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+
+  load_seq();
+  {
+    const int off = u0 - uniform(s_pre[cb_seq]);
+    ct = off / c_n;
+    tile = off % c_n;
+  }
+  open_task();
+  if (tid == 0) desc[r] = make_int4(0, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fetch(i);
+
+  int cslot = 0;
+  for (int t = 0; t < n_w; ++t) {
+    // This wave's loads of tile t have landed once at most those of the tiles behind it are outstanding; after the
+    // barrier everyone's have, and nobody reads the slot the next fetch fills any more.
+    if (QW > 1)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * LPT) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * LPT) : "memory");
+    const bool ok0 = ok_bits & 1, ok1 = ok_bits & 2;
+    ok_bits >>= 2;
+    const uint8_t *src = slots + cslot * Shape::kTileBytes;
+    if (QW > 1) fetch(AHEAD - 1);
+
+    const int t0 = (c_first + tile) * kTile;
+    const int seen_end = min(seq.ctx, seq.cap);  // cached tokens
+    const int lo_most = a.window > 0 ? seq.ctx + a.max_rows - a.window : 0;
+    const bool edge = !(ok0 && ok1) || t0 + kTile > seen_end || t0 < lo_most;
+
+    if (edge)
+      step(std::true_type(), src, t0, ok0, ok1);
+    else
+      step(std::false_type(), src, t0, true, true);
+    if (QW == 1) fetch(AHEAD - 1);
+    cslot = cslot + 1 == NS ? 0 : cslot + 1;
+
+    if (++tile == c_n) {  // the task ends here
+      close_task(seg_first == 0);
+      first_piece = false;
+      tile = 0;
+      if (t + 1 < n_w) {
+        if (++ct == c_qts * a.n_kv) {
+          ct = 0;
+          ++cb_seq;
+          while (uniform(s_pre[cb_seq + 1]) == uniform(s_pre[cb_seq])) ++cb_seq;
+          load_seq();
+        }
+        open_task();
+      }
+    }
+  }
+  // No load may still be writing LDS when the workgroup retires.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if (tile > 0) {  // the range ends inside a task
+    close_task(false);
+    if (tid == 0 && seg_first == 0) {  // ... that began in it: this range names the records to join
+      const int begin = uniform(s_pre[cb_seq]) + ct * c_n, end = begin + c_n;
+      desc[r] = make_int4(cb_seq, ct, (end - 1) / S - r + 1, 2 * r + (first_piece ? 0 : 1));
+    }
+  }
+}
+
+// Joins the records of the tasks that begin in range blockIdx.x and end in a
+// later one: o[d] = sum_i 2^(m_i - M) acc_i[d] / sum_i 2^(m_i - M) l_i. One wave
+// per column, D / 4 lanes per record. Also writes the zeros of sequences that
+// are left alone.
+template <int D>
+__global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const int QT, const float *__restrict__ rec_acc,
+                                                        const float2 *__restrict__ rec_ml, const int4 *__restrict__ desc) {
+  constexpr int LPR = D / 4, RPW = kWave / LPR;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (blockIdx.y == 0) {
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+      if (a.ctx_lens[b] >= 0) continue;
+      const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
+      const int64_t n = (int64_t)s.n * a.n_q * D / 8;
+      u32x4 *dst = (u32x4 *)(a.o + (int64_t)s.r0 * a.n_q * D);
+      for (int64_t i = threadIdx.x; i < n; i += 256) dst[i] = u32x4{0u, 0u, 0u, 0u};
+    }
+  }
+  const int4 e = desc[blockIdx.x];
+  if (e.z <= 1) return;
+  const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, e.x, a.rows, a.max_rows, a.cols, a.ring);
+  const int group = a.n_q / a.n_kv, cols = s.n * group, n_qt = (cols + QT - 1) / QT;
+  const int head = e.y / n_qt, qt = e.y % n_qt;
+  const int at = blockIdx.y * 4 + wave, c = qt * QT + at;
+  if (c >= cols) return;
+  const int d = (lane % LPR) * 4, sub = lane / LPR;
+  // piece i: the record e.w names, then slot 0 of the ranges that follow
+  auto rec = [&](int i) { return ((int64_t)(i == 0 ? e.w : (e.w & ~1) + 2 * i) * QT + at); };
+  float M = -INFINITY;
+  for (int i = lane; i < e.z; i += 64) M = fmaxf(M, rec_ml[rec(i)].x);
+  M = wave_max(M);
+  float sum = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int i = sub; i < e.z; i += RPW) {
+    const float2 ml = rec_ml[rec(i)];
+    const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+    sum += w * ml.y;
+    acc += w * *(const f32x4 *)(rec_acc + rec(i) * D + d);
+  }
+#pragma unroll
+  for (int o = LPR; o < kWave; o <<= 1) {
+    sum += __shfl_xor(sum, o, kWave);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], o, kWave);
+  }
+  if (sub != 0) return;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  u32x2 out;
+  out[0] = pack2(acc[0] * inv, acc[1] * inv);
+  out[1] = pack2(acc[2] * inv, acc[3] * inv);
+  *(u32x2 *)(a.o + ((int64_t)(s.r0 + c / group) * a.n_q + head * group + c % group) * D + d) = out;
+}
+
+template <int D, int NQ, int QW>
+hipError_t go_tree(const DraftArgs &a, const TreePlan &plan, void *ws, hipStream_t s) {
+  using Shape = TreeShape<D, NQ, QW>;
+  static std::atomic<uint64_t> lds_set{0};  // devices whose LDS limit is raised
+  auto lds = [](int B) { return ((3 * (size_t)B + 1) * 4 + 15) / 16 * 16 + (size_t)Shape::kSlots * Shape::kTileBytes; };
+  const auto kern = tree_attention_kernel<D, NQ, QW>;
+  if (hipError_t e = ensure_lds_limit((const void *)kern, lds(kMaxAttnBatch), lds_set); e != hipSuccess) return e;
+  int4 *desc = (int4 *)ws;
+  float2 *ml = (float2 *)(desc + plan.grid);
+  float *acc = (float *)(ml + (size_t)2 * plan.grid * plan.qt);
+  const float scale = (float)(1.4426950408889634 / sqrt((double)D));
+  hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * QW), lds(a.B), s, a, plan.min_tiles, scale, acc, ml, desc);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipLaunchKernelGGL(tree_join_kernel<D>, dim3(plan.grid, plan.qt / 4), dim3(256), 0, s, a, plan.qt, acc, ml, desc);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -120,10 +611,19 @@ hipError_t launch_draft_rope_append(const DraftArgs &a, bool do_rope, bool do_ap
   return hipGetLastError();
 }
 
-hipError_t launch_tree_attention(const DraftArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL(tree_attention_kernel, dim3(a.B, a.max_rows, a.n_q), dim3(64), 0, s, a,
-                     (float)(1.0 / sqrt((double)a.D)));
-  return hipGetLastError();
+hipError_t launch_tree_attention(const DraftArgs &a, const TreePlan &plan, void *ws, hipStream_t s) {
+  auto of_dim = [&](auto d) {
+    constexpr int D = decltype(d)::value;
+    switch (plan.qt) {
+      case 16: return go_tree<D, 16, 1>(a, plan, ws, s);
+      case 32: return go_tree<D, 16, 2>(a, plan, ws, s);
+      case 64: return go_tree<D, 16, 4>(a, plan, ws, s);
+      case 128: return go_tree<D, 32, 4>(a, plan, ws, s);
+      case 256: return go_tree<D, 32, 8>(a, plan, ws, s);
+    }
+    return hipErrorInvalidValue;
+  };
+  return a.D == 128 ? of_dim(std::integral_constant<int, 128>()) : of_dim(std::integral_constant<int, 64>());
 }
 
 }  // namespace ods

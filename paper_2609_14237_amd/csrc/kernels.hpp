@@ -86,7 +86,8 @@ struct DraftArgs {
   float amp, theta;
 };
 hipError_t launch_draft_rope_append(const DraftArgs &a, bool do_rope, bool do_append, hipStream_t s);
-hipError_t launch_tree_attention(const DraftArgs &a, hipStream_t s);
+// ws: tree_ws_bytes(plan, D).
+hipError_t launch_tree_attention(const DraftArgs &a, const TreePlan &plan, void *ws, hipStream_t s);
 
 // Pools of several layers, handed to one launch by value.
 constexpr int kPoolSet = 32;

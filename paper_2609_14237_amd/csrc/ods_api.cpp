@@ -341,8 +341,9 @@ ods_status ods_run_draft(const ods_block *blk, int32_t op_begin, int32_t op_end,
     }
     const OpRef op = op_at(blk, step.begin);
     const DraftArgs a = draft_args(blk, op.layer, batch, draft, st);
-    const hipError_t e = step.attn ? launch_tree_attention(a, stream)
-                                   : launch_draft_rope_append(a, step.rope, step.append, stream);
+    const hipError_t e =
+        step.attn ? launch_tree_attention(a, tree_plan(blk->layers[op.layer].cfg, batch, draft, cus), st->ws, stream)
+                  : launch_draft_rope_append(a, step.rope, step.append, stream);
     const char *what = step.rope && step.append ? "rope+kv_append" : op_kind_name(op.kind);
     if (trace)
       fprintf(stderr, "[ods] layer %d drafted %s B=%d rows=%d -> %s\n", op.layer, what, a.B, a.rows, hipGetErrorString(e));

@@ -124,6 +124,28 @@ DraftStep draft_step(const ods_block *blk, int begin, int op_end) {
   return s;
 }
 
+TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus) {
+  TreePlan p;
+  const int64_t nq = (int64_t)draft->max_rows * (c.n_q / c.n_kv);
+  p.qt = 16;
+  while (p.qt < nq && p.qt < 256) p.qt *= 2;
+  p.max_qt = (int)((nq + p.qt - 1) / p.qt);
+  // tokens of a sequence a layer may read: the table's, or a window with the drafted rows
+  int64_t tokens = (int64_t)kv_map(c, batch).cols * ODS_PAGE_TOKENS;
+  if (c.window > 0) tokens = std::min(tokens, (int64_t)c.window + draft->max_rows + 64);
+  const int64_t units = (int64_t)batch->batch * c.n_kv * p.max_qt * ((tokens + 31) / 32 + 1);
+  p.units_ok = units < (int64_t)1 << 30;
+  const int per_cu = p.qt <= 16 ? (c.head_dim == 64 ? 8 : 4) : p.qt <= 32 ? 4 : p.qt <= 128 ? 2 : 1;
+  p.min_tiles = 2;
+  p.grid = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)std::max(cus, 1) * per_cu, (units + p.min_tiles - 1) / p.min_tiles));
+  return p;
+}
+
+// Per range: a descriptor, and two records of qt columns (maximum and denominator, then the sums).
+size_t tree_ws_bytes(const TreePlan &p, int D) {
+  return (size_t)p.grid * 16 + (size_t)2 * p.grid * p.qt * (D + 2) * sizeof(float);
+}
+
 ods_batch row_batch(const ods_batch *batch, const ods_draft *draft) {
   ods_batch b = *batch;
   b.batch = draft->rows;
@@ -134,7 +156,13 @@ ods_batch row_batch(const ods_batch *batch, const ods_draft *draft) {
 size_t draft_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, const ods_draft *draft,
                       int cus) {
   const ods_batch rb = row_batch(batch, draft);
-  return std::max<size_t>(256, range_ws_bytes(blk, op_begin, op_end, &rb, cus, false));
+  size_t w = std::max<size_t>(256, range_ws_bytes(blk, op_begin, op_end, &rb, cus, false));
+  for (int g = op_begin; g < op_end; ++g) {
+    const OpRef op = op_at(blk, g);
+    const ods_layer_cfg &c = blk->layers[op.layer].cfg;
+    if (op.kind == K_ATTN_CORE) w = std::max(w, tree_ws_bytes(tree_plan(c, batch, draft, cus), c.head_dim));
+  }
+  return w;
 }
 
 ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch,
@@ -147,6 +175,8 @@ ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, con
     const ods_layer_cfg &c = blk->layers[op.layer].cfg;
     if (is_kv_op(op.kind) && (int64_t)draft->rows * c.n_q > INT32_MAX)
       return set_error(ODS_EUNSUPPORTED, "layer %d: draft rows * n_q exceeds 2^31", op.layer);
+    if (op.kind == K_ATTN_CORE && !tree_plan(c, batch, draft, 1).units_ok)
+      return set_error(ODS_EUNSUPPORTED, "layer %d: batch * n_kv * query tiles * window pages exceeds 2^30", op.layer);
   }
   return ODS_OK;
 }

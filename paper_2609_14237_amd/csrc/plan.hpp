@@ -200,6 +200,17 @@ ods_status check_rope(const ods_rope *r, const char *who, bool need_freqs);
 ods_status check_rope_rows(const ods_rope *r, const void *x, int64_t xs, const void *y, int64_t ys, int rows, int heads,
                            const int32_t *pos);
 
+// Attention over drafted rows: query tile width and launch shape.
+struct TreePlan {
+  int qt;         // query vectors of a KV head that share a stream of tiles: 16, 32, 64, 128 or 256
+  int max_qt;     // query tiles of the longest tree
+  int grid;       // workgroups, one range each
+  int min_tiles;  // fewest 32-token tiles in a range
+  bool units_ok;  // batch * n_kv * query tiles * tiles fits the kernel's unit index
+};
+TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus);
+size_t tree_ws_bytes(const TreePlan &p, int D);
+
 inline bool is_kv_op(OpKind k) { return k == K_ROPE || k == K_KV_APPEND || k == K_ATTN_CORE; }
 // One step of a drafted range: a run [begin, end) of operators that only see rows (ods_run_partition on
 // row_batch()), or one of RoPE and/or append, or attention.
