@@ -73,16 +73,18 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
 // A workgroup is QW waves over one stream of tiles. The tiles (keys and values
 // of two pages) are fetched direct-to-LDS, two or three ahead; each wave holds NQ
 // of the tile's QT = QW * NQ columns in registers and reads every tile once:
-//   S = K Q^T      16x16x32: rows = 16 tokens, columns = 16 query vectors;
-//   softmax        a lane has 8 of the 32 scores of its column. The reference
-//                  point m is moved only when a score exceeds it by 2^8: a
-//                  probability then is at most 2^8 instead of 1, which no fp32
-//                  sum or bf16 rounding feels, and the cross-lane maximum and
-//                  the rescale of the sums are skipped for most tiles;
-//   O += V^T P     16x16x32 over both pages: the k index of lane quad r is
-//                  tokens 4 r .. 4 r + 3 of either page, which is how S leaves
-//                  P in registers and how 8-byte reads of the dim-major V find
-//                  its operand, so P never moves.
+//   S = K Q^T      16x16x32, twice: 16 tokens by 16 query vectors. Row 4 r + i of
+//                  product h is token 8 r + 4 h + i of the tile, so lane quad r
+//                  ends with the eight scores of tokens 8 r .. 8 r + 7;
+//   softmax        a lane's eight scores of its column. The reference point m is
+//                  moved only when a score exceeds it by 2^8: a probability then
+//                  is at most 2^8 instead of 1, which no fp32 sum or bf16
+//                  rounding feels, and the maximum across lanes and the rescale
+//                  of the sums are skipped for most tiles;
+//   O += V^T P     16x16x32 over both pages: the k index of lane quad r is tokens
+//                  8 r .. 8 r + 7, which is how S leaves P in registers, and one
+//                  16-byte read of a dim's slots in the dim-major V, so P never
+//                  moves.
 // P is rounded to bf16 for the product (the values it multiplies are bf16); its
 // sum, the maximum and the outputs are fp32.
 //
@@ -91,8 +93,15 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
 // finite is taken out of the product (0 * NaN would reach rows that may not
 // see it) and added only to the columns that see it.
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {  // one conversion for both
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
+}
+
 constexpr int kTile = 32;   // tokens per tile: two pages
 constexpr float kSlack = 8.f;
+constexpr float kNoScore = -1.7e38f;  // reference point before the first score: any score moves it, and 2^(kNoScore - m) is 0
 
 // Tiles of a sequence: [first, first + n). n = 0: nothing to do; the window of
 // a context past the page table may hold no token, one masked tile then.
@@ -232,19 +241,23 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   gather(32, page_nxt, head_nxt);
 
   const int64_t blk = (int64_t)kPage * D, page_stride = 2 * (int64_t)a.n_kv * blk;
-  const uint32_t key_off = (hl * D + rq * 8) * 2, val_off = lane * 16;
+  const uint32_t key_off = (((hl & 4) * 2 + (hl & 3)) * D + rq * 8) * 2, val_off = lane * 16;
   int it = 0, islot = 0;   // next unit to fetch, and its slot
   uint32_t ok_bits = 0;    // two bits per fetched unit, the next one to be consumed lowest
 
+  // Refills the page window before the fetch of every 32nd unit. The wait is here so that the steps between, which the
+  // compiler would otherwise make wait for every load in flight, have none to make.
+  auto next_window = [&]() {
+    page_cur = page_nxt;
+    head_cur = head_nxt;
+    gather(it + 32, page_nxt, head_nxt);
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  };
   // Fetches unit `it` (past the range: the first page of the pool, so that every call makes LPT loads and the waits can
-  // count them). Chunk c of the tile: keys of either page, then values; a wave takes LPT neighbouring ones. Keys: lane l
-  // brings the 16 bytes it reads as its fragment, K[l % 16][kk * 32 + l / 16 * 8 ..]; values: as they lie in the page.
+  // count them). Chunk c of the tile, 1 KB each: 2 KK of keys, then KK of values of either page; a wave takes LPT
+  // neighbouring ones. Keys: lane l brings the 16 bytes it reads as its fragment of product h, K[token 8 (l % 16 / 4) +
+  // 4 h + l % 4][kk * 32 + l / 16 * 8 ..]; values: as they lie in the page.
   auto fetch = [&](int age) {
-    if (it > 0 && (it & 31) == 0) {
-      page_cur = page_nxt;
-      head_cur = head_nxt;
-      gather(it + 32, page_nxt, head_nxt);
-    }
     const int at = (it & 31) * 2;
     const int p0 = __builtin_amdgcn_readlane(page_cur, at), p1 = __builtin_amdgcn_readlane(page_cur, at + 1);
     const int g = __builtin_amdgcn_readlane(head_cur, at);
@@ -255,11 +268,13 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     uint8_t *const dst = slots + islot * Shape::kTileBytes;
 #pragma unroll
     for (int i = 0; i < LPT; ++i) {
-      const int c = wave * LPT + i;             // 2 KK chunks of keys, then 2 KK of values
-      const int part = c / KK, kk = c % KK;     // 0, 1: keys of page 0, 1; 2, 3: values
-      const uint8_t *base = (part & 1 ? base1 : base0) + (part < 2 ? kk * 64 : a.n_kv * blk * 2 + kk * 1024);
-      __builtin_amdgcn_global_load_lds((const void *)(base + (part < 2 ? key_off : val_off)),
-                                       (__attribute__((address_space(3))) void *)(dst + c * 1024), 16, 0, 0);
+      const int c = wave * LPT + i;
+      const void *src;
+      if (c < 2 * KK)
+        src = (hl < 8 ? base0 : base1) + (c / KK * (4 * D * 2) + c % KK * 64) + key_off;
+      else
+        src = (c < 3 * KK ? base0 : base1) + (a.n_kv * blk * 2 + c % KK * 1024) + val_off;
+      __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void *)(dst + c * 1024), 16, 0, 0);
     }
     ++it;
     islot = islot + 1 == NS ? 0 : islot + 1;
@@ -303,7 +318,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       for (int kk = 0; kk < KK; ++kk) q[cb][kk] = *(const u32x4 *)(src + kk * 32);
       col_row[cb] = j;
       col_lo[cb] = a.window > 0 ? max(0, seq.ctx + clamp_depth(a.depth[seq.r0 + j], a.max_rows) - a.window + 1) : 0;
-      m[cb] = -INFINITY;
+      m[cb] = kNoScore;
       l[cb] = 0.f;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) acc[cb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -360,7 +375,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
         s[cb][half] = x;
       }
     }
-    uint32_t vis[CB];
+    uint32_t vis[CB];  // of this lane's eight tokens
     if (EDGE) {
       __builtin_amdgcn_sched_barrier(0);
       const int words = (a.max_rows + 63) / 64, seen_end = min(seq.ctx, seq.cap);
@@ -378,55 +393,55 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
         }
         v |= bits_between(col_lo[cb] - t0, seen_end - t0);
         v &= (ok0 ? 0x0000ffffu : 0u) | (ok1 ? 0xffff0000u : 0u);
-        vis[cb] = v;
+        vis[cb] = v >> (rq * 8);
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!(v >> (half * 16 + rq * 4 + i) & 1)) s[cb][half][i] = -INFINITY;
+        for (int i = 0; i < 8; ++i)
+          if (!(vis[cb] >> i & 1)) s[cb][i / 4][i % 4] = -INFINITY;
       }
     }
-    float top[CB];
+    float e[CB][8];
     bool move = false;
+    auto exponents = [&]() {
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-      const f32x4 x = s[cb][0], y = s[cb][1];
-      top[cb] = scale_log2 * fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
-      move |= top[cb] > m[cb] + kSlack;
-    }
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[cb][i] = s[cb][i / 4][i % 4] * scale_log2 - m[cb];
+    };
+    auto most = [](const float *x) {
+      return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    };
+    exponents();
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) move |= most(e[cb]) > kSlack;
     if (__any(move)) {  // move the reference points of whole columns
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
-        float to = fmaxf(m[cb], top[cb]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[cb][i] = s[cb][i / 4][i % 4] * scale_log2;
+        float to = fmaxf(m[cb], most(e[cb]));
         to = fmaxf(to, __shfl_xor(to, 16, kWave));
         to = fmaxf(to, __shfl_xor(to, 32, kWave));
-        const float alpha = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[cb] - to);
+        const float alpha = __builtin_amdgcn_exp2f(m[cb] - to);
         m[cb] = to;
         l[cb] *= alpha;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) acc[cb][nb] *= alpha;
       }
+      exponents();
     }
     u32x4 p[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
-      const float base = m[cb] == -INFINITY ? 0.f : m[cb];
-      float e[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(s[cb][0][i] * scale_log2 - base);
-        e[4 + i] = __builtin_amdgcn_exp2f(s[cb][1][i] * scale_log2 - base);
-      }
-      l[cb] += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+      for (int i = 0; i < 8; ++i) e[cb][i] = __builtin_amdgcn_exp2f(e[cb][i]);
+      l[cb] += ((e[cb][0] + e[cb][1]) + (e[cb][2] + e[cb][3])) + ((e[cb][4] + e[cb][5]) + (e[cb][6] + e[cb][7]));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[cb][i] = pack2(e[2 * i], e[2 * i + 1]);
+      for (int i = 0; i < 4; ++i) p[cb][i] = pack_pair(e[cb][2 * i], e[cb][2 * i + 1]);
     }
     bool nonfinite = false;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const u32x2 v0 = *(const u32x2 *)(src + 2 * PB + (nb * 16 + hl) * 32 + rq * 8);
-      const u32x2 v1 = *(const u32x2 *)(src + 3 * PB + (nb * 16 + hl) * 32 + rq * 8);
-      u32x4 v = {v0[0], v0[1], v1[0], v1[1]};
+      u32x4 v = *(const u32x4 *)(src + (2 + (rq >> 1)) * PB + (nb * 16 + hl) * 32 + (rq & 1) * 16);
       if (EDGE) {
         __builtin_amdgcn_sched_barrier(0);  // edge tiles are few: their registers count, not their overlap
 #pragma unroll
@@ -447,15 +462,13 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {  // dword i: tokens (i / 2) * 16 + rq * 4 + (i % 2) * 2 and the next
-          const uint32_t two = vis[cb] >> (i / 2 * 16 + rq * 4 + i % 2 * 2);
-          see[cb][i] = (two & 1 ? 0x3f80u : 0u) | (two & 2 ? 0x3f800000u : 0u);
-        }
+        for (int i = 0; i < 4; ++i)
+          see[cb][i] = (vis[cb] >> (2 * i) & 1 ? 0x3f80u : 0u) | (vis[cb] >> (2 * i) & 2 ? 0x3f800000u : 0u);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const u32x2 v0 = *(const u32x2 *)(src + 2 * PB + (nb * 16 + hl) * 32 + rq * 8);
-        const u32x2 v1 = *(const u32x2 *)(src + 3 * PB + (nb * 16 + hl) * 32 + rq * 8);
-        const u32x4 v = {nonfinite_weight(v0[0]), nonfinite_weight(v0[1]), nonfinite_weight(v1[0]), nonfinite_weight(v1[1])};
+        u32x4 v = *(const u32x4 *)(src + (2 + (rq >> 1)) * PB + (nb * 16 + hl) * 32 + (rq & 1) * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = nonfinite_weight(v[i]);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
           const f32x4 n = mfma_16x16x32(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, see[cb]), f32x4{0.f, 0.f, 0.f, 0.f});
@@ -483,36 +496,51 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) fetch(i);
 
-  int cslot = 0;
-  for (int t = 0; t < n_w; ++t) {
-    // This wave's loads of tile t have landed once at most those of the tiles behind it are outstanding; after the
-    // barrier everyone's have, and nobody reads the slot the next fetch fills any more.
-    if (QW > 1)
+  int cslot = 0, t = 0;
+  // Waits for tile t and fetches ahead. This wave's loads of tile t have landed once at most those of the tiles behind it
+  // are outstanding; after the barrier everyone's have, and nobody reads the slot the next fetch fills any more.
+  auto arrive = [&]() {
+    if (QW > 1) {
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * LPT) : "memory");
-    else
+      ok_bits >>= 2;
+      fetch(AHEAD - 1);
+    } else {
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * LPT) : "memory");
-    const bool ok0 = ok_bits & 1, ok1 = ok_bits & 2;
-    ok_bits >>= 2;
-    const uint8_t *src = slots + cslot * Shape::kTileBytes;
-    if (QW > 1) fetch(AHEAD - 1);
-
-    const int t0 = (c_first + tile) * kTile;
-    const int seen_end = min(seq.ctx, seq.cap);  // cached tokens
-    const int lo_most = a.window > 0 ? seq.ctx + a.max_rows - a.window : 0;
-    const bool edge = !(ok0 && ok1) || t0 + kTile > seen_end || t0 < lo_most;
-
-    if (edge)
-      step(std::true_type(), src, t0, ok0, ok1);
-    else
-      step(std::false_type(), src, t0, true, true);
-    if (QW == 1) fetch(AHEAD - 1);
+    }
+    return (const uint8_t *)(slots + cslot * Shape::kTileBytes);
+  };
+  auto leave = [&]() {
+    if (QW == 1) {
+      ok_bits >>= 2;
+      fetch(AHEAD - 1);
+    }
     cslot = cslot + 1 == NS ? 0 : cslot + 1;
-
-    if (++tile == c_n) {  // the task ends here
+    ++tile;
+    ++t;
+  };
+  while (t < n_w) {
+    if ((it & 31) == 0) next_window();
+    // Tiles that need no mask, up to the next page window: all of it cached tokens that every row sees, pages in the pool.
+    const int lo_most = a.window > 0 ? seq.ctx + a.max_rows - a.window : 0;
+    const int full_end = min(seq.ctx, seq.cap) / kTile - c_first, full_begin = (max(lo_most, 0) + kTile - 1) / kTile - c_first;
+    const int run = tile < full_begin ? 0 : min(min(n_w - t, full_end - tile), 32 - (it & 31));
+    int done = 0;
+    for (; done < run && (ok_bits & 3) == 3; ++done) {
+      const uint8_t *src = arrive();
+      step(std::false_type(), src, 0, true, true);
+      leave();
+    }
+    if (done == 0) {
+      const bool ok0 = ok_bits & 1, ok1 = ok_bits & 2;
+      const uint8_t *src = arrive();
+      step(std::true_type(), src, (c_first + tile) * kTile, ok0, ok1);
+      leave();
+    }
+    if (tile == c_n) {  // the task ends here
       close_task(seg_first == 0);
       first_piece = false;
       tile = 0;
-      if (t + 1 < n_w) {
+      if (t < n_w) {
         if (++ct == c_qts * a.n_kv) {
           ct = 0;
           ++cb_seq;
@@ -569,7 +597,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   for (int i = sub; i < e.z; i += RPW) {
     const float2 ml = rec_ml[rec(i)];
-    const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+    const float w = __builtin_amdgcn_exp2f(ml.x - M);
     sum += w * ml.y;
     acc += w * *(const f32x4 *)(rec_acc + rec(i) * D + d);
   }
