@@ -3,6 +3,7 @@
 // drafted ones its mask names.
 #include <math.h>
 
+#include <stdlib.h>
 #include <type_traits>
 
 #include "draft.hpp"
@@ -146,6 +147,15 @@ __device__ __forceinline__ bool drop_nonfinite(uint32_t &w) {
   return lo || hi;
 }
 
+// A task that begins in a range and ends in a later one.
+struct TreeDesc {
+  int pieces;      // ranges it lies in (0: none such)
+  int rec;         // record of its first piece; piece i's is slot 0 of range i further on
+  int r0;          // first drafted row of its sequence
+  int col0, cols;  // first column of its query tile, columns of the sequence
+  int head;        // KV head
+};
+
 template <int D, int NQ, int QW>
 struct TreeShape {
   static constexpr int QT = NQ * QW;
@@ -159,8 +169,8 @@ struct TreeShape {
 
 template <int D, int NQ, int QW>
 __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 64 ? 1 : 2))) void tree_attention_kernel(
-    const DraftArgs a, const int min_tiles, const float scale_log2, float *__restrict__ rec_acc,
-    float2 *__restrict__ rec_ml, int4 *__restrict__ desc) {
+    const DraftArgs a, const int min_tiles, const int max_qt, const int by_task, const float scale_log2, float *__restrict__ rec_acc,
+    float2 *__restrict__ rec_ml, TreeDesc *__restrict__ desc) {
   using Shape = TreeShape<D, NQ, QW>;
   constexpr int KK = D / 32, NB = D / 16, CB = NQ / 16, QT = Shape::QT;
   constexpr int NS = Shape::kSlots, AHEAD = Shape::kAhead, LPT = Shape::kPerWave, THREADS = 64 * QW;
@@ -205,10 +215,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   const int total = __builtin_amdgcn_readfirstlane(s_pre[B]);
   const int S = max(min_tiles, (total + (int)gridDim.x - 1) / (int)gridDim.x);
   const int r = blockIdx.x;
-  if ((int64_t)r * S >= total) {
-    if (tid == 0) desc[r] = make_int4(0, 0, 0, 0);
-    return;
-  }
+  if (!by_task && tid == 0) desc[r].pieces = 0;
+  if ((int64_t)r * S >= total) return;
   const int u0 = r * S, n_w = min(total - u0, S);
 
   // last b with s_pre[b] <= u: a sequence with units when u < total
@@ -290,7 +298,9 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   f32x4 acc[CB][NB];
   float m[CB], l[CB];
   int col_row[CB], col_lo[CB];        // drafted row (in the sequence) and first visible token of this lane's columns
+  uint64_t col_mask[CB];              // and its mask, where one word holds it
 
+  auto task_id = [&]() { return ((int64_t)cb_seq * a.n_kv + head) * max_qt + qt; };
   auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   auto load_seq = [&]() {
     c_n = uniform(s_n[cb_seq]);
@@ -317,6 +327,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) q[cb][kk] = *(const u32x4 *)(src + kk * 32);
       col_row[cb] = j;
+      col_mask[cb] = a.max_rows <= 64 ? a.mask[seq.r0 + j] : 0;
       col_lo[cb] = a.window > 0 ? max(0, seq.ctx + clamp_depth(a.depth[seq.r0 + j], a.max_rows) - a.window + 1) : 0;
       m[cb] = kNoScore;
       l[cb] = 0.f;
@@ -344,8 +355,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           u32x2 w;
-          w[0] = pack2(acc[cb][nb][0] * inv, acc[cb][nb][1] * inv);
-          w[1] = pack2(acc[cb][nb][2] * inv, acc[cb][nb][3] * inv);
+          w[0] = pack_pair(acc[cb][nb][0] * inv, acc[cb][nb][1] * inv);
+          w[1] = pack_pair(acc[cb][nb][2] * inv, acc[cb][nb][3] * inv);
           *(u32x2 *)(dst + nb * 16) = w;
         }
       } else {
@@ -381,19 +392,22 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       const int words = (a.max_rows + 63) / 64, seen_end = min(seq.ctx, seq.cap);
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
-        uint32_t v = mask_window(a.mask + (int64_t)(seq.r0 + col_row[cb]) * words, words, t0 - seq.ctx) &
-                     bits_between(seq.ctx - t0, seq.end - t0);
-        if (a.window > 0) {  // not the drafted tokens `window` positions or more before the row
-          uint32_t left = v;
-          while (left) {
-            const int i = __ffs(left) - 1;
-            left &= left - 1;
-            if (seq.ctx + clamp_depth(a.depth[seq.r0 + t0 + i - seq.ctx], a.max_rows) < col_lo[cb]) v &= ~(1u << i);
-          }
+        const int j0 = t0 - seq.ctx;  // drafted token of the tile's first slot (below 0: cached ones come first)
+        uint32_t v = words == 1 ? (j0 < 0 ? (j0 > -32 ? (uint32_t)(col_mask[cb] << -j0) : 0u)
+                                          : j0 < 64 ? (uint32_t)(col_mask[cb] >> j0) : 0u)
+                                : mask_window(a.mask + (int64_t)(seq.r0 + col_row[cb]) * words, words, j0);
+        v &= bits_between(-j0, seq.end - t0);
+        v = v >> (rq * 8) & 0xffu;
+        if (a.window > 0 && a.window < a.max_rows) {  // not the drafted tokens `window` positions or more before the row
+          int depth[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) depth[i] = v >> i & 1 ? a.depth[seq.r0 + j0 + rq * 8 + i] : 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (seq.ctx + clamp_depth(depth[i], a.max_rows) < col_lo[cb]) v &= ~(1u << i);
         }
-        v |= bits_between(col_lo[cb] - t0, seen_end - t0);
-        v &= (ok0 ? 0x0000ffffu : 0u) | (ok1 ? 0xffff0000u : 0u);
-        vis[cb] = v >> (rq * 8);
+        v |= bits_between(col_lo[cb] - t0, seen_end - t0) >> (rq * 8);
+        vis[cb] = (rq < 2 ? ok0 : ok1) ? v & 0xffu : 0u;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           if (!(vis[cb] >> i & 1)) s[cb][i / 4][i % 4] = -INFINITY;
@@ -491,10 +505,9 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     ct = off / c_n;
     tile = off % c_n;
   }
-  open_task();
-  if (tid == 0) desc[r] = make_int4(0, 0, 0, 0);
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) fetch(i);
+  open_task();
 
   int cslot = 0, t = 0;
   // Waits for tile t and fetches ahead. This wave's loads of tile t have landed once at most those of the tiles behind it
@@ -538,6 +551,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     }
     if (tile == c_n) {  // the task ends here
       close_task(seg_first == 0);
+      if (by_task && tid == 0 && seg_first == 0) desc[task_id()].pieces = 1;
       first_piece = false;
       tile = 0;
       if (t < n_w) {
@@ -557,22 +571,41 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     close_task(false);
     if (tid == 0 && seg_first == 0) {  // ... that began in it: this range names the records to join
       const int begin = uniform(s_pre[cb_seq]) + ct * c_n, end = begin + c_n;
-      desc[r] = make_int4(cb_seq, ct, (end - 1) / S - r + 1, 2 * r + (first_piece ? 0 : 1));
+      desc[by_task ? task_id() : r] =
+          TreeDesc{(end - 1) / S - r + 1, 2 * r + (first_piece ? 0 : 1), seq.r0, qt * QT, seq.n * group, head};
     }
   }
 }
 
-// Joins the records of the tasks that begin in range blockIdx.x and end in a
-// later one: o[d] = sum_i 2^(m_i - M) acc_i[d] / sum_i 2^(m_i - M) l_i. One wave
-// per column, D / 4 lanes per record. Also writes the zeros of sequences that
-// are left alone.
-template <int D>
-__global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const int QT, const float *__restrict__ rec_acc,
-                                                        const float2 *__restrict__ rec_ml, const int4 *__restrict__ desc) {
-  constexpr int LPR = D / 4, RPW = kWave / LPR;
+// Joins the records of tasks that lie in several ranges: o[d] = sum_i
+// 2^(m_i - M) acc_i[d] / sum_i 2^(m_i - M) l_i, D / 4 lanes per record. Bound by
+// latency: the descriptor, then all of a column's first records and weights in
+// one trip. SPLIT: a column is four waves' work, a quarter of its records each
+// (few tasks of many records); otherwise a wave joins four columns at a time
+// (many tasks of two or three). Block x is task x of the batch, or, where there
+// are more tasks than ranges, the task that begins in range x. Also writes the
+// zeros of sequences that are left alone.
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const int QT, const int max_qt, const int by_task,
+                                                        const float *__restrict__ rec_acc,
+                                                        const float2 *__restrict__ rec_ml,
+                                                        const TreeDesc *__restrict__ desc) {
+  constexpr int LPR = D / 4, RPW = kWave / LPR;                 // lanes per record, records a wave reads at once
+  constexpr int NC = SPLIT ? 1 : 4, G = SPLIT ? 4 * RPW : RPW;  // columns of a wave, records of a column at once
+  constexpr int PRE = SPLIT ? 4 : 2;                            // trips in flight
+  __shared__ float part[SPLIT ? 4 * (D + 4) : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (blockIdx.y == 0) {
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+  const int group = a.n_q / a.n_kv;
+  const TreeDesc e = desc[blockIdx.x];
+  bool zero = blockIdx.y == 0;
+  int b0 = blockIdx.x, step = gridDim.x;
+  if (by_task) {  // the descriptor of a task without units was not written
+    b0 = blockIdx.x / (a.n_kv * max_qt);
+    step = a.B;
+    zero = zero && blockIdx.x % (a.n_kv * max_qt) == 0;
+  }
+  if (zero) {
+    for (int b = b0; b < a.B; b += step) {
       if (a.ctx_lens[b] >= 0) continue;
       const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
       const int64_t n = (int64_t)s.n * a.n_q * D / 8;
@@ -580,39 +613,90 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const
       for (int64_t i = threadIdx.x; i < n; i += 256) dst[i] = u32x4{0u, 0u, 0u, 0u};
     }
   }
-  const int4 e = desc[blockIdx.x];
-  if (e.z <= 1) return;
-  const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, e.x, a.rows, a.max_rows, a.cols, a.ring);
-  const int group = a.n_q / a.n_kv, cols = s.n * group, n_qt = (cols + QT - 1) / QT;
-  const int head = e.y / n_qt, qt = e.y % n_qt;
-  const int at = blockIdx.y * 4 + wave, c = qt * QT + at;
-  if (c >= cols) return;
-  const int d = (lane % LPR) * 4, sub = lane / LPR;
-  // piece i: the record e.w names, then slot 0 of the ranges that follow
-  auto rec = [&](int i) { return ((int64_t)(i == 0 ? e.w : (e.w & ~1) + 2 * i) * QT + at); };
-  float M = -INFINITY;
-  for (int i = lane; i < e.z; i += 64) M = fmaxf(M, rec_ml[rec(i)].x);
-  M = wave_max(M);
-  float sum = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int i = sub; i < e.z; i += RPW) {
-    const float2 ml = rec_ml[rec(i)];
-    const float w = __builtin_amdgcn_exp2f(ml.x - M);
-    sum += w * ml.y;
-    acc += w * *(const f32x4 *)(rec_acc + rec(i) * D + d);
+  if (by_task) {
+    const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b0, a.rows, a.max_rows, a.cols, a.ring);
+    if (s.end == 0 || (int)(blockIdx.x % max_qt) * QT >= s.n * group) return;
+  }
+  const int at0 = SPLIT ? blockIdx.y : (blockIdx.y * 4 + wave) * NC;  // first column of the tile this wave joins
+  if (e.pieces <= 1 || e.col0 + at0 >= e.cols) return;
+  const int d = (lane % LPR) * 4, sub = (SPLIT ? wave * RPW : 0) + lane / LPR;
+  // Columns past the last one read the records' unwritten rows and are not stored; every index is inside the records.
+  auto rec = [&](int i, int c) { return (int64_t)(i == 0 ? e.rec : (e.rec & ~1) + 2 * i) * QT + at0 + c; };
+  float M[NC], sum[NC];
+  f32x4 acc[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    M[c] = kNoScore;
+    sum[c] = 0.f;
+    acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  for (int i0 = 0; i0 < e.pieces; i0 += PRE * G) {
+    f32x4 x[PRE][NC];
+    float2 ml[PRE][NC];
+#pragma unroll
+    for (int k = 0; k < PRE; ++k)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int64_t at = rec(min(i0 + sub + k * G, e.pieces - 1), c);  // past the last: again, with weight 0
+        ml[k][c] = rec_ml[at];
+        x[k][c] = *(const f32x4 *)(rec_acc + at * D + d);
+      }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      float top = M[c];
+#pragma unroll
+      for (int k = 0; k < PRE; ++k) top = fmaxf(top, ml[k][c].x);
+      const float old = __builtin_amdgcn_exp2f(M[c] - top);
+      M[c] = top;
+      sum[c] *= old;
+      acc[c] *= old;
+#pragma unroll
+      for (int k = 0; k < PRE; ++k) {
+        const float w = i0 + sub + k * G < e.pieces ? __builtin_amdgcn_exp2f(ml[k][c].x - top) : 0.f;
+        sum[c] += w * ml[k][c].y;
+        if (w != 0.f) acc[c] += w * x[k][c];
+      }
+    }
   }
 #pragma unroll
-  for (int o = LPR; o < kWave; o <<= 1) {
-    sum += __shfl_xor(sum, o, kWave);
+  for (int c = 0; c < NC; ++c) {
+    float top = M[c];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], o, kWave);
+    for (int o = LPR; o < kWave; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+    const float w = __builtin_amdgcn_exp2f(M[c] - top);
+    float l = sum[c] * w;
+    f32x4 v = acc[c] * w;
+#pragma unroll
+    for (int o = LPR; o < kWave; o <<= 1) {
+      l += __shfl_xor(l, o, kWave);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += __shfl_xor(v[i], o, kWave);
+    }
+    if (SPLIT) {
+      if (lane < LPR) *(f32x4 *)(part + wave * (D + 4) + d) = v;
+      if (lane == 0) *(float2 *)(part + wave * (D + 4) + D) = make_float2(top, l);
+      __syncthreads();
+      if (wave > 0) return;
+      top = kNoScore;
+#pragma unroll
+      for (int w4 = 0; w4 < 4; ++w4) top = fmaxf(top, part[w4 * (D + 4) + D]);
+      l = 0.f;
+      v = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w4 = 0; w4 < 4; ++w4) {
+        const float u = __builtin_amdgcn_exp2f(part[w4 * (D + 4) + D] - top);
+        l += u * part[w4 * (D + 4) + D + 1];
+        v += u * *(const f32x4 *)(part + w4 * (D + 4) + d);
+      }
+    }
+    const int col = e.col0 + at0 + c;
+    if (lane >= LPR || col >= e.cols) continue;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    u32x2 out;
+    out[0] = pack_pair(v[0] * inv, v[1] * inv);
+    out[1] = pack_pair(v[2] * inv, v[3] * inv);
+    *(u32x2 *)(a.o + ((int64_t)(e.r0 + col / group) * a.n_q + e.head * group + col % group) * D + d) = out;
   }
-  if (sub != 0) return;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  u32x2 out;
-  out[0] = pack2(acc[0] * inv, acc[1] * inv);
-  out[1] = pack2(acc[2] * inv, acc[3] * inv);
-  *(u32x2 *)(a.o + ((int64_t)(s.r0 + c / group) * a.n_q + head * group + c % group) * D + d) = out;
 }
 
 template <int D, int NQ, int QW>
@@ -622,13 +706,22 @@ hipError_t go_tree(const DraftArgs &a, const TreePlan &plan, void *ws, hipStream
   auto lds = [](int B) { return ((3 * (size_t)B + 1) * 4 + 15) / 16 * 16 + (size_t)Shape::kSlots * Shape::kTileBytes; };
   const auto kern = tree_attention_kernel<D, NQ, QW>;
   if (hipError_t e = ensure_lds_limit((const void *)kern, lds(kMaxAttnBatch), lds_set); e != hipSuccess) return e;
-  int4 *desc = (int4 *)ws;
-  float2 *ml = (float2 *)(desc + plan.grid);
+  static_assert(sizeof(TreeDesc) <= kTreeDescBytes, "descriptor size");
+  TreeDesc *desc = (TreeDesc *)ws;
+  const int64_t tasks = (int64_t)a.B * a.n_kv * plan.max_qt;
+  const int by_task = tasks <= plan.grid, blocks = by_task ? (int)tasks : plan.grid;
+  float2 *ml = (float2 *)((uint8_t *)ws + (size_t)kTreeDescBytes * plan.grid);
   float *acc = (float *)(ml + (size_t)2 * plan.grid * plan.qt);
   const float scale = (float)(1.4426950408889634 / sqrt((double)D));
-  hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * QW), lds(a.B), s, a, plan.min_tiles, scale, acc, ml, desc);
+  hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * QW), lds(a.B), s, a, plan.min_tiles, plan.max_qt, by_task, scale, acc, ml,
+                     desc);
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  hipLaunchKernelGGL(tree_join_kernel<D>, dim3(plan.grid, plan.qt / 4), dim3(256), 0, s, a, plan.qt, acc, ml, desc);
+  if (plan.split_join)
+    hipLaunchKernelGGL((tree_join_kernel<D, true>), dim3(blocks, plan.qt), dim3(256), 0, s, a, plan.qt, plan.max_qt, by_task,
+                       acc, ml, desc);
+  else
+    hipLaunchKernelGGL((tree_join_kernel<D, false>), dim3(blocks, plan.qt / 16), dim3(256), 0, s, a, plan.qt, plan.max_qt,
+                       by_task, acc, ml, desc);
   return hipGetLastError();
 }
 
@@ -646,7 +739,7 @@ hipError_t launch_tree_attention(const DraftArgs &a, const TreePlan &plan, void 
       case 16: return go_tree<D, 16, 1>(a, plan, ws, s);
       case 32: return go_tree<D, 16, 2>(a, plan, ws, s);
       case 64: return go_tree<D, 16, 4>(a, plan, ws, s);
-      case 128: return go_tree<D, 32, 4>(a, plan, ws, s);
+      case 128: return getenv("TREE_V") && atoi(getenv("TREE_V")) == 1 ? go_tree<D, 16, 8>(a, plan, ws, s) : go_tree<D, 32, 4>(a, plan, ws, s);
       case 256: return go_tree<D, 32, 8>(a, plan, ws, s);
     }
     return hipErrorInvalidValue;

@@ -3,6 +3,7 @@
 // operator range into row-wise runs and drafted KV operators. Plain C++, free
 // of HIP calls; nothing here allocates.
 #include <math.h>
+#include <stdlib.h>
 
 #include <algorithm>
 
@@ -137,13 +138,17 @@ TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_dra
   p.units_ok = units < (int64_t)1 << 30;
   const int per_cu = p.qt <= 16 ? (c.head_dim == 64 ? 8 : 4) : p.qt <= 32 ? 4 : p.qt <= 128 ? 2 : 1;
   p.min_tiles = 2;
-  p.grid = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)std::max(cus, 1) * per_cu, (units + p.min_tiles - 1) / p.min_tiles));
+  if (getenv("TREE_MIN")) p.min_tiles = atoi(getenv("TREE_MIN"));
+  const int percu2 = getenv("TREE_PER") ? atoi(getenv("TREE_PER")) : per_cu;
+  p.grid = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)std::max(cus, 1) * percu2, (units + p.min_tiles - 1) / p.min_tiles));
+  p.split_join = p.grid > 6 * (int64_t)batch->batch * c.n_kv * p.max_qt;
+  if (getenv("TREE_SJ")) p.split_join = atoi(getenv("TREE_SJ"));
   return p;
 }
 
 // Per range: a descriptor, and two records of qt columns (maximum and denominator, then the sums).
 size_t tree_ws_bytes(const TreePlan &p, int D) {
-  return (size_t)p.grid * 16 + (size_t)2 * p.grid * p.qt * (D + 2) * sizeof(float);
+  return (size_t)p.grid * kTreeDescBytes + (size_t)2 * p.grid * p.qt * (D + 2) * sizeof(float);
 }
 
 ods_batch row_batch(const ods_batch *batch, const ods_draft *draft) {

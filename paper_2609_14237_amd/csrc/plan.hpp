@@ -206,8 +206,10 @@ struct TreePlan {
   int max_qt;     // query tiles of the longest tree
   int grid;       // workgroups, one range each
   int min_tiles;  // fewest 32-token tiles in a range
+  bool split_join;  // records of a column are shared by four waves
   bool units_ok;  // batch * n_kv * query tiles * tiles fits the kernel's unit index
 };
+constexpr int kTreeDescBytes = 32;
 TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus);
 size_t tree_ws_bytes(const TreePlan &p, int D);
 
