@@ -160,9 +160,8 @@ template <int D, int NQ, int QW>
 struct TreeShape {
   static constexpr int QT = NQ * QW;
   static constexpr int kTileBytes = kTile * D * 2 * 2;
-  static constexpr int kSlots = QW == 1 ? 2 : QW == 2 ? 3 : 4;
-  // Tiles in flight. One wave alone refills the slot it has just read; several need a slot nobody reads.
-  static constexpr int kAhead = QW == 1 ? kSlots : kSlots - 1;
+  // Tiles in LDS. Two workgroups of 4 waves share a compute unit, or 4 (D = 128) or 8 of one wave; 8 waves have it alone.
+  static constexpr int kSlots = QW == 1 ? 2 : QW == 8 ? (D == 64 ? 8 : 6) : (D == 64 ? 6 : 4);
   static constexpr int kChunks = kTileBytes / 1024;   // 1 KB direct-to-LDS loads of a tile
   static constexpr int kPerWave = kChunks / QW;
 };
@@ -173,7 +172,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     float2 *__restrict__ rec_ml, TreeDesc *__restrict__ desc) {
   using Shape = TreeShape<D, NQ, QW>;
   constexpr int KK = D / 32, NB = D / 16, CB = NQ / 16, QT = Shape::QT;
-  constexpr int NS = Shape::kSlots, AHEAD = Shape::kAhead, LPT = Shape::kPerWave, THREADS = 64 * QW;
+  constexpr int NS = Shape::kSlots, LPT = Shape::kPerWave, THREADS = 64 * QW;
   constexpr int PB = kPage * D * 2;  // bytes of one page block of a head
   extern __shared__ __align__(16) int smem[];
   const int B = a.B, group = a.n_q / a.n_kv;
@@ -261,18 +260,25 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     gather(it + 32, page_nxt, head_nxt);
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
   };
-  // Fetches unit `it` (past the range: the first page of the pool, so that every call makes LPT loads and the waits can
-  // count them). Chunk c of the tile, 1 KB each: 2 KK of keys, then KK of values of either page; a wave takes LPT
-  // neighbouring ones. Keys: lane l brings the 16 bytes it reads as its fragment of product h, K[token 8 (l % 16 / 4) +
-  // 4 h + l % 4][kk * 32 + l / 16 * 8 ..]; values: as they lie in the page.
-  auto fetch = [&](int age) {
+  // Fetching unit `it` (past the range: the first page of the pool, so that every fetch makes LPT loads and the waits can
+  // count them) in two steps: where its pages are, scalar work that hides behind products, and the loads. Chunk c of the
+  // tile, 1 KB each: 2 KK of keys, then KK of values of either page; a wave takes LPT neighbouring ones. Keys: lane l
+  // brings the 16 bytes it reads as its fragment of product h, K[token 8 (l % 16 / 4) + 4 h + l % 4][kk * 32 + l / 16 * 8
+  // ..]; values: as they lie in the page.
+  const uint8_t *base0 = nullptr, *base1 = nullptr;
+  uint32_t ok_next = 0;
+  auto find_pages = [&]() {
     const int at = (it & 31) * 2;
     const int p0 = __builtin_amdgcn_readlane(page_cur, at), p1 = __builtin_amdgcn_readlane(page_cur, at + 1);
     const int g = __builtin_amdgcn_readlane(head_cur, at);
     const bool live = it < n_w, ok0 = live && p0 >= 0, ok1 = live && p1 >= 0;
-    ok_bits |= ((ok0 ? 1u : 0u) | (ok1 ? 2u : 0u)) << (2 * age);
-    const uint8_t *base0 = (const uint8_t *)(a.pool + (int64_t)(ok0 ? p0 : 0) * page_stride + g * blk);
-    const uint8_t *base1 = ok1 ? (const uint8_t *)(a.pool + (int64_t)p1 * page_stride + g * blk) : base0;
+    ok_next = (ok0 ? 1u : 0u) | (ok1 ? 2u : 0u);
+    base0 = (const uint8_t *)(a.pool + (int64_t)(ok0 ? p0 : 0) * page_stride + g * blk);
+    base1 = ok1 ? (const uint8_t *)(a.pool + (int64_t)p1 * page_stride + g * blk) : base0;
+    ++it;
+  };
+  auto issue = [&](int age) {
+    ok_bits |= ok_next << (2 * age);
     uint8_t *const dst = slots + islot * Shape::kTileBytes;
 #pragma unroll
     for (int i = 0; i < LPT; ++i) {
@@ -284,7 +290,6 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
         src = (c < 3 * KK ? base0 : base1) + (a.n_kv * blk * 2 + c % KK * 1024) + val_off;
       __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void *)(dst + c * 1024), 16, 0, 0);
     }
-    ++it;
     islot = islot + 1 == NS ? 0 : islot + 1;
   };
 
@@ -296,6 +301,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   bool first_piece = true;
   u32x4 q[CB][KK];
   f32x4 acc[CB][NB];
+  u32x4 kf[2][KK], vf[NB], p[CB];     // operands of the next products: keys, values and probabilities
+  f32x4 s[CB][2];
   float m[CB], l[CB];
   int col_row[CB], col_lo[CB];        // drafted row (in the sequence) and first visible token of this lane's columns
   uint64_t col_mask[CB];              // and its mask, where one word holds it
@@ -334,6 +341,10 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) acc[cb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) p[cb] = u32x4{0u, 0u, 0u, 0u};  // the first products add nothing
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) vf[nb] = u32x4{0u, 0u, 0u, 0u};
     // The q rows wait here, once per task: waited for at their first use, the compiler would drain the tiles in flight
     // in every step.
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
@@ -368,27 +379,40 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     }
   };
 
-  // One tile in LDS at src: tokens [t0, t0 + 32). EDGE: masked score by score.
-  auto step = [&](auto edge, const uint8_t *src, int t0, bool ok0, bool ok1) {
+  // ---- the phases of a tile
+  auto load_k = [&](const uint8_t *src) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) kf[half][kk] = *(const u32x4 *)(src + half * PB + kk * 1024 + lane * 16);
+  };
+  auto load_v = [&](const uint8_t *src) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+      vf[nb] = *(const u32x4 *)(src + (2 + (rq >> 1)) * PB + (nb * 16 + hl) * 32 + (rq & 1) * 16);
+  };
+  auto scores = [&]() {  // S = K Q^T
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)  // the products of a sum lie apart: each waits for the one before
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+          s[cb][half] = mfma_16x16x32(__builtin_bit_cast(bf16x8, kf[half][kk]), __builtin_bit_cast(bf16x8, q[cb][kk]),
+                                      kk == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[cb][half]);
+  };
+  auto values = [&]() {  // O += V^T P
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+        acc[cb][nb] = mfma_16x16x32(__builtin_bit_cast(bf16x8, vf[nb]), __builtin_bit_cast(bf16x8, p[cb]), acc[cb][nb]);
+  };
+  // Scores of tokens [t0, t0 + 32) to probabilities. EDGE: masked score by score.
+  auto softmax = [&](auto edge, int t0, bool ok0, bool ok1) {
     constexpr bool EDGE = decltype(edge)::value;
-    f32x4 s[CB][2];
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      u32x4 k[KK];
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) k[kk] = *(const u32x4 *)(src + half * PB + kk * 1024 + lane * 16);
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-          x = mfma_16x16x32(__builtin_bit_cast(bf16x8, k[kk]), __builtin_bit_cast(bf16x8, q[cb][kk]), x);
-        s[cb][half] = x;
-      }
-    }
     uint32_t vis[CB];  // of this lane's eight tokens
     if (EDGE) {
-      __builtin_amdgcn_sched_barrier(0);
       const int words = (a.max_rows + 63) / 64, seen_end = min(seq.ctx, seq.cap);
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
@@ -443,7 +467,6 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       }
       exponents();
     }
-    u32x4 p[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
 #pragma unroll
@@ -452,26 +475,21 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
 #pragma unroll
       for (int i = 0; i < 4; ++i) p[cb][i] = pack_pair(e[cb][2 * i], e[cb][2 * i + 1]);
     }
+    if (!EDGE) return;
+    // What is not finite leaves the product ...
+    u32x4 kept[NB];
     bool nonfinite = false;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      u32x4 v = *(const u32x4 *)(src + (2 + (rq >> 1)) * PB + (nb * 16 + hl) * 32 + (rq & 1) * 16);
-      if (EDGE) {
-        __builtin_amdgcn_sched_barrier(0);  // edge tiles are few: their registers count, not their overlap
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t w = v[i];
-          nonfinite |= drop_nonfinite(w);
-          v[i] = w;
-        }
+      for (int i = 0; i < 4; ++i) {
+        uint32_t w = vf[nb][i];
+        nonfinite |= drop_nonfinite(w);
+        kept[nb][i] = w;
       }
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb)
-        acc[cb][nb] = mfma_16x16x32(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, p[cb]), acc[cb][nb]);
-    }
-    if (EDGE && __any(nonfinite)) {
-      // Rare. How many +inf, -inf and NaN of each dim a column sees, 32 at most of each, as one product: weights 1, 64
-      // and 4096 times the column's visible tokens. What it sees is added.
+    if (__any(nonfinite)) {
+      // ... and, rarely, is added to the columns that see it: how many +inf, -inf and NaN of each dim they see, 32 at
+      // most of each, as one product: weights 1, 64 and 4096 times the column's visible tokens.
       u32x4 see[CB];
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb)
@@ -480,7 +498,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
           see[cb][i] = (vis[cb] >> (2 * i) & 1 ? 0x3f80u : 0u) | (vis[cb] >> (2 * i) & 2 ? 0x3f800000u : 0u);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        u32x4 v = *(const u32x4 *)(src + (2 + (rq >> 1)) * PB + (nb * 16 + hl) * 32 + (rq & 1) * 16);
+        u32x4 v = vf[nb];
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = nonfinite_weight(v[i]);
 #pragma unroll
@@ -497,6 +515,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) vf[nb] = kept[nb];
   };
 
   load_seq();
@@ -505,29 +525,69 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     ct = off / c_n;
     tile = off % c_n;
   }
+  constexpr int LEAD = QW == 1 ? NS : NS - 1;  // tiles fetched before the first is used
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) fetch(i);
-  open_task();
-
-  int cslot = 0, t = 0;
-  // Waits for tile t and fetches ahead. This wave's loads of tile t have landed once at most those of the tiles behind it
-  // are outstanding; after the barrier everyone's have, and nobody reads the slot the next fetch fills any more.
-  auto arrive = [&]() {
-    if (QW > 1) {
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((AHEAD - 1) * LPT) : "memory");
-      ok_bits >>= 2;
-      fetch(AHEAD - 1);
-    } else {
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * LPT) : "memory");
-    }
-    return (const uint8_t *)(slots + cslot * Shape::kTileBytes);
+  for (int i = 0; i < LEAD; ++i) {
+    find_pages();
+    issue(i);
+  }
+  open_task();  // ends with a wait for every load
+  int t = 0;
+  // A tile takes two phases: products (the last tile's values, this one's scores) and softmax, which also reads the
+  // operands of the next products from LDS and fetches ahead.
+  //  - Barriers: softmax of tile t reads tile t + 1's keys, so everyone's loads of it have landed before; and it fetches
+  //    into the slot of tile t - 1, so everyone has read its values before.
+  //  - Eight waves, two per SIMD, run half a tile apart: while one of a SIMD's waves is at its products the other is at its
+  //    softmax, with a barrier after either phase. In step, they would queue for the matrix cores together and for the
+  //    vector unit together (64 sequences of 8192 tokens, 64 rows: FIGPING).
+  //  - One wave alone has no barrier and reads each tile's keys when it starts on it.
+  constexpr bool PING = QW == 8;
+  int slot = 0;
+  auto next_slot = [](int x) { return x + 1 == NS ? 0 : x + 1; };
+  auto at_slot = [&](int x) { return (const uint8_t *)(slots + x * Shape::kTileBytes); };
+  auto landed = [&]() {  // before softmax of tile t: tile t + 1 is there
+    if (PING) __builtin_amdgcn_sched_barrier(0);  // products stay in their phase
+    if (QW > 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((QW > 1 ? NS - 3 : 0) * LPT) : "memory");
+    if (PING) __builtin_amdgcn_sched_barrier(0);
   };
-  auto leave = [&]() {
-    if (QW == 1) {
-      ok_bits >>= 2;
-      fetch(AHEAD - 1);
+  auto meet = [&]() {
+    if (!PING) return;
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (QW > 1) {
+    asm volatile("s_barrier" ::: "memory");
+    load_k(at_slot(0));
+  }
+  if (PING && wave >= 4) meet();
+  auto products = [&]() {
+    find_pages();
+    if (QW > 1) {
+      values();
+      scores();
+    } else {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 1) * LPT) : "memory");
+      load_k(at_slot(slot));
+      load_v(at_slot(slot));
+      scores();
     }
-    cslot = cslot + 1 == NS ? 0 : cslot + 1;
+  };
+  auto to_softmax = [&](auto edge, int t0, bool ok0, bool ok1) {
+    if (PING) meet(); else landed();
+    if (QW > 1) {
+      issue(NS - 1);
+      load_v(at_slot(slot));
+      load_k(at_slot(next_slot(slot)));
+    }
+    ok_bits >>= 2;
+    softmax(edge, t0, ok0, ok1);
+    if (QW == 1) {
+      values();
+      issue(NS - 1);
+    }
+    if (PING) landed();
+    slot = next_slot(slot);
     ++tile;
     ++t;
   };
@@ -539,17 +599,16 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     const int run = tile < full_begin ? 0 : min(min(n_w - t, full_end - tile), 32 - (it & 31));
     int done = 0;
     for (; done < run && (ok_bits & 3) == 3; ++done) {
-      const uint8_t *src = arrive();
-      step(std::false_type(), src, 0, true, true);
-      leave();
+      products();
+      to_softmax(std::false_type(), 0, true, true);
     }
     if (done == 0) {
       const bool ok0 = ok_bits & 1, ok1 = ok_bits & 2;
-      const uint8_t *src = arrive();
-      step(std::true_type(), src, (c_first + tile) * kTile, ok0, ok1);
-      leave();
+      products();
+      to_softmax(std::true_type(), (c_first + tile) * kTile, ok0, ok1);
     }
     if (tile == c_n) {  // the task ends here
+      if (QW > 1) values();
       close_task(seg_first == 0);
       if (by_task && tid == 0 && seg_first == 0) desc[task_id()].pieces = 1;
       first_piece = false;
@@ -565,6 +624,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       }
     }
   }
+  if (PING && wave < 4) meet();  // as many barriers as the other half
+  if (QW > 1 && tile > 0) values();
   // No load may still be writing LDS when the workgroup retires.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if (tile > 0) {  // the range ends inside a task
