@@ -3,7 +3,6 @@
 // drafted ones its mask names.
 #include <math.h>
 
-#include <stdlib.h>
 #include <type_traits>
 
 #include "draft.hpp"
@@ -160,8 +159,8 @@ template <int D, int NQ, int QW>
 struct TreeShape {
   static constexpr int QT = NQ * QW;
   static constexpr int kTileBytes = kTile * D * 2 * 2;
-  // Tiles in LDS. Two workgroups of 4 waves share a compute unit, or 4 (D = 128) or 8 of one wave; 8 waves have it alone.
-  static constexpr int kSlots = QW == 1 ? 2 : QW == 8 ? (D == 64 ? 8 : 6) : (D == 64 ? 6 : 4);
+  // Tiles in LDS: 128 KB of them, or two of each of the one-wave workgroups that share a compute unit.
+  static constexpr int kSlots = QW == 1 ? 2 : 8;
   static constexpr int kChunks = kTileBytes / 1024;   // 1 KB direct-to-LDS loads of a tile
   static constexpr int kPerWave = kChunks / QW;
 };
@@ -241,55 +240,59 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     const int lp = 2 * (s_first[b] + off % n) + (lane & 1);
     if (a.ring <= 0 && lp >= a.cols) return;
     page = a.table[(int64_t)b * a.cols + (a.ring > 0 ? lp % a.ring : lp)];
-    if (page >= a.pool_pages) page = -1;
   };
   int page_cur, head_cur, page_nxt, head_nxt;
   gather(0, page_cur, head_cur);
   gather(32, page_nxt, head_nxt);
 
-  const int64_t blk = (int64_t)kPage * D, page_stride = 2 * (int64_t)a.n_kv * blk;
-  const uint32_t key_off = (((hl & 4) * 2 + (hl & 3)) * D + rq * 8) * 2, val_off = lane * 16;
+  constexpr int64_t blk = (int64_t)kPage * D;
   int it = 0, islot = 0;   // next unit to fetch, and its slot
   uint32_t ok_bits = 0;    // two bits per fetched unit, the next one to be consumed lowest
-
-  // Refills the page window before the fetch of every 32nd unit. The wait is here so that the steps between, which the
-  // compiler would otherwise make wait for every load in flight, have none to make.
+  // Refills the page window before the fetch of every 32nd unit. The new entries are used 32 units later: nothing waits
+  // for them here, where a wait would drain the tiles in flight.
   auto next_window = [&]() {
     page_cur = page_nxt;
     head_cur = head_nxt;
     gather(it + 32, page_nxt, head_nxt);
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
   };
   // Fetching unit `it` (past the range: the first page of the pool, so that every fetch makes LPT loads and the waits can
-  // count them) in two steps: where its pages are, scalar work that hides behind products, and the loads. Chunk c of the
-  // tile, 1 KB each: 2 KK of keys, then KK of values of either page; a wave takes LPT neighbouring ones. Keys: lane l
-  // brings the 16 bytes it reads as its fragment of product h, K[token 8 (l % 16 / 4) + 4 h + l % 4][kk * 32 + l / 16 * 8
-  // ..]; values: as they lie in the page.
+  // count them) in two steps: where its pages are, and the loads. Chunk c of the tile, 1 KB each: 2 KK of keys, then KK of
+  // values of either page; a wave takes LPT neighbouring ones. Keys: lane l brings the 16 bytes it reads as its fragment
+  // of product h, K[token 8 (l % 16 / 4) + 4 h + l % 4][kk * 32 + l / 16 * 8 ..]; values: as they lie in the page.
+  const uint32_t stride = (uint32_t)(a.n_kv * blk * 4), head_bytes = (uint32_t)(blk * 2);  // of a page, of a head in it
+  const uint32_t pages = (uint32_t)min(a.pool_pages, (int64_t)0x7fffffff);
+  uint32_t chunk_off[LPT];  // this lane's bytes of a chunk, from its page's head
+  bool chunk_p1[LPT];       // and whether that is the second page
+#pragma unroll
+  for (int i = 0; i < LPT; ++i) {
+    const int c = wave * LPT + i;
+    const bool keys = c < 2 * KK;
+    chunk_off[i] = keys ? (uint32_t)(c / KK * (4 * D * 2) + c % KK * 64 + (((hl & 4) * 2 + (hl & 3)) * D + rq * 8) * 2)
+                        : (uint32_t)(stride / 2 + c % KK * 1024 + lane * 16);
+    chunk_p1[i] = keys ? hl >= 8 : c >= 3 * KK;
+  }
   const uint8_t *base0 = nullptr, *base1 = nullptr;
   uint32_t ok_next = 0;
   auto find_pages = [&]() {
     const int at = (it & 31) * 2;
-    const int p0 = __builtin_amdgcn_readlane(page_cur, at), p1 = __builtin_amdgcn_readlane(page_cur, at + 1);
-    const int g = __builtin_amdgcn_readlane(head_cur, at);
-    const bool live = it < n_w, ok0 = live && p0 >= 0, ok1 = live && p1 >= 0;
+    const uint32_t p0 = __builtin_amdgcn_readlane(page_cur, at), p1 = __builtin_amdgcn_readlane(page_cur, at + 1);
+    const uint32_t g = __builtin_amdgcn_readlane(head_cur, at);
+    const uint32_t most = it < n_w ? pages : 0u;
+    const bool ok0 = p0 < most, ok1 = p1 < most;
     ok_next = (ok0 ? 1u : 0u) | (ok1 ? 2u : 0u);
-    base0 = (const uint8_t *)(a.pool + (int64_t)(ok0 ? p0 : 0) * page_stride + g * blk);
-    base1 = ok1 ? (const uint8_t *)(a.pool + (int64_t)p1 * page_stride + g * blk) : base0;
+    const uint32_t q0 = ok0 ? p0 : 0u, q1 = ok1 ? p1 : q0;
+    const uint8_t *pool = (const uint8_t *)a.pool + (uint64_t)g * head_bytes;
+    base0 = pool + (uint64_t)q0 * stride;
+    base1 = pool + (uint64_t)q1 * stride;
     ++it;
   };
   auto issue = [&](int age) {
     ok_bits |= ok_next << (2 * age);
     uint8_t *const dst = slots + islot * Shape::kTileBytes;
 #pragma unroll
-    for (int i = 0; i < LPT; ++i) {
-      const int c = wave * LPT + i;
-      const void *src;
-      if (c < 2 * KK)
-        src = (hl < 8 ? base0 : base1) + (c / KK * (4 * D * 2) + c % KK * 64) + key_off;
-      else
-        src = (c < 3 * KK ? base0 : base1) + (a.n_kv * blk * 2 + c % KK * 1024) + val_off;
-      __builtin_amdgcn_global_load_lds(src, (__attribute__((address_space(3))) void *)(dst + c * 1024), 16, 0, 0);
-    }
+    for (int i = 0; i < LPT; ++i)
+      __builtin_amdgcn_global_load_lds((const void *)((chunk_p1[i] ? base1 : base0) + chunk_off[i]),
+                                       (__attribute__((address_space(3))) void *)(dst + (wave * LPT + i) * 1024), 16, 0, 0);
     islot = islot + 1 == NS ? 0 : islot + 1;
   };
 
@@ -380,33 +383,33 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   };
 
   // ---- the phases of a tile
-  auto load_k = [&](const uint8_t *src) {
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) kf[half][kk] = *(const u32x4 *)(src + half * PB + kk * 1024 + lane * 16);
+  auto key = [&](const uint8_t *src, int half, int kk) { return *(const u32x4 *)(src + half * PB + kk * 1024 + lane * 16); };
+  auto value = [&](const uint8_t *src, int nb) {
+    return *(const u32x4 *)(src + (2 + (rq >> 1)) * PB + (nb * 16 + hl) * 32 + (rq & 1) * 16);
   };
-  auto load_v = [&](const uint8_t *src) {
+  // O += V^T P; S = K Q^T. NEXT: an operand is replaced right after its last product, by this tile's values at src_v and
+  // the next one's keys at src_k, so the reads run under the products.
+  auto values = [&](auto next, const uint8_t *src_v) {
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-      vf[nb] = *(const u32x4 *)(src + (2 + (rq >> 1)) * PB + (nb * 16 + hl) * 32 + (rq & 1) * 16);
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+        acc[cb][nb] = mfma_16x16x32(__builtin_bit_cast(bf16x8, vf[nb]), __builtin_bit_cast(bf16x8, p[cb]), acc[cb][nb]);
+      if (decltype(next)::value) vf[nb] = value(src_v, nb);
+    }
   };
-  auto scores = [&]() {  // S = K Q^T
+  auto scores = [&](auto next, const uint8_t *src_k) {
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk)  // the products of a sum lie apart: each waits for the one before
+    for (int kk = 0; kk < KK; ++kk) {  // the products of a sum lie apart: each waits for the one before
 #pragma unroll
-      for (int half = 0; half < 2; ++half)
+      for (int half = 0; half < 2; ++half) {
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb)
           s[cb][half] = mfma_16x16x32(__builtin_bit_cast(bf16x8, kf[half][kk]), __builtin_bit_cast(bf16x8, q[cb][kk]),
                                       kk == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[cb][half]);
-  };
-  auto values = [&]() {  // O += V^T P
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb)
-        acc[cb][nb] = mfma_16x16x32(__builtin_bit_cast(bf16x8, vf[nb]), __builtin_bit_cast(bf16x8, p[cb]), acc[cb][nb]);
+        if (decltype(next)::value) kf[half][kk] = key(src_k, half, kk);
+      }
+    }
   };
   // Scores of tokens [t0, t0 + 32) to probabilities. EDGE: masked score by score.
   auto softmax = [&](auto edge, int t0, bool ok0, bool ok1) {
@@ -533,66 +536,79 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   }
   open_task();  // ends with a wait for every load
   int t = 0;
-  // A tile takes two phases: products (the last tile's values, this one's scores) and softmax, which also reads the
-  // operands of the next products from LDS and fetches ahead.
-  //  - Barriers: softmax of tile t reads tile t + 1's keys, so everyone's loads of it have landed before; and it fetches
-  //    into the slot of tile t - 1, so everyone has read its values before.
-  //  - Eight waves, two per SIMD, run half a tile apart: while one of a SIMD's waves is at its products the other is at its
-  //    softmax, with a barrier after either phase. In step, they would queue for the matrix cores together and for the
-  //    vector unit together (64 sequences of 8192 tokens, 64 rows: FIGPING).
-  //  - One wave alone has no barrier and reads each tile's keys when it starts on it.
+  // A tile takes two phases: products (the last tile's values, then this one's scores; each operand is replaced from LDS
+  // after its last use, by this tile's values and the next one's keys) and softmax, which also fetches a tile.
+  //  - Products of tile t read tiles t and t + 1, so everyone's loads of t + 1 have landed before; softmax of tile t
+  //    fetches into the slot of tile t - 1, whose last reads were made in products t - 1.
+  //  - Two or four waves meet once a tile, before its products.
+  //  - Eight waves, two per SIMD, run half a tile apart and meet after either phase: while one of a SIMD's waves is at its
+  //    products the other is at its softmax. In step they queue for the matrix cores and for the vector unit in turn.
+  //    The later half's products t are the earlier half's softmax t: what the products of t + 1 read (tile t + 2) has to
+  //    have landed when anyone's products t end.
+  //  - One wave alone has no barrier; it reads a tile when it starts on it.
   constexpr bool PING = QW == 8;
   int slot = 0;
   auto next_slot = [](int x) { return x + 1 == NS ? 0 : x + 1; };
   auto at_slot = [&](int x) { return (const uint8_t *)(slots + x * Shape::kTileBytes); };
-  auto landed = [&]() {  // before softmax of tile t: tile t + 1 is there
-    if (PING) __builtin_amdgcn_sched_barrier(0);  // products stay in their phase
-    if (QW > 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((QW > 1 ? NS - 3 : 0) * LPT) : "memory");
-    if (PING) __builtin_amdgcn_sched_barrier(0);
-  };
-  auto meet = [&]() {
-    if (!PING) return;
+  // At most `tiles` of this wave's fetches are outstanding; `reads`: its LDS reads are done. Then a barrier.
+  auto meet = [&](auto tiles, bool reads) {
+    constexpr int n = decltype(tiles)::value * LPT;
     __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (reads) __builtin_amdgcn_s_waitcnt((n & 15) | 7 << 4 | 0 << 8 | n >> 4 << 14);
+    else __builtin_amdgcn_s_waitcnt((n & 15) | 7 << 4 | 15 << 8 | n >> 4 << 14);
+    asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
+  using All = std::integral_constant<int, 63 / LPT>;  // as many as the counter holds: no wait
+  using Prod = std::integral_constant<int, PING ? NS - 4 : 63 / LPT>;
+  using Soft = std::integral_constant<int, PING || QW == 1 ? 63 / LPT : NS - 3>;
   if (QW > 1) {
     asm volatile("s_barrier" ::: "memory");
-    load_k(at_slot(0));
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) kf[half][kk] = key(at_slot(0), half, kk);
   }
-  if (PING && wave >= 4) meet();
+  if (PING && wave >= 4) meet(All(), true);
   auto products = [&]() {
-    find_pages();
     if (QW > 1) {
-      values();
-      scores();
+      values(std::true_type(), at_slot(slot));
+      scores(std::true_type(), at_slot(next_slot(slot)));
+#pragma unroll
+      for (int i = 0; i < NB + 2 * KK; ++i) {  // a read after every pair (CB = 2) of products
+        __builtin_amdgcn_sched_group_barrier(0x8, CB, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      if (PING) meet(Prod(), false);
     } else {
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 1) * LPT) : "memory");
-      load_k(at_slot(slot));
-      load_v(at_slot(slot));
-      scores();
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) kf[half][kk] = key(at_slot(slot), half, kk);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) vf[nb] = value(at_slot(slot), nb);
+      scores(std::false_type(), nullptr);
     }
   };
   auto to_softmax = [&](auto edge, int t0, bool ok0, bool ok1) {
-    if (PING) meet(); else landed();
-    if (QW > 1) {
-      issue(NS - 1);
-      load_v(at_slot(slot));
-      load_k(at_slot(next_slot(slot)));
-    }
+    find_pages();
+    if (QW > 1) issue(NS - 1);
     ok_bits >>= 2;
     softmax(edge, t0, ok0, ok1);
     if (QW == 1) {
-      values();
+      values(std::false_type(), nullptr);
       issue(NS - 1);
+    } else {
+      meet(Soft(), true);
     }
-    if (PING) landed();
     slot = next_slot(slot);
     ++tile;
     ++t;
   };
   while (t < n_w) {
     if ((it & 31) == 0) next_window();
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): what is pending here is not waited for in every product phase below
     // Tiles that need no mask, up to the next page window: all of it cached tokens that every row sees, pages in the pool.
     const int lo_most = a.window > 0 ? seq.ctx + a.max_rows - a.window : 0;
     const int full_end = min(seq.ctx, seq.cap) / kTile - c_first, full_begin = (max(lo_most, 0) + kTile - 1) / kTile - c_first;
@@ -608,7 +624,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       to_softmax(std::true_type(), (c_first + tile) * kTile, ok0, ok1);
     }
     if (tile == c_n) {  // the task ends here
-      if (QW > 1) values();
+      if (QW > 1) values(std::false_type(), nullptr);
       close_task(seg_first == 0);
       if (by_task && tid == 0 && seg_first == 0) desc[task_id()].pieces = 1;
       first_piece = false;
@@ -624,8 +640,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       }
     }
   }
-  if (PING && wave < 4) meet();  // as many barriers as the other half
-  if (QW > 1 && tile > 0) values();
+  if (PING && wave < 4) meet(All(), true);  // as many barriers as the other half
+  if (QW > 1 && tile > 0) values(std::false_type(), nullptr);
   // No load may still be writing LDS when the workgroup retires.
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if (tile > 0) {  // the range ends inside a task
@@ -760,30 +776,42 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const
   }
 }
 
+// Sequences per launch: what LDS has room for beside the tiles. Larger batches take several launches, one after the other
+// on the same records.
+constexpr int kTreeBatch = 2048;
+
 template <int D, int NQ, int QW>
-hipError_t go_tree(const DraftArgs &a, const TreePlan &plan, void *ws, hipStream_t s) {
+hipError_t go_tree(DraftArgs a, const TreePlan &plan, void *ws, hipStream_t s) {
   using Shape = TreeShape<D, NQ, QW>;
   static std::atomic<uint64_t> lds_set{0};  // devices whose LDS limit is raised
   auto lds = [](int B) { return ((3 * (size_t)B + 1) * 4 + 15) / 16 * 16 + (size_t)Shape::kSlots * Shape::kTileBytes; };
   const auto kern = tree_attention_kernel<D, NQ, QW>;
-  if (hipError_t e = ensure_lds_limit((const void *)kern, lds(kMaxAttnBatch), lds_set); e != hipSuccess) return e;
+  if (hipError_t e = ensure_lds_limit((const void *)kern, lds(kTreeBatch), lds_set); e != hipSuccess) return e;
   static_assert(sizeof(TreeDesc) <= kTreeDescBytes, "descriptor size");
   TreeDesc *desc = (TreeDesc *)ws;
-  const int64_t tasks = (int64_t)a.B * a.n_kv * plan.max_qt;
-  const int by_task = tasks <= plan.grid, blocks = by_task ? (int)tasks : plan.grid;
   float2 *ml = (float2 *)((uint8_t *)ws + (size_t)kTreeDescBytes * plan.grid);
   float *acc = (float *)(ml + (size_t)2 * plan.grid * plan.qt);
   const float scale = (float)(1.4426950408889634 / sqrt((double)D));
-  hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * QW), lds(a.B), s, a, plan.min_tiles, plan.max_qt, by_task, scale, acc, ml,
-                     desc);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (plan.split_join)
-    hipLaunchKernelGGL((tree_join_kernel<D, true>), dim3(blocks, plan.qt), dim3(256), 0, s, a, plan.qt, plan.max_qt, by_task,
-                       acc, ml, desc);
-  else
-    hipLaunchKernelGGL((tree_join_kernel<D, false>), dim3(blocks, plan.qt / 16), dim3(256), 0, s, a, plan.qt, plan.max_qt,
-                       by_task, acc, ml, desc);
-  return hipGetLastError();
+  const int B = a.B;
+  for (int b0 = 0; b0 < B; b0 += kTreeBatch) {
+    a.B = B - b0 < kTreeBatch ? B - b0 : kTreeBatch;
+    const int64_t tasks = (int64_t)a.B * a.n_kv * plan.max_qt;
+    const int by_task = tasks <= plan.grid, blocks = by_task ? (int)tasks : plan.grid;
+    hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * QW), lds(a.B), s, a, plan.min_tiles, plan.max_qt, by_task, scale, acc,
+                       ml, desc);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (plan.split_join)
+      hipLaunchKernelGGL((tree_join_kernel<D, true>), dim3(blocks, plan.qt), dim3(256), 0, s, a, plan.qt, plan.max_qt, by_task,
+                         acc, ml, desc);
+    else
+      hipLaunchKernelGGL((tree_join_kernel<D, false>), dim3(blocks, plan.qt / 16), dim3(256), 0, s, a, plan.qt, plan.max_qt,
+                         by_task, acc, ml, desc);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    a.row_off += a.B;
+    a.ctx_lens += a.B;
+    a.table += (int64_t)a.B * a.cols;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
@@ -800,7 +828,7 @@ hipError_t launch_tree_attention(const DraftArgs &a, const TreePlan &plan, void 
       case 16: return go_tree<D, 16, 1>(a, plan, ws, s);
       case 32: return go_tree<D, 16, 2>(a, plan, ws, s);
       case 64: return go_tree<D, 16, 4>(a, plan, ws, s);
-      case 128: return getenv("TREE_V") && atoi(getenv("TREE_V")) == 1 ? go_tree<D, 16, 8>(a, plan, ws, s) : go_tree<D, 32, 4>(a, plan, ws, s);
+      case 128: return go_tree<D, 16, 8>(a, plan, ws, s);
       case 256: return go_tree<D, 32, 8>(a, plan, ws, s);
     }
     return hipErrorInvalidValue;

@@ -136,7 +136,7 @@ TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_dra
   if (c.window > 0) tokens = std::min(tokens, (int64_t)c.window + draft->max_rows + 64);
   const int64_t units = (int64_t)batch->batch * c.n_kv * p.max_qt * ((tokens + 31) / 32 + 1);
   p.units_ok = units < (int64_t)1 << 30;
-  const int per_cu = p.qt <= 16 ? (c.head_dim == 64 ? 8 : 4) : p.qt <= 128 ? 2 : 1;
+  const int per_cu = p.qt <= 16 ? (c.head_dim == 64 ? 8 : 4) : c.head_dim == 64 && p.qt <= 64 ? 2 : 1;
   p.min_tiles = 2;
   if (getenv("TREE_MIN")) p.min_tiles = atoi(getenv("TREE_MIN"));
   const int percu2 = getenv("TREE_PER") ? atoi(getenv("TREE_PER")) : per_cu;
