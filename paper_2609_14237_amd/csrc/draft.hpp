@@ -13,8 +13,13 @@ struct DraftSeq {
   int ctx, end, cap;
 };
 
-__device__ __forceinline__ DraftSeq draft_seq(const int32_t *__restrict__ row_off, const int32_t *__restrict__ ctx_lens,
-                                              int b, int rows, int max_rows, int cols, int ring) {
+// Arrays a kernel only reads, as constant memory: a uniform index becomes a scalar load, which does not queue behind the
+// vector loads in flight.
+typedef const __attribute__((address_space(4))) int32_t *ConstInts;
+
+template <typename Ints>  // const int32_t * or ConstInts
+__device__ __forceinline__ DraftSeq draft_seq(Ints row_off, Ints ctx_lens, int b, int rows, int max_rows, int cols,
+                                              int ring) {
   DraftSeq s;
   const int a = row_off[b], e = row_off[b + 1], c = ctx_lens[b];
   s.r0 = a;

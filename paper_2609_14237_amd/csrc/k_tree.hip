@@ -138,12 +138,10 @@ __device__ __forceinline__ uint32_t nonfinite_weight(uint32_t w) {
   return of(w & 0xffffu) | of(w >> 16) << 16;
 }
 
-// Non-finite bf16 halves of a dword are cleared; true if there were any.
-__device__ __forceinline__ bool drop_nonfinite(uint32_t &w) {
-  const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
-  if (lo) w &= 0xffff0000u;
-  if (hi) w &= 0x0000ffffu;
-  return lo || hi;
+// Non-finite bf16 halves of a dword are cleared.
+__device__ __forceinline__ void drop_nonfinite(uint32_t &w) {
+  if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0x0000ffffu;
 }
 
 // A task that begins in a range and ends in a later one.
@@ -177,11 +175,14 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   const int B = a.B, group = a.n_q / a.n_kv;
   int *s_pre = smem, *s_first = smem + B + 1, *s_n = s_first + B;  // units before, first tile, tiles of a sequence
   uint8_t *const slots = (uint8_t *)smem + ((3 * B + 1) * 4 + 15) / 16 * 16;
-  __shared__ int s_tot[QW];
+  __shared__ int s_tot[QW], s_ids[QW * 64];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hl = lane & 15, rq = lane >> 4;
+  // c / group and c % group of a column, c < 2^13: exact, (c + 1/2) / group is 1/32 off an integer at least
+  const float inv_group = 1.f / (float)group;
+  auto row_of = [&](int c) { return (int)(((float)c + 0.5f) * inv_group); };
 
   {  // ---- units before each sequence
     const int per = (B + THREADS - 1) / THREADS;
@@ -227,34 +228,46 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     return b;
   };
 
-  // Pages and KV head of units [t0, t0 + 32) of the range: lane l has page l % 2 of unit t0 + l / 2 (-1: none).
-  auto gather = [&](int t0, int &page, int &head) {
+  // The page window: of units [t0, t0 + 32) of the range lane l knows page l % 2 of unit t0 + l / 2 and the unit's KV head.
+  // entry: where in the table that page stands (-1: nowhere), from LDS alone.
+  auto entry = [&](int t0, int &head) -> int64_t {
     const int t = t0 + (lane >> 1);
-    page = -1;
     head = 0;
-    if (t >= n_w) return;
+    if (t >= n_w) return -1;
     const int u = u0 + t, b = find_seq(u), n = s_n[b];
-    const int off = u - s_pre[b], task = off / n;
-    const int n_qt = (s_pre[b + 1] - s_pre[b]) / (n * a.n_kv);
-    head = task / n_qt;
-    const int lp = 2 * (s_first[b] + off % n) + (lane & 1);
-    if (a.ring <= 0 && lp >= a.cols) return;
-    page = a.table[(int64_t)b * a.cols + (a.ring > 0 ? lp % a.ring : lp)];
+    const int off = u - s_pre[b];
+    head = off / n;
+    const int lp = 2 * (s_first[b] + off - head * n) + (lane & 1);
+    if (max_qt > 1) head /= (s_pre[b + 1] - s_pre[b]) / (n * a.n_kv);
+    if (a.ring <= 0 && lp >= a.cols) return -1;
+    return (int64_t)b * a.cols + (a.ring > 0 ? lp % a.ring : lp);
   };
-  int page_cur, head_cur, page_nxt, head_nxt;
-  gather(0, page_cur, head_cur);
-  gather(32, page_nxt, head_nxt);
-
   constexpr int64_t blk = (int64_t)kPage * D;
   int it = 0, islot = 0;   // next unit to fetch, and its slot
   uint32_t ok_bits = 0;    // two bits per fetched unit, the next one to be consumed lowest
-  // Refills the page window before the fetch of every 32nd unit. The new entries are used 32 units later: nothing waits
-  // for them here, where a wait would drain the tiles in flight.
-  auto next_window = [&]() {
-    page_cur = page_nxt;
-    head_cur = head_nxt;
-    gather(it + 32, page_nxt, head_nxt);
+  // The next window's pages come to LDS like the tiles, 32 units before they are used: nothing ever waits for them, where a
+  // wait for a register would drain the tiles in flight (6 us every 32 tiles: 64 sequences x 8192 tokens x 64 rows 634 ->
+  // FIGWIN us).
+  int page_cur, head_cur, head_nxt;
+  bool has_nxt;
+  int *const ids = s_ids + wave * 64;
+  auto fetch_window = [&](int t0) {
+    const int64_t e = entry(t0, head_nxt);
+    has_nxt = e >= 0;
+    __builtin_amdgcn_global_load_lds((const void *)(a.table + (has_nxt ? e : 0)),
+                                     (__attribute__((address_space(3))) void *)ids, 4, 0, 0);
   };
+  auto next_window = [&]() {  // before the fetch of every 32nd unit
+    page_cur = has_nxt ? ids[lane] : -1;
+    head_cur = head_nxt;
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): read before it is overwritten
+    fetch_window(it + 32);
+  };
+  {
+    const int64_t e = entry(0, head_cur);
+    page_cur = e >= 0 ? a.table[e] : -1;
+    fetch_window(32);
+  }
   // Fetching unit `it` (past the range: the first page of the pool, so that every fetch makes LPT loads and the waits can
   // count them) in two steps: where its pages are, and the loads. Chunk c of the tile, 1 KB each: 2 KK of keys, then KK of
   // values of either page; a wave takes LPT neighbouring ones. Keys: lane l brings the 16 bytes it reads as its fragment
@@ -300,6 +313,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   int cb_seq = __builtin_amdgcn_readfirstlane(find_seq(u0)), ct, c_n, c_first, c_qts;  // sequence, task in it, its tiles
   int tile;                                                                          // next tile of the task
   DraftSeq seq;
+  bool busy;                          // this wave has columns in it
   int head, qt, seg_first;            // KV head, query tile, first tile of this range's piece
   bool first_piece = true;
   u32x4 q[CB][KK];
@@ -315,8 +329,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   auto load_seq = [&]() {
     c_n = uniform(s_n[cb_seq]);
     c_first = uniform(s_first[cb_seq]);
-    c_qts = uniform((s_pre[cb_seq + 1] - s_pre[cb_seq]) / (c_n * a.n_kv));
-    const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, cb_seq, a.rows, a.max_rows, a.cols, a.ring);
+    c_qts = max_qt > 1 ? uniform((s_pre[cb_seq + 1] - s_pre[cb_seq]) / (c_n * a.n_kv)) : 1;
+    const DraftSeq s = draft_seq((ConstInts)a.row_off, (ConstInts)a.ctx_lens, cb_seq, a.rows, a.max_rows, a.cols, a.ring);
     seq.r0 = uniform(s.r0);
     seq.n = uniform(s.n);
     seq.ctx = uniform(s.ctx);
@@ -324,16 +338,17 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     seq.cap = s.cap;
   };
   auto open_task = [&]() {
-    head = ct / c_qts;
-    qt = ct % c_qts;
+    head = max_qt > 1 ? ct / c_qts : ct;
+    qt = max_qt > 1 ? ct % c_qts : 0;
     seg_first = tile;
     const int cols = seq.n * group;
+    busy = qt * QT + wave * NQ < cols;
     const int64_t row_elems = (int64_t)(a.n_q + 2 * a.n_kv) * D;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       const int c = min(qt * QT + wave * NQ + cb * 16 + hl, cols - 1);  // columns past the last repeat it, unwritten
-      const int j = c / group;
-      const uint16_t *src = a.qkv + (seq.r0 + j) * row_elems + (head * group + c % group) * D + rq * 8;
+      const int j = row_of(c);
+      const uint16_t *src = a.qkv + (seq.r0 + j) * row_elems + (head * group + c - j * group) * D + rq * 8;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) q[cb][kk] = *(const u32x4 *)(src + kk * 32);
       col_row[cb] = j;
@@ -365,7 +380,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       if (c >= cols) continue;
       if (whole) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        uint16_t *dst = a.o + ((int64_t)(seq.r0 + c / group) * a.n_q + head * group + c % group) * D + rq * 4;
+        const int j = row_of(c);
+        uint16_t *dst = a.o + ((int64_t)(seq.r0 + j) * a.n_q + head * group + c - j * group) * D + rq * 4;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           u32x2 w;
@@ -479,20 +495,15 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       for (int i = 0; i < 4; ++i) p[cb][i] = pack_pair(e[cb][2 * i], e[cb][2 * i + 1]);
     }
     if (!EDGE) return;
-    // What is not finite leaves the product ...
-    u32x4 kept[NB];
-    bool nonfinite = false;
+    // Zeros times the values tell whether all of them are finite.
+    f32x4 zero[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t w = vf[nb][i];
-        nonfinite |= drop_nonfinite(w);
-        kept[nb][i] = w;
-      }
-    if (__any(nonfinite)) {
-      // ... and, rarely, is added to the columns that see it: how many +inf, -inf and NaN of each dim they see, 32 at
-      // most of each, as one product: weights 1, 64 and 4096 times the column's visible tokens.
+      zero[nb & 1] = mfma_16x16x32(__builtin_bit_cast(bf16x8, vf[nb]), __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u}), zero[nb & 1]);
+    const f32x4 nan = zero[0] + zero[1];
+    if (__any(!(nan[0] + nan[1] + nan[2] + nan[3] == 0.f))) {
+      // Rare. What is not finite leaves the product and is added to the columns that see it: how many +inf, -inf and NaN
+      // of each dim they see, 32 at most of each, as one product: weights 1, 64 and 4096 times the column's visible tokens.
       u32x4 see[CB];
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb)
@@ -503,7 +514,12 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       for (int nb = 0; nb < NB; ++nb) {
         u32x4 v = vf[nb];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = nonfinite_weight(v[i]);
+        for (int i = 0; i < 4; ++i) {
+          uint32_t w = v[i];
+          drop_nonfinite(w);
+          vf[nb][i] = w;
+          v[i] = nonfinite_weight(v[i]);
+        }
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
           const f32x4 n = mfma_16x16x32(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, see[cb]), f32x4{0.f, 0.f, 0.f, 0.f});
@@ -518,8 +534,6 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) vf[nb] = kept[nb];
   };
 
   load_seq();
@@ -562,30 +576,32 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   using All = std::integral_constant<int, 63 / LPT>;  // as many as the counter holds: no wait
   using Prod = std::integral_constant<int, PING ? NS - 4 : 63 / LPT>;
   using Soft = std::integral_constant<int, PING || QW == 1 ? 63 / LPT : NS - 3>;
-  if (QW > 1) {
-    asm volatile("s_barrier" ::: "memory");
+  auto first_keys = [&]() {
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) kf[half][kk] = key(at_slot(0), half, kk);
+      for (int kk = 0; kk < KK; ++kk) kf[half][kk] = key(at_slot(slot), half, kk);
+  };
+  if (QW > 1) {
+    asm volatile("s_barrier" ::: "memory");
+    first_keys();
   }
   if (PING && wave >= 4) meet(All(), true);
   auto products = [&]() {
     if (QW > 1) {
-      values(std::true_type(), at_slot(slot));
-      scores(std::true_type(), at_slot(next_slot(slot)));
+      if (busy) {
+        values(std::true_type(), at_slot(slot));
+        scores(std::true_type(), at_slot(next_slot(slot)));
 #pragma unroll
-      for (int i = 0; i < NB + 2 * KK; ++i) {  // a read after every pair (CB = 2) of products
-        __builtin_amdgcn_sched_group_barrier(0x8, CB, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        for (int i = 0; i < NB + 2 * KK; ++i) {  // a read after every pair (CB = 2) of products
+          __builtin_amdgcn_sched_group_barrier(0x8, CB, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
       }
       if (PING) meet(Prod(), false);
     } else {
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 1) * LPT) : "memory");
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) kf[half][kk] = key(at_slot(slot), half, kk);
+      first_keys();
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) vf[nb] = value(at_slot(slot), nb);
       scores(std::false_type(), nullptr);
@@ -595,7 +611,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     find_pages();
     if (QW > 1) issue(NS - 1);
     ok_bits >>= 2;
-    softmax(edge, t0, ok0, ok1);
+    if (busy) softmax(edge, t0, ok0, ok1);
     if (QW == 1) {
       values(std::false_type(), nullptr);
       issue(NS - 1);
@@ -624,6 +640,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       to_softmax(std::true_type(), (c_first + tile) * kTile, ok0, ok1);
     }
     if (tile == c_n) {  // the task ends here
+      if (PING && wave < 4) meet(All(), true);  // the halves change tasks together
       if (QW > 1) values(std::false_type(), nullptr);
       close_task(seg_first == 0);
       if (by_task && tid == 0 && seg_first == 0) desc[task_id()].pieces = 1;
@@ -637,7 +654,9 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
           load_seq();
         }
         open_task();
+        if (QW > 1) first_keys();  // the last products did not read them if this wave had no columns there
       }
+      if (PING && wave >= 4) meet(All(), true);
     }
   }
   if (PING && wave < 4) meet(All(), true);  // as many barriers as the other half
