@@ -271,7 +271,9 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   // Fetching unit `it` (past the range: the first page of the pool, so that every fetch makes LPT loads and the waits can
   // count them) in two steps: where its pages are, and the loads. Chunk c of the tile, 1 KB each: 2 KK of keys, then KK of
   // values of either page; a wave takes LPT neighbouring ones. Keys: lane l brings the 16 bytes it reads as its fragment
-  // of product h, K[token 8 (l % 16 / 4) + 4 h + l % 4][kk * 32 + l / 16 * 8 ..]; values: as they lie in the page.
+  // of product h, K[token 8 (l % 16 / 4) + 4 h + l % 4][kk * 32 + l / 16 * 8 ..]. Values: 32 dims, the first eight slots of
+  // each, then the last eight, so that sixteen lanes read 256 neighbouring bytes (as they lie in the page, every other 16:
+  // half the banks).
   const uint32_t stride = (uint32_t)(a.n_kv * blk * 4), head_bytes = (uint32_t)(blk * 2);  // of a page, of a head in it
   const uint32_t pages = (uint32_t)min(a.pool_pages, (int64_t)0x7fffffff);
   uint32_t chunk_off[LPT];  // this lane's bytes of a chunk, from its page's head
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     const int c = wave * LPT + i;
     const bool keys = c < 2 * KK;
     chunk_off[i] = keys ? (uint32_t)(c / KK * (4 * D * 2) + c % KK * 64 + (((hl & 4) * 2 + (hl & 3)) * D + rq * 8) * 2)
-                        : (uint32_t)(stride / 2 + c % KK * 1024 + lane * 16);
+                        : (uint32_t)(stride / 2 + c % KK * 1024 + (lane & 31) * 32 + (lane >> 5) * 16);
     chunk_p1[i] = keys ? hl >= 8 : c >= 3 * KK;
   }
   const uint8_t *base0 = nullptr, *base1 = nullptr;
@@ -321,8 +323,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   u32x4 kf[2][KK], vf[NB], p[CB];     // operands of the next products: keys, values and probabilities
   f32x4 s[CB][2];
   float m[CB], l[CB];
-  int col_row[CB], col_lo[CB];        // drafted row (in the sequence) and first visible token of this lane's columns
-  uint64_t col_mask[CB];              // and its mask, where one word holds it
+  int col_lo[CB];                     // first visible token of this lane's columns
+  uint64_t col_mask[CB];              // their rows' masks, or, where those are of several words, the rows themselves
 
   auto task_id = [&]() { return ((int64_t)cb_seq * a.n_kv + head) * max_qt + qt; };
   auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
@@ -351,8 +353,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       const uint16_t *src = a.qkv + (seq.r0 + j) * row_elems + (head * group + c - j * group) * D + rq * 8;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) q[cb][kk] = *(const u32x4 *)(src + kk * 32);
-      col_row[cb] = j;
-      col_mask[cb] = a.max_rows <= 64 ? a.mask[seq.r0 + j] : 0;
+      col_mask[cb] = a.max_rows <= 64 ? a.mask[seq.r0 + j] : (uint64_t)(seq.r0 + j);
       col_lo[cb] = a.window > 0 ? max(0, seq.ctx + clamp_depth(a.depth[seq.r0 + j], a.max_rows) - a.window + 1) : 0;
       m[cb] = kNoScore;
       l[cb] = 0.f;
@@ -401,7 +402,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   // ---- the phases of a tile
   auto key = [&](const uint8_t *src, int half, int kk) { return *(const u32x4 *)(src + half * PB + kk * 1024 + lane * 16); };
   auto value = [&](const uint8_t *src, int nb) {
-    return *(const u32x4 *)(src + (2 + (rq >> 1)) * PB + (nb * 16 + hl) * 32 + (rq & 1) * 16);
+    return *(const u32x4 *)(src + (2 + (rq >> 1)) * PB + (nb >> 1) * 1024 + (rq & 1) * 512 + ((nb & 1) * 16 + hl) * 16);
   };
   // O += V^T P; S = K Q^T. NEXT: an operand is replaced right after its last product, by this tile's values at src_v and
   // the next one's keys at src_k, so the reads run under the products.
@@ -438,7 +439,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
         const int j0 = t0 - seq.ctx;  // drafted token of the tile's first slot (below 0: cached ones come first)
         uint32_t v = words == 1 ? (j0 < 0 ? (j0 > -32 ? (uint32_t)(col_mask[cb] << -j0) : 0u)
                                           : j0 < 64 ? (uint32_t)(col_mask[cb] >> j0) : 0u)
-                                : mask_window(a.mask + (int64_t)(seq.r0 + col_row[cb]) * words, words, j0);
+                                : mask_window(a.mask + (int64_t)col_mask[cb] * words, words, j0);
         v &= bits_between(-j0, seq.end - t0);
         v = v >> (rq * 8) & 0xffu;
         if (a.window > 0 && a.window < a.max_rows) {  // not the drafted tokens `window` positions or more before the row
@@ -593,7 +594,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
         values(std::true_type(), at_slot(slot));
         scores(std::true_type(), at_slot(next_slot(slot)));
 #pragma unroll
-        for (int i = 0; i < NB + 2 * KK; ++i) {  // a read after every pair (CB = 2) of products
+        for (int i = 0; i < NB + 2 * KK; ++i) {  // a read after the products of an operand
           __builtin_amdgcn_sched_group_barrier(0x8, CB, 0);
           __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
