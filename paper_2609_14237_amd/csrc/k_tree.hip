@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
 // kernel joins them.
 //
 // A workgroup is QW waves over one stream of tiles. The tiles (keys and values
-// of two pages) are fetched direct-to-LDS, two or three ahead; each wave holds NQ
+// of two pages) are fetched direct-to-LDS, up to seven ahead; each wave holds NQ
 // of the tile's QT = QW * NQ columns in registers and reads every tile once:
 //   S = K Q^T      16x16x32, twice: 16 tokens by 16 query vectors. Row 4 r + i of
 //                  product h is token 8 r + 4 h + i of the tile, so lane quad r
@@ -164,7 +164,7 @@ struct TreeShape {
 };
 
 template <int D, int NQ, int QW>
-__global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 64 ? 1 : 2))) void tree_attention_kernel(
+__global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) void tree_attention_kernel(
     const DraftArgs a, const int min_tiles, const int max_qt, const int by_task, const float scale_log2, float *__restrict__ rec_acc,
     float2 *__restrict__ rec_ml, TreeDesc *__restrict__ desc) {
   using Shape = TreeShape<D, NQ, QW>;
@@ -180,6 +180,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hl = lane & 15, rq = lane >> 4;
+  const int col0 = NQ * wave;  // this wave's columns of a query tile
   // c / group and c % group of a column, c < 2^13: exact, (c + 1/2) / group is 1/32 off an integer at least
   const float inv_group = 1.f / (float)group;
   auto row_of = [&](int c) { return (int)(((float)c + 0.5f) * inv_group); };
@@ -245,9 +246,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   constexpr int64_t blk = (int64_t)kPage * D;
   int it = 0, islot = 0;   // next unit to fetch, and its slot
   uint32_t ok_bits = 0;    // two bits per fetched unit, the next one to be consumed lowest
-  // The next window's pages come to LDS like the tiles, 32 units before they are used: nothing ever waits for them, where a
-  // wait for a register would drain the tiles in flight (6 us every 32 tiles: 64 sequences x 8192 tokens x 64 rows 634 ->
-  // FIGWIN us).
+  // The next window's pages come to LDS like the tiles, 32 units before they are used: nothing waits for them, where a wait
+  // for a register would drain the tiles in flight.
   int page_cur, head_cur, head_nxt;
   bool has_nxt;
   int *const ids = s_ids + wave * 64;
@@ -344,11 +344,11 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
     qt = max_qt > 1 ? ct % c_qts : 0;
     seg_first = tile;
     const int cols = seq.n * group;
-    busy = qt * QT + wave * NQ < cols;
+    busy = qt * QT + col0 < cols;
     const int64_t row_elems = (int64_t)(a.n_q + 2 * a.n_kv) * D;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
-      const int c = min(qt * QT + wave * NQ + cb * 16 + hl, cols - 1);  // columns past the last repeat it, unwritten
+      const int c = min(qt * QT + col0 + cb * 16 + hl, cols - 1);  // columns past the last repeat it, unwritten
       const int j = row_of(c);
       const uint16_t *src = a.qkv + (seq.r0 + j) * row_elems + (head * group + c - j * group) * D + rq * 8;
 #pragma unroll
@@ -377,7 +377,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
       float sum = l[cb];
       sum += __shfl_xor(sum, 16, kWave);
       sum += __shfl_xor(sum, 32, kWave);
-      const int at = wave * NQ + cb * 16 + hl, c = qt * QT + at;
+      const int at = col0 + cb * 16 + hl, c = qt * QT + at;
       if (c >= cols) continue;
       if (whole) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -555,9 +555,10 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(NQ == 6
   // after its last use, by this tile's values and the next one's keys) and softmax, which also fetches a tile.
   //  - Products of tile t read tiles t and t + 1, so everyone's loads of t + 1 have landed before; softmax of tile t
   //    fetches into the slot of tile t - 1, whose last reads were made in products t - 1.
-  //  - Two or four waves meet once a tile, before its products.
+  //  - Two or four waves meet once a tile, after its softmax.
   //  - Eight waves, two per SIMD, run half a tile apart and meet after either phase: while one of a SIMD's waves is at its
-  //    products the other is at its softmax. In step they queue for the matrix cores and for the vector unit in turn.
+  //    products the other is at its softmax. In step they queue for the matrix cores and for the vector unit in turn (64
+  //    sequences x 8192 tokens x 64 rows: 680 us, apart 630; at 16 columns a wave the two do not differ).
   //    The later half's products t are the earlier half's softmax t: what the products of t + 1 read (tile t + 2) has to
   //    have landed when anyone's products t end.
   //  - One wave alone has no barrier; it reads a tile when it starts on it.
