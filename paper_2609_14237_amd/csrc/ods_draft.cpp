@@ -3,7 +3,6 @@
 // operator range into row-wise runs and drafted KV operators. Plain C++, free
 // of HIP calls; nothing here allocates.
 #include <math.h>
-#include <stdlib.h>
 
 #include <algorithm>
 
@@ -136,13 +135,19 @@ TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_dra
   if (c.window > 0) tokens = std::min(tokens, (int64_t)c.window + draft->max_rows + 64);
   const int64_t units = (int64_t)batch->batch * c.n_kv * p.max_qt * ((tokens + 31) / 32 + 1);
   p.units_ok = units < (int64_t)1 << 30;
-  const int per_cu = p.qt <= 16 ? (c.head_dim == 64 ? 8 : 4) : c.head_dim == 64 && p.qt <= 64 ? 2 : 1;
   p.min_tiles = 2;
-  if (getenv("TREE_MIN")) p.min_tiles = atoi(getenv("TREE_MIN"));
-  const int percu2 = getenv("TREE_PER") ? atoi(getenv("TREE_PER")) : per_cu;
-  p.grid = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)std::max(cus, 1) * percu2, (units + p.min_tiles - 1) / p.min_tiles));
+  cus = std::max(cus, 1);
+  // Workgroups per compute unit. Up to 16 columns are one wave's work and 128 KB of its tiles fit beside each other (64
+  // sequences of up to 4096 tokens, 4 rows, us at 1, 2 and 4 of them: D = 128 124, 121, 126; D = 64 at 4 and 8 of
+  // them 68). Up to 64 columns of 64 dims fit twice, which pays once a range is long (16 rows: 64 sequences 85
+  // us, one each 95; 8 sequences 26 and 22). Else one has all the LDS, or all the matrix cores (32 rows of 64 dims: 130,
+  // two 134).
+  int per_cu = p.qt <= 16 ? 256 / c.head_dim : 1;
+  if (p.qt > 16 && p.qt <= 64 && c.head_dim == 64 && units >= (int64_t)2 * cus * 64) per_cu = 2;
+  p.grid = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)cus * per_cu, (units + p.min_tiles - 1) / p.min_tiles));
+  // A task in many ranges (one sequence: 18 us, by whole waves 23), or few ranges a task (64 ragged sequences: 157 us, by
+  // quarters of a column 173; a window of 1024 on 32 sequences: 48 us, 76).
   p.split_join = p.grid > 6 * (int64_t)batch->batch * c.n_kv * p.max_qt;
-  if (getenv("TREE_SJ")) p.split_join = atoi(getenv("TREE_SJ"));
   return p;
 }
 
