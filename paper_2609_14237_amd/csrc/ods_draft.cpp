@@ -92,7 +92,7 @@ ods_status check_rope_rows(const ods_rope *r, const void *x, int64_t xs, const v
                      (long long)ys, (long long)width);
   if (xs > INT64_MAX / 4 / rows || ys > INT64_MAX / 4 / rows) return set_error(ODS_EINVAL, "%s: strides too large", who);
   const uintptr_t a = (uintptr_t)x, b = (uintptr_t)y;
-  if (a == b && xs == ys) return ODS_OK;
+  if (a == b && (xs == ys || rows == 1)) return ODS_OK;
   const uintptr_t ax = a + (uintptr_t)(((int64_t)(rows - 1) * xs + width) * 2);
   const uintptr_t bx = b + (uintptr_t)(((int64_t)(rows - 1) * ys + width) * 2);
   if (a < bx && b < ax) {  // the spans meet: fine only as columns of the same rows that lie beside each other
