@@ -490,7 +490,7 @@ ods_status ods_kv_copy_pages(const ods_block *blk, int32_t layer_begin, int32_t 
  * moves to that of token position ctx + k, for k < path_len[b], in every layer
  * of [layer_begin, layer_end) (through the ring in ring layers), and
  * ctx_out[b] = ctx + path_len[b] (device [batch]; NULL: not written; may be
- * batch->ctx_lens itself). A path is strictly ascending and below the
+ * batch->ctx_lens itself, else it overlaps no array the call reads). A path is strictly ascending and below the
  * sequence's row count; the first entry that is not ends it there, and a
  * length past path_cols is cut. The slots of a sequence being kept must lie on
  * pages that no other sequence holds. draft: rows, max_rows and row_off are

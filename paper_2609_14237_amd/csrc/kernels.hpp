@@ -105,7 +105,8 @@ struct AcceptArgs {
   const int32_t *row_off, *ctx_lens, *path, *path_len;
 };
 hipError_t launch_copy_pages(const PoolSet &pools, int n_pools, const int32_t *pairs, int n, hipStream_t s);
-hipError_t launch_accept(const AcceptArgs &a, const PoolSet &pools, int n_pools, int max_kv, hipStream_t s);
+// ctx_out: NULL or where the new contexts go; launch_accept_ctx for one that is a.ctx_lens, after all of launch_accept.
+hipError_t launch_accept(const AcceptArgs &a, const PoolSet &pools, int n_pools, int max_kv, int32_t *ctx_out, hipStream_t s);
 hipError_t launch_accept_ctx(const AcceptArgs &a, int32_t *ctx_out, hipStream_t s);
 
 }  // namespace ods

@@ -381,9 +381,14 @@ ods_status ods_kv_accept(const ods_block *blk, int32_t layer_begin, int32_t laye
     a.row_off = draft->row_off; a.ctx_lens = batch->ctx_lens; a.path = path; a.path_len = path_len;
     int max_kv = 0;
     for (int l = layer_begin; l < layer_end; ++l) max_kv = blk->layers[l].cfg.n_kv > max_kv ? blk->layers[l].cfg.n_kv : max_kv;
-    hipError_t e = each_pool_set(blk, layer_begin, layer_end, batch,
-                                 [&](const PoolSet &set, int n) { return launch_accept(a, set, n, max_kv, stream); });
-    if (e == hipSuccess && ctx_out) e = launch_accept_ctx(a, ctx_out, stream);
+    const bool in_place = ctx_out == batch->ctx_lens;
+    int32_t *out = in_place ? nullptr : ctx_out;  // written by the first set's launch
+    hipError_t e = each_pool_set(blk, layer_begin, layer_end, batch, [&](const PoolSet &set, int n) {
+      const hipError_t rc = launch_accept(a, set, n, max_kv, out, stream);
+      out = nullptr;
+      return rc;
+    });
+    if (e == hipSuccess && in_place) e = launch_accept_ctx(a, ctx_out, stream);
     if (e != hipSuccess) return set_error(ODS_EHIP, "ods_kv_accept: %s", hipGetErrorString(e));
   }
   clear_error();

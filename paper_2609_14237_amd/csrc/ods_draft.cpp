@@ -266,8 +266,13 @@ ods_status check_accept(const ods_block *blk, int layer_begin, int layer_end, co
       (rc = check_ptr(draft->row_off, who, "row_off")) != ODS_OK ||
       (ctx_out && (rc = check_ptr(ctx_out, who, "ctx_out")) != ODS_OK))
     return rc;
-  const uintptr_t a = (uintptr_t)ctx_out, b = (uintptr_t)batch->ctx_lens, n = (uintptr_t)batch->batch * 4;
-  if (ctx_out && a != b && a < b + n && b < a + n) return set_error(ODS_EINVAL, "%s: ctx_out overlaps ctx_lens", who);
+  const uintptr_t out = (uintptr_t)ctx_out, out_end = out + (uintptr_t)batch->batch * 4;
+  auto meets = [&](const int32_t *p, int64_t count) {
+    return ctx_out && out < (uintptr_t)p + (uintptr_t)(count * 4) && (uintptr_t)p < out_end;
+  };
+  if ((ctx_out != batch->ctx_lens && meets(batch->ctx_lens, batch->batch)) || meets(path_len, batch->batch) ||
+      meets(path, (int64_t)batch->batch * path_cols) || meets(draft->row_off, (int64_t)batch->batch + 1))
+    return set_error(ODS_EINVAL, "%s: ctx_out overlaps an array the call reads", who);
   for (int l = layer_begin; l < layer_end; ++l)
     if ((rc = check_table(blk->layers[l], l, batch, draft)) != ODS_OK) return rc;
   return ODS_OK;

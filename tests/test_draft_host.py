@@ -205,6 +205,17 @@ def test_page_operator_refusals():
     assert B.ods_kv_copy_pages(none.c, 0, 1, FAKE, 4, None) == B.ODS_EINVAL
 
 
+def test_new_contexts_over_an_array_that_is_read_are_refused():
+    blk, far = fake_block([CFG]), FAKE + 65536
+    acc = lambda out, batch=None, draft=None, path=far, n=far: B.ods_kv_accept(  # noqa: E731
+        blk.c, 0, 1, batch or fake_batch(ctx_lens=far), draft or fake_draft(row_off=far), path, 4, n, out, None)
+    assert acc(FAKE, path=FAKE) == B.ODS_EINVAL
+    assert acc(FAKE, n=FAKE) == B.ODS_EINVAL
+    assert acc(FAKE, draft=fake_draft(row_off=FAKE)) == B.ODS_EINVAL
+    assert acc(FAKE, batch=fake_batch(ctx_lens=FAKE), n=FAKE) == B.ODS_EINVAL      # in place, but over path_len
+    assert "overlaps" in B.ods_last_error()
+
+
 # ---------------------------------------------------------------- page bookkeeping
 
 def check_model(k, contents, rows):
