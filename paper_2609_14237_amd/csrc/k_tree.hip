@@ -7,37 +7,41 @@
 
 #include "draft.hpp"
 #include "kernels.hpp"
+#include "turn.hpp"
 
 namespace ods {
 
 namespace {
 
 // RoPE of the q and k heads of one drafted row and/or append of its k and v to
-// its cache slot. One block per (sequence, drafted row).
+// its cache slot. One block per (sequence, drafted row); bound by memory (64
+// sequences of 64 rows, 40 heads turned, 8 of keys and of values appended: 24 us,
+// two bytes a load 28).
 __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int do_rope, int do_append) {
-  __shared__ float cs[128], sn[128];
+  __shared__ __align__(16) float cs[128], sn[128];
   const int b = blockIdx.x, j = blockIdx.y, D = a.D;
   const DraftSeq q = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
   if (j >= q.n || q.ctx < 0) return;
   uint16_t *row = a.qkv + (int64_t)(q.r0 + j) * (a.n_q + 2 * a.n_kv) * D;
   if (do_rope) {
-    const int p = q.ctx + clamp_depth(a.depth[q.r0 + j], a.max_rows);
-    const int rdim = a.freqs ? a.rdim : D, np = rdim / 2;
-    if (threadIdx.x < np) {
-      float c, s;
-      if (a.freqs)
-        turn_by((double)p * a.freqs[threadIdx.x], c, s);
-      else
-        rope_angle(p, threadIdx.x, D, a.theta, c, s);
-      cs[threadIdx.x] = a.freqs ? c * a.amp : c;
-      sn[threadIdx.x] = a.freqs ? s * a.amp : s;
-    }
-    __syncthreads();
-    for (int t = threadIdx.x; t < (a.n_q + a.n_kv) * np; t += 256) {
-      const int i = t % np, at = t / np * D + (a.interleaved ? 2 * i : i), mate = at + (a.interleaved ? 1 : np);
-      const float u = bf2f(row[at]), v = bf2f(row[mate]), c = cs[i], s = sn[i];
-      row[at] = f2bf(u * c - v * s);
-      row[mate] = f2bf(v * c + u * s);
+    const int rdim = a.freqs ? a.rdim : D, heads = a.n_q + a.n_kv;
+    auto turns = [&]() {
+      const int p = q.ctx + clamp_depth(a.depth[q.r0 + j], a.max_rows);
+      row_turns(rdim / 2, a.freqs ? a.amp : 1.f, cs, sn, [&](int i, float &c, float &s) {
+        if (a.freqs)
+          turn_by((double)p * a.freqs[i], c, s);
+        else
+          rope_angle(p, i, D, a.theta, c, s);
+      });
+    };
+    const bool wide = turns_wide(rdim, a.interleaved);
+    if (wide && a.interleaved) {
+      turn_row<true>(row, row, heads, D, rdim, cs, sn, turns);
+    } else if (wide) {
+      turn_row<false>(row, row, heads, D, rdim, cs, sn, turns);
+    } else {
+      turns();
+      turn_row_by_values(row, row, heads, D, rdim, a.interleaved, cs, sn);
     }
     __syncthreads();
   }
@@ -48,11 +52,12 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
   if (page < 0) return;
   const int64_t blk = (int64_t)kPage * D;
   uint16_t *kb = a.pool + (int64_t)page * 2 * a.n_kv * blk, *vb = kb + a.n_kv * blk;
-  for (int e = threadIdx.x; e < a.n_kv * D; e += 256) {
-    const int g = e / D, i = e % D;
-    kb[g * blk + slot * D + i] = row[a.n_q * D + e];
-    vb[g * blk + i * kPage + slot] = row[(a.n_q + a.n_kv) * D + e];
-  }
+  const uint16_t *k = row + a.n_q * D, *v = k + a.n_kv * D;
+  const int log_d = D == 128 ? 7 : 6;
+  for (int e = threadIdx.x * 8; e < a.n_kv * D; e += 256 * 8)
+    *(u32x4 *)(kb + (e >> log_d) * blk + slot * D + (e & (D - 1))) = *(const u32x4 *)(k + e);
+  for (int e = threadIdx.x; e < a.n_kv * D; e += 256)  // dim-major: two bytes a store
+    vb[(e >> log_d) * blk + (e & (D - 1)) * kPage + slot] = v[e];
 }
 
 // ---------------------------------------------------------------- attention
