@@ -404,3 +404,34 @@ def test_layers_of_different_shapes_share_a_call():
     assert torch.equal(outs[0][0], outs[1][0])
     for p, q in zip(outs[0][1], outs[1][1]):
         assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("batch,rows,n_kv", [(2049, 3, 1), (4096, 2, 2)])
+def test_batches_of_several_launches(batch, rows, n_kv):
+    """More sequences than one launch takes, some left alone, the last launch with few of them."""
+    say("several launches", batch)
+    rng = np.random.default_rng(batch)
+    ctx = rng.integers(-1, 40, batch)
+    c = Case(ctx, rng.integers(0, rows + 1, batch), 2 * n_kv, n_kv, 64, seed=1, max_rows=rows, pad=1).device()
+    c.check(c.attend())
+
+
+@pytest.mark.parametrize("rows", [7, 16, 30])
+def test_short_contexts_in_a_wide_table(rows):
+    """The launch is laid out for the table's length: most workgroups find nothing to do."""
+    say("wide table", rows)
+    rng = np.random.default_rng(rows)
+    c = Case(rng.integers(0, 100, 32), rng.integers(1, rows + 1, 32), 16, 8, 64, seed=2, max_rows=rows, extra_pages=270).device()
+    c.check(c.attend())
+
+
+@pytest.mark.parametrize("n_q,hd,rows", [(2, 64, 4), (2, 128, 24), (8, 128, 40)])
+def test_tables_that_end_with_the_context(n_q, hd, rows):
+    """The context fills the table to a tile's end or a page past it; no drafted token has a slot."""
+    say("full table", rows)
+    c = Case([64, 48, 128, 16, 33], [rows, 1, rows, 3, rows], n_q, 1, hd, seed=5, max_rows=rows)
+    cols = 4
+    c.ctx = np.array([64, 48, 64, 16, 33], np.int32)
+    c.table = np.ascontiguousarray(c.table[:, :cols])
+    c.device()
+    c.check(c.attend())
