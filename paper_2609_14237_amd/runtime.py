@@ -116,6 +116,17 @@ _BUF_DTYPE = {"logits": torch.float32, "topk_w": torch.float32, "topk_ids": torc
               "perm": torch.int32, "slot_pos": torch.int32, "expert_off": torch.int32}
 
 
+def _stream_of(who: str, stream: int | None, *tensors: torch.Tensor | None) -> int:
+    """`stream`, or the current one, which has to be of the device the tensors are on."""
+    if stream is not None:
+        return stream
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{who}: a tensor is on {t.device}, the current device is cuda:{device}")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 class Rope:
     """Rotary positions with their device table of frequencies (ods_rope): theta, the rotated part of the head
     (rotary_dim, default all), pair layout, and scaling for long contexts: "plain", "linear", "base", "rotations" or
@@ -155,7 +166,7 @@ def rope(r: Rope, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor | None =
     width = heads * r.c.head_dim  # the stride of a single row means nothing
     xs, ys = (t.stride(0) if rows > 1 else width for t in (x, y))
     _b._check(_b.ods_rope_rows(r.c, x.data_ptr(), xs, y.data_ptr(), ys, rows, heads, pos.data_ptr(),
-                               current_stream() if stream is None else stream), "ods_rope_rows")
+                               _stream_of("rope", stream, x, y, pos, r.freqs)), "ods_rope_rows")
     return y
 
 
@@ -291,7 +302,7 @@ def run_draft(block: DeviceBlock, op_begin: int, op_end: int, batch: DeviceBatch
     tokens, the drafted ones not among them."""
     draft.check(block, batch)
     st = _b.ods_run_draft(block.c, op_begin, op_end, batch.c, draft.c, state.c,
-                          current_stream() if stream is None else stream)
+                          _stream_of("run_draft", stream, draft.row_off, batch.ctx_lens))
     _b._check(st, f"ods_run_draft[{op_begin},{op_end})")
 
 
@@ -324,19 +335,17 @@ def kv_accept(block: DeviceBlock, batch: DeviceBatch, draft: DeviceDraft, path: 
             raise ValueError(f"kv_accept: {name} must be contiguous int32 {shape}, got {t.dtype} {tuple(t.shape)}")
     a, b = _layers(block, layers)
     st = _b.ods_kv_accept(block.c, a, b, batch.c, draft.c, path.data_ptr(), path.shape[1], path_len.data_ptr(),
-                          _ptr(ctx_out), current_stream() if stream is None else stream)
+                          _ptr(ctx_out), _stream_of("kv_accept", stream, batch.ctx_lens, path, path_len, ctx_out))
     _b._check(st, "ods_kv_accept")
 
 
 def kv_copy_pages(block: DeviceBlock, pairs: torch.Tensor, layers=None, stream: int | None = None) -> None:
     """Copy pages pairs[i, 0] -> pairs[i, 1] (device int32 [n, 2]) in the pools of every layer (or layers = (begin,
     end)). No page may be a dst twice, or both a src and a dst."""
-    if pairs.dtype != torch.int32 or pairs.dim() != 2 or pairs.shape[1] != 2:
-        raise ValueError(f"kv_copy_pages: pairs must be int32 [n, 2], got {pairs.dtype} {tuple(pairs.shape)}")
-    pairs = pairs.contiguous()
+    if pairs.dtype != torch.int32 or pairs.dim() != 2 or pairs.shape[1] != 2 or not pairs.is_contiguous():
+        raise ValueError(f"kv_copy_pages: pairs must be contiguous int32 [n, 2], got {pairs.dtype} {tuple(pairs.shape)}")
     a, b = _layers(block, layers)
-    st = _b.ods_kv_copy_pages(block.c, a, b, pairs.data_ptr(), pairs.shape[0],
-                              current_stream() if stream is None else stream)
+    st = _b.ods_kv_copy_pages(block.c, a, b, pairs.data_ptr(), pairs.shape[0], _stream_of("kv_copy_pages", stream, pairs))
     _b._check(st, "ods_kv_copy_pages")
 
 

@@ -152,3 +152,29 @@ def test_draft_verify_keep_and_decode(kind):
     for b in range(4):
         k.release(b)
     assert k.free == P
+
+
+def test_tensors_off_the_current_device_are_refused():
+    """Host tensors stand in for another device's: the check is the same."""
+    r = R.Rope(64)
+    x, pos = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    for a, b, out in ((x, pos, None), (x.cuda(), pos, None), (x, pos.cuda(), None), (x.cuda(), pos.cuda(), x)):
+        with pytest.raises(ValueError, match="current device"):
+            R.rope(r, a, b, out=out)
+    with pytest.raises(ValueError, match="current device"):
+        R.rope(R.Rope(64, device="cpu"), x.cuda(), pos.cuda())
+    cfg = W.LayerCfg(hidden=256, n_q=4, n_kv=2, head_dim=64, ffn=512)
+    pool = torch.zeros(8, 2, 2, 16 * 64, dtype=torch.bfloat16, device="cuda")
+    block = R.DeviceBlock([cfg], [{}], [pool], 8)
+    ints = lambda *v, **kw: torch.tensor(v, dtype=torch.int32, **kw)  # noqa: E731
+    with pytest.raises(ValueError, match="current device"):
+        R.kv_copy_pages(block, ints(0, 1).reshape(1, 2))
+    with pytest.raises(ValueError, match="contiguous"):
+        R.kv_copy_pages(block, torch.zeros(4, 2, dtype=torch.int32, device="cuda")[:, :1].expand(4, 2))
+    batch = R.DeviceBatch(ints(3, device="cuda"), ints(0, 1, device="cuda").reshape(1, 2))
+    draft = R.DeviceDraft(ints(0, 2), ints(0, 1), torch.ones(2, dtype=torch.int64), max_rows=2)
+    state = R.DeviceState(block, batch, draft=draft)
+    with pytest.raises(ValueError, match="current device"):
+        R.run_draft(block, 4, 5, batch, draft, state)
+    with pytest.raises(ValueError, match="current device"):
+        R.kv_accept(block, batch, draft, ints(0, 1).reshape(1, 2), ints(1))
