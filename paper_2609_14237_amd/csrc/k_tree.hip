@@ -68,12 +68,20 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
 // group) are columns of one problem, and up to QT of them (a query tile) share
 // every K/V byte read.
 //
-// Work split: the (sequence, KV head, query tile, 32-token tile) units of the
-// batch are numbered in that order and workgroup r takes the range [r S, (r +
-// 1) S), so ragged contexts and trees load every workgroup alike. Ranges may
-// end inside a task (sequence, KV head, query tile); such a task leaves a
-// record (sums, running maximum, running denominator) per range, and a second
-// kernel joins them.
+// Work split: a task is a (sequence, KV head, query tile), its units are tiles of
+// 32 tokens. Every workgroup gets a range of units, in one of three ways, which
+// each works out from the same metadata:
+//   - one whole task, where there are no more tasks than workgroups and the
+//     longest is not much longer than an even share;
+//   - up to four whole tasks, dealt out by length (longest first, every second
+//     round backwards), where the longest range that gives is not much longer;
+//   - else the units are numbered in order and cut into equal ranges, which may
+//     end inside a task. Such a task leaves a record (sums, running maximum,
+//     running denominator) per range, and a second kernel joins them.
+// What records cost (written, read, one more change of tasks) is kSplitTiles
+// units' time: 32 sequences of 3600 to 4096 tokens, 24 rows, 8 heads: whole 110
+// us, cut 126; of 2048 to 4096 (32 tiles more than even) 111 and 112; 64 ragged
+// sequences of 512 to 4096: dealt 140 us, cut 157; a window of 1024: 44 and 48.
 //
 // A workgroup is QW waves over one stream of tiles. The tiles (keys and values
 // of two pages) are fetched direct-to-LDS, up to seven ahead; each wave holds NQ
@@ -106,6 +114,7 @@ __device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {  // one conv
 
 constexpr int kTile = 32;   // tokens per tile: two pages
 constexpr float kSlack = 8.f;
+constexpr int kSplitTiles = 24;       // tiles a range may have above an even share, so that no task is cut
 constexpr float kNoScore = -1.7e38f;  // reference point before the first score: any score moves it, and 2^(kNoScore - m) is 0
 
 // Tiles of a sequence: [first, first + n). n = 0: nothing to do; the window of
@@ -133,6 +142,18 @@ __device__ __forceinline__ uint32_t mask_window(const uint64_t *__restrict__ m, 
   uint64_t v = m[w] >> sh;
   if (sh > 32 && w + 1 < words) v |= m[w + 1] << (64 - sh);
   return (uint32_t)v;
+}
+
+// op of this lane's value and those of the lanes below it; op(x, 0) is x.
+template <typename Op>
+__device__ __forceinline__ int wave_scan(int x, Op op) {
+  // within rows of sixteen lanes, then from row to row; a lane without a source takes 0
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = op(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+  return op(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
 }
 
 // The two bf16 halves of a dword as weights of what is not finite: 1 for +inf, 64 for -inf, 4096 for NaN, else 0.
@@ -176,11 +197,12 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   constexpr int KK = D / 32, NB = D / 16, CB = NQ / 16, QT = Shape::QT;
   constexpr int NS = Shape::kSlots, LPT = Shape::kPerWave, THREADS = 64 * QW;
   constexpr int PB = kPage * D * 2;  // bytes of one page block of a head
+  constexpr int DEAL = NQ == 16 ? 4 : 1;  // most whole tasks of a range; wider waves have no registers left for a list
   extern __shared__ __align__(16) int smem[];
   const int B = a.B, group = a.n_q / a.n_kv;
   int *s_pre = smem, *s_first = smem + B + 1, *s_n = s_first + B;  // units before, first tile, tiles of a sequence
   uint8_t *const slots = (uint8_t *)smem + ((3 * B + 1) * 4 + 15) / 16 * 16;
-  __shared__ int s_tot[QW], s_ids[QW * 64];
+  __shared__ int s_tot[QW][3], s_ids[THREADS], s_ord[THREADS], s_list[DEAL][4], s_most;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -190,49 +212,113 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   const float inv_group = 1.f / (float)group;
   auto row_of = [&](int c) { return (int)(((float)c + 0.5f) * inv_group); };
 
-  {  // ---- units before each sequence
+  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  // last i with s_pre[i] <= u
+  auto find = [&](int u) {
+    int i = 0, hi = B;
+    while (hi - i > 1) {
+      const int mid = (i + hi) >> 1;
+      if (s_pre[mid] <= u) i = mid; else hi = mid;
+    }
+    return i;
+  };
+
+  const int r = blockIdx.x, G = gridDim.x;
+  if (!by_task && tid == 0) desc[r].pieces = 0;
+  int total = 0, all_tasks = 0, most = 0, S, each;
+  bool whole = false, dealt = false;  // ranges are lists of whole tasks; dealt out by length
+  // Task of round j of range x.
+  auto deal = [&](int x, int j) { return j & 1 ? (j + 1) * G - 1 - x : j * G + x; };
+  {
     const int per = (B + THREADS - 1) / THREADS;
     const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
-    int loc = 0;
+    int loc = 0, tasks = 0;
     for (int b = b0; b < b1; ++b) {
       const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
       int first, n;
       tiles_of(s, a.window, first, n);
       s_first[b] = first;
       s_n[b] = n;
-      const int u = n * a.n_kv * ((s.n * group + QT - 1) / QT);
-      s_pre[b] = loc;
-      loc += u;
+      const int of_seq = n == 0 ? 0 : a.n_kv * ((s.n * group + QT - 1) / QT);
+      s_pre[b] = of_seq;
+      loc += n * of_seq;
+      tasks += of_seq;
+      most = max(most, n);
     }
-    int inc = loc;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(inc, d, kWave);
-      if (lane >= d) inc += y;
-    }
-    if (lane == 63) s_tot[wave] = inc;
+    auto plus = [](int x, int y) { return x + y; };
+    const int inc = wave_scan(loc, plus), inc_tasks = wave_scan(tasks, plus);
+    most = wave_scan(most, [](int x, int y) { return max(x, y); });
+    if (lane == 63) s_tot[wave][0] = inc, s_tot[wave][1] = inc_tasks, s_tot[wave][2] = most;
     __syncthreads();
-    int run = inc - loc;
-    for (int w = 0; w < wave; ++w) run += s_tot[w];
-    for (int b = b0; b < b1; ++b) s_pre[b] += run;
-    if (tid == THREADS - 1) s_pre[B] = run + loc;
+    int run = inc - loc, run_tasks = inc_tasks - tasks;
+    most = 0;
+    for (int w = 0; w < QW; ++w) {
+      if (w < wave) run += s_tot[w][0], run_tasks += s_tot[w][1];
+      total += s_tot[w][0];
+      all_tasks += s_tot[w][1];
+      most = max(most, s_tot[w][2]);
+    }
+    total = uniform(total);
+    all_tasks = uniform(all_tasks);
+    S = max(min_tiles, (total + G - 1) / G);
+    each = (all_tasks + G - 1) / G;
+    whole = each == 1 && uniform(most) <= S + kSplitTiles;  // then s_pre counts tasks, not units
+    if (DEAL > 1 && each > 1 && each <= DEAL && B <= THREADS) {  // s_ord: sequences by length; s_pre: tasks before each of them
+      const int n = tid < B ? s_n[tid] : 0, of_seq = tid < B ? s_pre[tid] : 0;
+      s_ids[tid] = of_seq;
+      if (tid == 0) s_most = 0;
+      __syncthreads();
+      int rank = 0, before = 0;  // sequences that are longer, and their tasks
+      for (int b = 0; b < B; ++b) {
+        const int m = s_n[b];
+        if (m > n || (m == n && b < tid)) ++rank, before += s_ids[b];
+      }
+      if (tid < B) {
+        s_ord[rank] = tid;
+        s_pre[rank] = before;
+      }
+      __syncthreads();
+      // The longest range has the first or the last task of some sequence.
+      for (int k = before, i = 0; i < 2 && of_seq > 0; k = before + of_seq - 1, ++i) {
+        const int j = k / G, x = j & 1 ? (j + 1) * G - 1 - k : k - j * G;
+        int load = 0;
+        for (int y = 0; y < each; ++y)
+          if (deal(x, y) < all_tasks) load += s_n[s_ord[find(deal(x, y))]];
+        atomicMax(&s_most, load);
+      }
+      __syncthreads();
+      whole = dealt = uniform(s_most) <= S + kSplitTiles;
+      if (!dealt && tid < B) s_pre[tid] = of_seq;  // per is 1
+    }
+    if (!dealt)
+      for (int b = b0; b < b1; ++b) {
+        const int of_seq = s_pre[b];
+        s_pre[b] = whole ? run_tasks : run;
+        run += s_n[b] * of_seq;
+        run_tasks += of_seq;
+      }
+    if (tid == 0) s_pre[B] = whole ? all_tasks : total;
     __syncthreads();
   }
-  const int total = __builtin_amdgcn_readfirstlane(s_pre[B]);
-  const int S = max(min_tiles, (total + (int)gridDim.x - 1) / (int)gridDim.x);
-  const int r = blockIdx.x;
-  if (!by_task && tid == 0) desc[r].pieces = 0;
-  if ((int64_t)r * S >= total) return;
-  const int u0 = r * S, n_w = min(total - u0, S);
-
-  // last b with s_pre[b] <= u: a sequence with units when u < total
-  auto find_seq = [&](int u) {
-    int b = 0, hi = B;
-    while (hi - b > 1) {
-      const int mid = (b + hi) >> 1;
-      if (s_pre[mid] <= u) b = mid; else hi = mid;
+  int u0 = 0, n_w;
+  if (whole) {
+    if (tid < each) {
+      const int k = deal(r, tid), i = k < all_tasks ? find(k) : 0, b = dealt ? s_ord[i] : i;
+      const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
+      s_list[tid][0] = b;
+      s_list[tid][1] = k - s_pre[i];
+      s_list[tid][2] = k < all_tasks ? s_n[b] : 0;
+      s_list[tid][3] = (k - s_pre[i]) / max(1, (s.n * group + QT - 1) / QT);
     }
-    return b;
-  };
+    __syncthreads();
+    n_w = 0;
+    for (int i = 0; i < each; ++i) n_w += uniform(s_list[i][2]);
+    if (n_w == 0) return;
+  } else {
+    if ((int64_t)r * S >= total) return;
+    u0 = r * S;
+    n_w = min(total - u0, S);
+  }
 
   // The page window: of units [t0, t0 + 32) of the range lane l knows page l % 2 of unit t0 + l / 2 and the unit's KV head.
   // entry: where in the table that page stands (-1: nowhere), from LDS alone.
@@ -240,11 +326,22 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
     const int t = t0 + (lane >> 1);
     head = 0;
     if (t >= n_w) return -1;
-    const int u = u0 + t, b = find_seq(u), n = s_n[b];
-    const int off = u - s_pre[b];
-    head = off / n;
-    const int lp = 2 * (s_first[b] + off - head * n) + (lane & 1);
-    if (max_qt > 1) head /= (s_pre[b + 1] - s_pre[b]) / (n * a.n_kv);
+    int b, off = t;
+    if (whole) {
+      int i = 0;
+      if (DEAL > 1)
+        while (i + 1 < each && off >= s_list[i][2]) off -= s_list[i++][2];
+      b = s_list[i][0];
+      head = s_list[i][3];
+    } else {
+      b = find(u0 + t);
+      const int n = s_n[b];
+      off = u0 + t - s_pre[b];
+      head = off / n;
+      off -= head * n;
+      if (max_qt > 1) head /= (s_pre[b + 1] - s_pre[b]) / (n * a.n_kv);
+    }
+    const int lp = 2 * (s_first[b] + off) + (lane & 1);
     if (a.ring <= 0 && lp >= a.cols) return -1;
     return (int64_t)b * a.cols + (a.ring > 0 ? lp % a.ring : lp);
   };
@@ -317,7 +414,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   };
 
   // ---- the task being accumulated
-  int cb_seq = __builtin_amdgcn_readfirstlane(find_seq(u0)), ct, c_n, c_first, c_qts;  // sequence, task in it, its tiles
+  int cb_seq, ct, c_n, c_first, c_qts, item = 0;  // sequence, task in it, its tiles; where in the list
   int tile;                                                                          // next tile of the task
   DraftSeq seq;
   bool busy;                          // this wave has columns in it
@@ -332,14 +429,13 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   uint64_t col_mask[CB];              // their rows' masks, or, where those are of several words, the rows themselves
 
   auto task_id = [&]() { return ((int64_t)cb_seq * a.n_kv + head) * max_qt + qt; };
-  auto uniform = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
   auto load_seq = [&]() {
     c_n = uniform(s_n[cb_seq]);
     c_first = uniform(s_first[cb_seq]);
-    c_qts = max_qt > 1 ? uniform((s_pre[cb_seq + 1] - s_pre[cb_seq]) / (c_n * a.n_kv)) : 1;
     const DraftSeq s = draft_seq((ConstInts)a.row_off, (ConstInts)a.ctx_lens, cb_seq, a.rows, a.max_rows, a.cols, a.ring);
     seq.r0 = uniform(s.r0);
     seq.n = uniform(s.n);
+    c_qts = max_qt > 1 ? (seq.n * group + QT - 1) / QT : 1;
     seq.ctx = uniform(s.ctx);
     seq.end = uniform(s.end);
     seq.cap = s.cap;
@@ -542,8 +638,14 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
     }
   };
 
-  load_seq();
-  {
+  if (whole) {
+    cb_seq = uniform(s_list[0][0]);
+    ct = uniform(s_list[0][1]);
+    tile = 0;
+    load_seq();
+  } else {
+    cb_seq = uniform(find(u0));
+    load_seq();
     const int off = u0 - uniform(s_pre[cb_seq]);
     ct = off / c_n;
     tile = off % c_n;
@@ -654,7 +756,12 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
       first_piece = false;
       tile = 0;
       if (t < n_w) {
-        if (++ct == c_qts * a.n_kv) {
+        if (DEAL > 1 && whole) {
+          ++item;
+          cb_seq = uniform(s_list[item][0]);
+          ct = uniform(s_list[item][1]);
+          load_seq();
+        } else if (++ct == c_qts * a.n_kv) {
           ct = 0;
           ++cb_seq;
           while (uniform(s_pre[cb_seq + 1]) == uniform(s_pre[cb_seq])) ++cb_seq;

@@ -145,8 +145,8 @@ TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_dra
   int per_cu = p.qt <= 16 ? 256 / c.head_dim : 1;
   if (p.qt > 16 && p.qt <= 64 && c.head_dim == 64 && units >= (int64_t)2 * cus * 64) per_cu = 2;
   p.grid = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)cus * per_cu, (units + p.min_tiles - 1) / p.min_tiles));
-  // A task in many ranges (one sequence: 18 us, by whole waves 23), or few ranges a task (64 ragged sequences: 157 us, by
-  // quarters of a column 173; a window of 1024 on 32 sequences: 48 us, 76).
+  // Joining a task of many ranges (one sequence: 18 us, by whole waves 23), or of few (64 ragged sequences cut into even
+  // ranges: 157 us, by quarters of a column 173).
   p.split_join = p.grid > 6 * (int64_t)batch->batch * c.n_kv * p.max_qt;
   return p;
 }

@@ -435,3 +435,26 @@ def test_tables_that_end_with_the_context(n_q, hd, rows):
     c.table = np.ascontiguousarray(c.table[:, :cols])
     c.device()
     c.check(c.attend())
+
+
+@pytest.mark.parametrize("batch,n_q,n_kv,hd,rows", [(160, 8, 2, 64, 8), (200, 16, 4, 64, 5), (90, 12, 3, 128, 30), (40, 16, 16, 64, 3),
+                                                    (130, 6, 6, 128, 20)])
+@pytest.mark.parametrize("longest", [0, 6000])
+def test_more_tasks_than_workgroups(batch, n_q, n_kv, hd, rows, longest):
+    """Two to four whole tasks for each workgroup, or, with one long sequence among them, tasks in several."""
+    say("dealt", batch, n_kv, longest)
+    rng = np.random.default_rng(batch + n_kv)
+    ctx, n = rng.integers(-40, 500, batch), rng.integers(0, rows + 1, batch)
+    if longest:
+        ctx[batch // 3], n[batch // 3] = longest, rows
+    c = Case(np.maximum(ctx, -1), n, n_q, n_kv, hd, seed=7, max_rows=rows, pad=2).device()
+    c.check(c.attend())
+
+
+def test_sequences_of_one_length():
+    """Equal tasks, one to a workgroup and two, and a window that cuts unequal contexts to equal tasks."""
+    say("equal")
+    for batch, n_kv, window in ((20, 2, 0), (150, 2, 0), (64, 8, 0), (60, 4, 100)):
+        ctx = np.full(batch, 300) if not window else 300 + 7 * np.arange(batch)
+        c = Case(ctx, np.full(batch, 6), 2 * n_kv, n_kv, 64, window=window, seed=batch, max_rows=12).device()
+        c.check(c.attend())
