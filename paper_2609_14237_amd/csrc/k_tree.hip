@@ -189,7 +189,8 @@ struct TreeShape {
   static constexpr int kPerWave = kChunks / QW;
 };
 
-template <int D, int NQ, int QW>
+// STREAM: K and V go past the caches.
+template <int D, int NQ, int QW, bool STREAM>
 __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) void tree_attention_kernel(
     const DraftArgs a, const int min_tiles, const int max_qt, const int by_task, const float scale_log2, float *__restrict__ rec_acc,
     float2 *__restrict__ rec_ml, TreeDesc *__restrict__ desc) {
@@ -409,7 +410,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
     for (int i = 0; i < LPT; ++i)
       __builtin_amdgcn_global_load_lds((const void *)((chunk_p1[i] ? base1 : base0) + chunk_off[i]),
-                                       (__attribute__((address_space(3))) void *)(dst + (wave * LPT + i) * 1024), 16, 0, 0);
+                                       (__attribute__((address_space(3))) void *)(dst + (wave * LPT + i) * 1024), 16, 0,
+                                       STREAM ? 2 : 0);  // 2: nt
     islot = islot + 1 == NS ? 0 : islot + 1;
   };
 
@@ -913,12 +915,12 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const
 // on the same records.
 constexpr int kTreeBatch = 2048;
 
-template <int D, int NQ, int QW>
+template <int D, int NQ, int QW, bool STREAM>
 hipError_t go_tree(DraftArgs a, const TreePlan &plan, void *ws, hipStream_t s) {
   using Shape = TreeShape<D, NQ, QW>;
   static std::atomic<uint64_t> lds_set{0};  // devices whose LDS limit is raised
   auto lds = [](int B) { return ((3 * (size_t)B + 1) * 4 + 15) / 16 * 16 + (size_t)Shape::kSlots * Shape::kTileBytes; };
-  const auto kern = tree_attention_kernel<D, NQ, QW>;
+  const auto kern = tree_attention_kernel<D, NQ, QW, STREAM>;
   if (hipError_t e = ensure_lds_limit((const void *)kern, lds(kTreeBatch), lds_set); e != hipSuccess) return e;
   static_assert(sizeof(TreeDesc) <= kTreeDescBytes, "descriptor size");
   TreeDesc *desc = (TreeDesc *)ws;
@@ -955,18 +957,22 @@ hipError_t launch_draft_rope_append(const DraftArgs &a, bool do_rope, bool do_ap
 }
 
 hipError_t launch_tree_attention(const DraftArgs &a, const TreePlan &plan, void *ws, hipStream_t s) {
-  auto of_dim = [&](auto d) {
+  auto of = [&](auto d, auto stream) {
     constexpr int D = decltype(d)::value;
+    constexpr bool STREAM = decltype(stream)::value;
     switch (plan.qt) {
-      case 16: return go_tree<D, 16, 1>(a, plan, ws, s);
-      case 32: return go_tree<D, 16, 2>(a, plan, ws, s);
-      case 64: return go_tree<D, 16, 4>(a, plan, ws, s);
-      case 128: return go_tree<D, 16, 8>(a, plan, ws, s);
-      case 256: return go_tree<D, 32, 8>(a, plan, ws, s);
+      case 16: return go_tree<D, 16, 1, STREAM>(a, plan, ws, s);
+      case 32: return go_tree<D, 16, 2, STREAM>(a, plan, ws, s);
+      case 64: return go_tree<D, 16, 4, STREAM>(a, plan, ws, s);
+      case 128: return go_tree<D, 16, 8, STREAM>(a, plan, ws, s);
+      case 256: return go_tree<D, 32, 8, STREAM>(a, plan, ws, s);
     }
     return hipErrorInvalidValue;
   };
-  return a.D == 128 ? of_dim(std::integral_constant<int, 128>()) : of_dim(std::integral_constant<int, 64>());
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  if (plan.stream) return a.D == 128 ? of(D128(), std::true_type()) : of(D64(), std::true_type());
+  return a.D == 128 ? of(D128(), std::false_type()) : of(D64(), std::false_type());
 }
 
 }  // namespace ods

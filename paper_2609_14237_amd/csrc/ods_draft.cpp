@@ -145,6 +145,10 @@ TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_dra
   int per_cu = p.qt <= 16 ? 256 / c.head_dim : 1;
   if (p.qt > 16 && p.qt <= 64 && c.head_dim == 64 && units >= (int64_t)2 * cus * 64) per_cu = 2;
   p.grid = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)cus * per_cu, (units + p.min_tiles - 1) / p.min_tiles));
+  // Each tile is read once, and all of them are more than the last-level cache holds (256 MB): past the caches (64
+  // sequences of 9216 tokens, 4 rows: 362 us, through them 402; 64 ragged ones 129, 138). What fits may still be there
+  // (16 sequences of 1000 to 2000 tokens, read again: 32 us, 34 past the caches), and query tiles read the same tiles again.
+  p.stream = p.max_qt == 1 && units * 32 * c.head_dim * 4 > (int64_t)256 << 20;
   // Joining a task of many ranges (one sequence: 18 us, by whole waves 23), or of few (64 ragged sequences cut into even
   // ranges: 157 us, by quarters of a column 173).
   p.split_join = p.grid > 6 * (int64_t)batch->batch * c.n_kv * p.max_qt;

@@ -458,3 +458,15 @@ def test_sequences_of_one_length():
         ctx = np.full(batch, 300) if not window else 300 + 7 * np.arange(batch)
         c = Case(ctx, np.full(batch, 6), 2 * n_kv, n_kv, 64, window=window, seed=batch, max_rows=12).device()
         c.check(c.attend())
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("rows", [3, 7, 14, 30, 50])
+def test_every_width_past_the_caches(hd, rows):
+    """A table of 70000 tokens: more than the caches hold, so K and V are not read through them."""
+    say("past the caches", hd, rows)
+    rng = np.random.default_rng(rows)
+    c = Case(rng.integers(0, 700, 8), rng.integers(1, rows + 1, 8), 8, 2, hd, seed=rows, max_rows=rows)
+    c.table = np.pad(c.table, ((0, 0), (0, 4400)))
+    c.device()
+    c.check(c.attend())
