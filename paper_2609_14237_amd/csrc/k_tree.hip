@@ -79,9 +79,10 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
 //     end inside a task. Such a task leaves a record (sums, running maximum,
 //     running denominator) per range, and a second kernel joins them.
 // What records cost (written, read, one more change of tasks) is kSplitTiles
-// units' time: 32 sequences of 3600 to 4096 tokens, 24 rows, 8 heads: whole 110
-// us, cut 126; of 2048 to 4096 (32 tiles more than even) 111 and 112; 64 ragged
-// sequences of 512 to 4096: dealt 140 us, cut 157; a window of 1024: 44 and 48.
+// units' time. Through the caches: 32 sequences of 3600 to 4096 tokens, 24 rows,
+// 8 heads: whole 110 us, cut 126; of 2048 to 4096 (32 tiles more than even) 111
+// and 112; 64 ragged sequences of 512 to 4096: dealt 140 us, cut 157 (past the
+// caches, as such a batch now is, dealt 129).
 //
 // A workgroup is QW waves over one stream of tiles. The tiles (keys and values
 // of two pages) are fetched direct-to-LDS, up to seven ahead; each wave holds NQ
@@ -183,8 +184,8 @@ template <int D, int NQ, int QW>
 struct TreeShape {
   static constexpr int QT = NQ * QW;
   static constexpr int kTileBytes = kTile * D * 2 * 2;
-  // Tiles in LDS: 128 KB of them, or two of each of the one-wave workgroups that share a compute unit.
-  static constexpr int kSlots = QW == 1 ? 2 : 8;
+  // Tiles in LDS: 128 KB of them, or 64 or 32 for each of the smaller workgroups that share a compute unit.
+  static constexpr int kSlots = QW == 1 ? 2 : QW <= 4 ? 4 : 8;
   static constexpr int kChunks = kTileBytes / 1024;   // 1 KB direct-to-LDS loads of a tile
   static constexpr int kPerWave = kChunks / QW;
 };
@@ -661,17 +662,21 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   open_task();  // ends with a wait for every load
   int t = 0;
   // A tile takes two phases: products (the last tile's values, then this one's scores; each operand is replaced from LDS
-  // after its last use, by this tile's values and the next one's keys) and softmax, which also fetches a tile.
-  //  - Products of tile t read tiles t and t + 1, so everyone's loads of t + 1 have landed before; softmax of tile t
-  //    fetches into the slot of tile t - 1, whose last reads were made in products t - 1.
-  //  - Two or four waves meet once a tile, after its softmax.
-  //  - Eight waves, two per SIMD, run half a tile apart and meet after either phase: while one of a SIMD's waves is at its
-  //    products the other is at its softmax. In step they queue for the matrix cores and for the vector unit in turn (64
-  //    sequences x 8192 tokens x 64 rows: 680 us, apart 630; at 16 columns a wave the two do not differ).
+  // after its last use) and softmax, which also fetches a tile.
+  //  - Softmax of tile t fetches into the slot of tile t - 1, whose last reads were made in products t - 1.
+  //  - Two or four waves meet once a tile, after its softmax; another workgroup of the compute unit fills the gaps. Products
+  //    of tile t read its keys first, so one tile fewer has to have landed (24 rows x 64 sequences: 123 us with the keys
+  //    read a tile ahead, 112).
+  //  - Eight waves have a compute unit to themselves. Their products read the next tile's keys, so that the reads run under
+  //    the products: everyone's loads of t + 1 have landed before products t. The two waves of a SIMD run half a tile apart
+  //    and all meet after either phase: while one is at its products the other is at its softmax. In step they queue for
+  //    the matrix cores and for the vector unit in turn (64 sequences x 8192 tokens x 64 rows: 680 us, apart 630; at 16
+  //    columns a wave the two do not differ).
   //    The later half's products t are the earlier half's softmax t: what the products of t + 1 read (tile t + 2) has to
   //    have landed when anyone's products t end.
   //  - One wave alone has no barrier; it reads a tile when it starts on it.
   constexpr bool PING = QW == 8;
+  constexpr bool AHEAD = QW == 8;  // keys are read a tile ahead
   int slot = 0;
   auto next_slot = [](int x) { return x + 1 == NS ? 0 : x + 1; };
   auto at_slot = [&](int x) { return (const uint8_t *)(slots + x * Shape::kTileBytes); };
@@ -686,7 +691,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   };
   using All = std::integral_constant<int, 63 / LPT>;  // as many as the counter holds: no wait
   using Prod = std::integral_constant<int, PING ? NS - 4 : 63 / LPT>;
-  using Soft = std::integral_constant<int, PING || QW == 1 ? 63 / LPT : NS - 3>;
+  using Soft = std::integral_constant<int, PING || QW == 1 ? 63 / LPT : AHEAD ? NS - 3 : NS - 2>;
   auto first_keys = [&]() {
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -695,16 +700,18 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   };
   if (QW > 1) {
     asm volatile("s_barrier" ::: "memory");
-    first_keys();
+    if (AHEAD) first_keys();
   }
   if (PING && wave >= 4) meet(All(), true);
   auto products = [&]() {
     if (QW > 1) {
       if (busy) {
+        if (!AHEAD) first_keys();
         values(std::true_type(), at_slot(slot));
-        scores(std::true_type(), at_slot(next_slot(slot)));
+        scores(std::integral_constant<bool, AHEAD>(), at_slot(next_slot(slot)));
+        if (!AHEAD) __builtin_amdgcn_sched_group_barrier(0x100, 2 * KK, 0);
 #pragma unroll
-        for (int i = 0; i < NB + 2 * KK; ++i) {  // a read after the products of an operand
+        for (int i = 0; i < (AHEAD ? NB + 2 * KK : NB); ++i) {  // a read after the products of an operand
           __builtin_amdgcn_sched_group_barrier(0x8, CB, 0);
           __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
@@ -770,7 +777,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
           load_seq();
         }
         open_task();
-        if (QW > 1) first_keys();  // the last products did not read them if this wave had no columns there
+        if (AHEAD) first_keys();  // the last products did not read them if this wave had no columns there
       }
       if (PING && wave >= 4) meet(All(), true);
     }
@@ -964,7 +971,9 @@ hipError_t launch_tree_attention(const DraftArgs &a, const TreePlan &plan, void 
       case 16: return go_tree<D, 16, 1, STREAM>(a, plan, ws, s);
       case 32: return go_tree<D, 16, 2, STREAM>(a, plan, ws, s);
       case 64: return go_tree<D, 16, 4, STREAM>(a, plan, ws, s);
-      case 128: return go_tree<D, 16, 8, STREAM>(a, plan, ws, s);
+      case 128:
+        if (plan.equal) return go_tree<D, 32, 4, STREAM>(a, plan, ws, s);
+        return go_tree<D, 16, 8, STREAM>(a, plan, ws, s);
       case 256: return go_tree<D, 32, 8, STREAM>(a, plan, ws, s);
     }
     return hipErrorInvalidValue;

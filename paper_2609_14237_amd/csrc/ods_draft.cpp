@@ -137,13 +137,17 @@ TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_dra
   p.units_ok = units < (int64_t)1 << 30;
   p.min_tiles = 2;
   cus = std::max(cus, 1);
-  // Workgroups per compute unit. Up to 16 columns are one wave's work and 128 KB of its tiles fit beside each other (64
-  // sequences of up to 4096 tokens, 4 rows, us at 1, 2 and 4 of them: D = 128 124, 121, 126; D = 64 at 4 and 8 of
-  // them 68). Up to 64 columns of 64 dims fit twice, which pays once a range is long (16 rows: 64 sequences 85
-  // us, one each 95; 8 sequences 26 and 22). Else one has all the LDS, or all the matrix cores (32 rows of 64 dims: 130,
-  // two 134).
+  // 128 columns: a window makes the tasks nearly equal, so that they need no cutting or dealing, and two workgroups of four
+  // waves fill each other's gaps (32 sequences, window 1024: 42 us, one of eight waves 44; 64 of 2304 tokens each 112, 139).
+  // Contexts that differ are better dealt out to workgroups of eight (64 of 512 to 4096: 129 us, 139).
+  p.equal = p.qt == 128 && c.window > 0;
+  // Workgroups per compute unit. Up to 16 columns are one wave's work, and two have room (64 sequences of up to 4096
+  // tokens, 4 rows, us at 1, 2 and 4: D = 128 124, 121, 126; D = 64 at 4 and 8 68). The workgroups of two or four waves
+  // fit twice, which pays once a range is long (64 sequences of 2304 tokens, 16 rows: 102 us, one each 119; 8 of 2000 to 8000,
+  // 12 rows: 44 and 42). Eight waves have all the LDS.
+  const bool small = p.qt <= 64 || p.equal;
   int per_cu = p.qt <= 16 ? 256 / c.head_dim : 1;
-  if (p.qt > 16 && p.qt <= 64 && c.head_dim == 64 && units >= (int64_t)2 * cus * 64) per_cu = 2;
+  if (p.qt > 16 && small && units >= (int64_t)2 * cus * 64) per_cu = 2;
   p.grid = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)cus * per_cu, (units + p.min_tiles - 1) / p.min_tiles));
   // Each tile is read once, and all of them are more than the last-level cache holds (256 MB): past the caches (64
   // sequences of 9216 tokens, 4 rows: 362 us, through them 402; 64 ragged ones 129, 138). What fits may still be there

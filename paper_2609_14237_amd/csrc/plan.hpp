@@ -206,6 +206,7 @@ struct TreePlan {
   int max_qt;     // query tiles of the longest tree
   int grid;       // workgroups, one range each
   int min_tiles;  // fewest 32-token tiles in a range
+  bool equal;     // 128 columns as four waves of 32, two workgroups per compute unit
   bool stream;    // K and V are read past the caches
   bool split_join;  // records of a column are shared by four waves
   bool units_ok;  // batch * n_kv * query tiles * tiles fits the kernel's unit index

@@ -470,3 +470,15 @@ def test_every_width_past_the_caches(hd, rows):
     c.table = np.pad(c.table, ((0, 0), (0, 4400)))
     c.device()
     c.check(c.attend())
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("batch,rows", [(5, 17), (60, 32), (1100, 32)])
+def test_windows_of_wide_trees(hd, batch, rows):
+    """65 to 128 query vectors per KV head in a sliding-window layer; the largest batch reads more than the caches hold."""
+    say("wide windows", hd, batch, rows)
+    rng = np.random.default_rng(batch)
+    n = rng.integers(0, rows + 1, batch) if batch < 100 else rng.integers(0, 3, batch)
+    n[0] = rows
+    c = Case(rng.integers(-1, 300, batch), n, 8, 2, hd, window=100, seed=3, max_rows=rows, pad=1).device()
+    c.check(c.attend())
