@@ -115,7 +115,6 @@ __device__ __forceinline__ uint32_t pack_pair(float lo, float hi) {  // one conv
 
 constexpr int kTile = 32;   // tokens per tile: two pages
 constexpr float kSlack = 8.f;
-constexpr int kSplitTiles = 24;       // tiles a range may have above an even share, so that no task is cut
 constexpr float kNoScore = -1.7e38f;  // reference point before the first score: any score moves it, and 2^(kNoScore - m) is 0
 
 // Tiles of a sequence: [first, first + n). n = 0: nothing to do; the window of
@@ -180,6 +179,15 @@ struct TreeDesc {
   int head;        // KV head
 };
 
+// Outputs of a sequence that is left alone; `threads` of them.
+__device__ __forceinline__ void zero_left_alone(const DraftArgs &a, int b, int threads) {
+  if (a.ctx_lens[b] >= 0) return;
+  const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
+  const int64_t n = (int64_t)s.n * a.n_q * a.D / 8;
+  u32x4 *dst = (u32x4 *)(a.o + (int64_t)s.r0 * a.n_q * a.D);
+  for (int64_t i = threadIdx.x; i < n; i += threads) dst[i] = u32x4{0u, 0u, 0u, 0u};
+}
+
 template <int D, int NQ, int QW>
 struct TreeShape {
   static constexpr int QT = NQ * QW;
@@ -193,7 +201,8 @@ struct TreeShape {
 // STREAM: K and V go past the caches.
 template <int D, int NQ, int QW, bool STREAM>
 __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) void tree_attention_kernel(
-    const DraftArgs a, const int min_tiles, const int max_qt, const int by_task, const float scale_log2, float *__restrict__ rec_acc,
+    const DraftArgs a, const int min_tiles, const int max_qt, const int by_task,
+    const int no_cut, const float scale_log2, float *__restrict__ rec_acc,
     float2 *__restrict__ rec_ml, TreeDesc *__restrict__ desc) {
   using Shape = TreeShape<D, NQ, QW>;
   constexpr int KK = D / 32, NB = D / 16, CB = NQ / 16, QT = Shape::QT;
@@ -227,6 +236,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
 
   const int r = blockIdx.x, G = gridDim.x;
   if (!by_task && tid == 0) desc[r].pieces = 0;
+  if (no_cut)  // no second launch
+    for (int b = r; b < B; b += G) zero_left_alone(a, b, THREADS);
   int total = 0, all_tasks = 0, most = 0, S, each;
   bool whole = false, dealt = false;  // ranges are lists of whole tasks; dealt out by length
   // Task of round j of range x.
@@ -824,13 +835,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const
     zero = zero && blockIdx.x % (a.n_kv * max_qt) == 0;
   }
   if (zero) {
-    for (int b = b0; b < a.B; b += step) {
-      if (a.ctx_lens[b] >= 0) continue;
-      const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
-      const int64_t n = (int64_t)s.n * a.n_q * D / 8;
-      u32x4 *dst = (u32x4 *)(a.o + (int64_t)s.r0 * a.n_q * D);
-      for (int64_t i = threadIdx.x; i < n; i += 256) dst[i] = u32x4{0u, 0u, 0u, 0u};
-    }
+    for (int b = b0; b < a.B; b += step) zero_left_alone(a, b, 256);
   }
   if (by_task) {
     const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b0, a.rows, a.max_rows, a.cols, a.ring);
@@ -939,16 +944,18 @@ hipError_t go_tree(DraftArgs a, const TreePlan &plan, void *ws, hipStream_t s) {
     a.B = B - b0 < kTreeBatch ? B - b0 : kTreeBatch;
     const int64_t tasks = (int64_t)a.B * a.n_kv * plan.max_qt;
     const int by_task = tasks <= plan.grid, blocks = by_task ? (int)tasks : plan.grid;
-    hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * QW), lds(a.B), s, a, plan.min_tiles, plan.max_qt, by_task, scale, acc,
+    hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * QW), lds(a.B), s, a, plan.min_tiles, plan.max_qt, by_task, (int)plan.no_cut, scale, acc,
                        ml, desc);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (plan.split_join)
-      hipLaunchKernelGGL((tree_join_kernel<D, true>), dim3(blocks, plan.qt), dim3(256), 0, s, a, plan.qt, plan.max_qt, by_task,
-                         acc, ml, desc);
-    else
-      hipLaunchKernelGGL((tree_join_kernel<D, false>), dim3(blocks, plan.qt / 16), dim3(256), 0, s, a, plan.qt, plan.max_qt,
-                         by_task, acc, ml, desc);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (!plan.no_cut) {
+      if (plan.split_join)
+        hipLaunchKernelGGL((tree_join_kernel<D, true>), dim3(blocks, plan.qt), dim3(256), 0, s, a, plan.qt, plan.max_qt,
+                           by_task, acc, ml, desc);
+      else
+        hipLaunchKernelGGL((tree_join_kernel<D, false>), dim3(blocks, plan.qt / 16), dim3(256), 0, s, a, plan.qt, plan.max_qt,
+                           by_task, acc, ml, desc);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
     a.row_off += a.B;
     a.ctx_lens += a.B;
     a.table += (int64_t)a.B * a.cols;

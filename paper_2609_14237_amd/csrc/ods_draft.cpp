@@ -155,6 +155,10 @@ TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_dra
   p.stream = p.max_qt == 1 && units * 32 * c.head_dim * 4 > (int64_t)256 << 20;
   // Joining a task of many ranges (one sequence: 18 us, by whole waves 23), or of few (64 ragged sequences cut into even
   // ranges: 157 us, by quarters of a column 173).
+  // One task a range, none long enough to be cut, whatever the contexts (4 short sequences: 7 us, with the second launch
+  // 10).
+  const int64_t tasks = (int64_t)batch->batch * c.n_kv * p.max_qt;
+  p.no_cut = tasks <= p.grid && (tokens + 31) / 32 + 1 <= p.min_tiles + kSplitTiles;
   p.split_join = p.grid > 6 * (int64_t)batch->batch * c.n_kv * p.max_qt;
   return p;
 }

@@ -201,6 +201,9 @@ ods_status check_rope_rows(const ods_rope *r, const void *x, int64_t xs, const v
                            const int32_t *pos);
 
 // Attention over drafted rows: query tile width and launch shape.
+// Tiles a range may have above an even share, so that no task is cut.
+constexpr int kSplitTiles = 24;
+
 struct TreePlan {
   int qt;         // query vectors of a KV head that share a stream of tiles: 16, 32, 64, 128 or 256
   int max_qt;     // query tiles of the longest tree
@@ -208,6 +211,7 @@ struct TreePlan {
   int min_tiles;  // fewest 32-token tiles in a range
   bool equal;     // 128 columns as four waves of 32, two workgroups per compute unit
   bool stream;    // K and V are read past the caches
+  bool no_cut;    // no task can lie in two ranges: nothing to join
   bool split_join;  // records of a column are shared by four waves
   bool units_ok;  // batch * n_kv * query tiles * tiles fits the kernel's unit index
 };

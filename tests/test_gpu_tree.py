@@ -482,3 +482,13 @@ def test_windows_of_wide_trees(hd, batch, rows):
     n[0] = rows
     c = Case(rng.integers(-1, 300, batch), n, 8, 2, hd, window=100, seed=3, max_rows=rows, pad=1).device()
     c.check(c.attend())
+
+
+@pytest.mark.parametrize("hd,n_q,n_kv,rows", [(64, 4, 2, 6), (128, 8, 2, 40), (128, 8, 1, 33)])
+@pytest.mark.parametrize("window,ring", [(0, 0), (60, 0), (60, 9)])
+def test_small_calls_in_one_launch(hd, n_q, n_kv, rows, window, ring):
+    """No task can be cut: sequences that are left alone get their zeros from the same launch."""
+    say("one launch", hd, rows, window, ring)
+    c = Case([300, -1, 0, 40, -7, 500, -1], [rows, 3, 2, rows, rows, 1, 0], n_q, n_kv, hd, window=window, ring=ring, seed=4,
+             max_rows=rows, pad=2).device()
+    c.check(c.attend())
