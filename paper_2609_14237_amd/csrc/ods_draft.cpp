@@ -135,7 +135,7 @@ TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_dra
   if (c.window > 0) tokens = std::min(tokens, (int64_t)c.window + draft->max_rows + 64);
   const int64_t units = (int64_t)batch->batch * c.n_kv * p.max_qt * ((tokens + 31) / 32 + 1);
   p.units_ok = units < (int64_t)1 << 30;
-  p.min_tiles = 2;
+  p.min_tiles = 4;  // one sequence of 3000 tokens, us at 2, 4 and 6: 16 rows 17.3, 16.8, 17.0, 32 rows 24.7, 23.8, 24.1
   cus = std::max(cus, 1);
   // 128 columns: a window makes the tasks nearly equal, so that they need no cutting or dealing, and two workgroups of four
   // waves fill each other's gaps (32 sequences, window 1024: 42 us, one of eight waves 44; 64 of 2304 tokens each 112, 139).
