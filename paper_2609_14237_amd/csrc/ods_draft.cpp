@@ -214,6 +214,7 @@ ods_status validate_draft(const ods_block *blk, int op_begin, int op_end, const 
   if ((rc = check_draft_sizes(blk, op_begin, op_end, batch, draft)) != ODS_OK) return rc;
   if (batch->batch == 0 || draft->rows == 0) return ODS_OK;
   const ods_batch rb = row_batch(batch, draft);
+  size_t need = 0;  // of the whole range: worked out once, at its first attention
   for (int g = op_begin; g < op_end;) {
     const DraftStep s = draft_step(blk, g, op_end);
     g = s.end;
@@ -240,7 +241,7 @@ ods_status validate_draft(const ods_block *blk, int op_begin, int op_end, const 
       if ((rc = check_ptr(draft->mask, who, "mask")) != ODS_OK || (rc = check_ptr(st->o, who, "o")) != ODS_OK ||
           (rc = check_ptr(st->ws, who, "ws")) != ODS_OK)
         return rc;
-      const size_t need = draft_ws_bytes(blk, op_begin, op_end, batch, draft, cus);
+      if (need == 0) need = draft_ws_bytes(blk, op_begin, op_end, batch, draft, cus);
       if (st->ws_bytes < need) return set_error(ODS_ENOMEM, "workspace %zu bytes < required %zu", st->ws_bytes, need);
     }
   }

@@ -1,0 +1,25 @@
+"""Host checks, without a GPU, of what a drafted range's validation costs and how its workspace is sized, under the CPU
+sanitizers."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CXX = os.environ.get("CXX", "g++")
+
+
+@pytest.mark.skipif(shutil.which(CXX) is None, reason="no host C++ compiler")
+def test_sizes_of_drafted_ranges(tmp_path):
+    exe, src = tmp_path / "draft_sizes_check", os.path.join(ROOT, "paper_2609_14237_amd", "csrc")
+    cmd = [CXX, "-std=c++17", "-g", "-O1", "-fno-omit-frame-pointer", "-fsanitize=address,undefined",
+           "-fno-sanitize-recover=all", "-D__HIP_PLATFORM_AMD__", "-I", "/opt/rocm/include", "-I",
+           os.path.join(ROOT, "include"), *(os.path.join(src, f) for f in ("ods_host.cpp", "ods_draft.cpp", "ods_pages.cpp")),
+           os.path.join(ROOT, "tests", "host", "draft_sizes_check.cpp"), "-o", str(exe)]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-4000:]
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
+    r = subprocess.run([str(exe)], capture_output=True, text=True, env=env, timeout=600)
+    assert r.returncode == 0, (r.stdout + r.stderr)[-4000:]
+    assert "draft_sizes_check OK" in r.stdout
