@@ -413,8 +413,10 @@ typedef struct {
   const ods_rope *rope;
 } ods_draft;
 
-/* Minimum ods_state.ws_bytes for any operator range of this block, batch and
- * draft (its pointers are not read); 0 on invalid arguments. */
+/* An ods_state.ws_bytes that is enough for any operator range of this block, for
+ * this batch and draft (its pointers are not read) and for every one of no more
+ * sequences, rows and max_rows over no wider a table: a state sized once for the
+ * widest trees serves all others. 0 on invalid arguments. */
 size_t ods_draft_workspace_bytes(const ods_block *blk, const ods_batch *batch, const ods_draft *draft);
 
 /* Enqueue operators [op_begin, op_end) of the block for drafted rows: the

@@ -318,7 +318,7 @@ ods_status ods_rope_rows(const ods_rope *rope, const void *x, int64_t x_stride, 
 
 size_t ods_draft_workspace_bytes(const ods_block *blk, const ods_batch *batch, const ods_draft *draft) {
   if (check_block(blk) != ODS_OK || check_draft_sizes(blk, 0, num_ops(blk), batch, draft) != ODS_OK) return 0;
-  return draft_ws_bytes(blk, 0, num_ops(blk), batch, draft, num_cus());
+  return draft_ws_most(blk, batch, draft, num_cus());
 }
 
 ods_status ods_run_draft(const ods_block *blk, int32_t op_begin, int32_t op_end, const ods_batch *batch,

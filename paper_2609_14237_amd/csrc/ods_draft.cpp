@@ -187,6 +187,24 @@ size_t draft_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_
   return w;
 }
 
+size_t draft_ws_most(const ods_block *blk, const ods_batch *batch, const ods_draft *draft, int cus) {
+  size_t w = std::max<size_t>(256, rows_ws_most(blk, draft->rows));
+  for (int l = 0; l < blk->n_layers; ++l) {
+    const ods_layer_cfg &c = blk->layers[l].cfg;
+    auto take = [&](int max_rows) {
+      ods_draft d = *draft;
+      d.max_rows = max_rows;
+      w = std::max(w, tree_ws_bytes(tree_plan(c, batch, &d, cus), c.head_dim));
+    };
+    // A query tile's width times the grid may be more for a narrower tree, of which more workgroups share a compute unit; of
+    // the trees of one width the longest needs most.
+    for (int qt = 16; qt <= 256; qt *= 2)
+      if (qt / (c.n_q / c.n_kv) >= 1) take(std::min(draft->max_rows, qt / (c.n_q / c.n_kv)));
+    take(draft->max_rows);
+  }
+  return w;
+}
+
 ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch,
                              const ods_draft *draft) {
   if (!batch || !draft) return set_error(ODS_EINVAL, "null batch or draft");

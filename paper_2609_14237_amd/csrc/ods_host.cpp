@@ -422,6 +422,32 @@ size_t range_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_
   return w;
 }
 
+size_t rows_ws_most(const ods_block *blk, int rows) {
+  // Split-K counts change only past these row counts and past multiples of 64, and between two changes partials grow with the
+  // rows: the last count before each change is enough. From 49152 rows on (192 tiles of 256) nothing is split.
+  const int steps[] = {8, 16, 24, 32, 64, 80};
+  size_t w = 0;
+  auto at = [&](const ods_layer &L, int n) {
+    ods_batch b{};
+    b.batch = n;
+    w = std::max(w, layer_ws_bytes(L, &b, 1, false));
+  };
+  for (int l = 0; l < blk->n_layers; ++l) {
+    const ods_layer &L = blk->layers[l];
+    auto same = [&](const ods_layer &o) {
+      const ods_layer_cfg &a = o.cfg, &c = L.cfg;
+      return o.weight_layout == L.weight_layout && a.hidden == c.hidden && a.n_q == c.n_q && a.n_kv == c.n_kv &&
+             a.head_dim == c.head_dim && a.ffn == c.ffn && a.n_experts == c.n_experts;
+    };
+    if (l > 0 && same(blk->layers[l - 1])) continue;
+    for (const int n : steps)
+      if (n < rows) at(L, n);
+    for (int n = 128; n < std::min(rows, 49152); n += 64) at(L, n);
+    at(L, rows);
+  }
+  return w;
+}
+
 size_t block_ws_bytes(const ods_block *blk, const ods_batch *batch, int cus) {
   size_t w = 256;
   for (int l = 0; l < blk->n_layers; ++l) w = std::max(w, layer_ws_bytes(blk->layers[l], batch, cus));

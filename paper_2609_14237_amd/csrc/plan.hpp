@@ -141,6 +141,8 @@ KvMap kv_map(const ods_layer_cfg &c, const ods_batch *b);
 size_t range_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, int cus,
                       bool with_attn = true);
 size_t block_ws_bytes(const ods_block *blk, const ods_batch *batch, int cus);
+// The most that the block's operators other than attention need for any batch of up to `rows`.
+size_t rows_ws_most(const ods_block *blk, int rows);
 
 // Every check ods_run_partition makes before it enqueues anything: block,
 // range, batch fields, every pointer each operator of the range touches
@@ -229,8 +231,10 @@ struct DraftStep {
 DraftStep draft_step(const ods_block *blk, int begin, int op_end);
 // The batch the row-wise operators see: draft->rows rows.
 ods_batch row_batch(const ods_batch *batch, const ods_draft *draft);
+// Workspace of one drafted range, and the most that any range needs for these or fewer sequences, rows and rows of a sequence.
 size_t draft_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, const ods_draft *draft,
                       int cus);
+size_t draft_ws_most(const ods_block *blk, const ods_batch *batch, const ods_draft *draft, int cus);
 // Counts and shapes of a drafted range, no pointers.
 ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch,
                              const ods_draft *draft);

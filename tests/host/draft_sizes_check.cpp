@@ -99,8 +99,57 @@ static void check_short_workspaces() {
     }
 }
 
+// A workspace of ods_draft_workspace_bytes serves every draft over no more sequences, rows and rows of a sequence: a server
+// sizes its state once, for its widest tree. (By the widest tree alone: 32 sequences in tables of 256 pages, 64-wide heads,
+// 8480 KB at 8 rows a sequence and 4232 at 9.)
+static void check_narrower_drafts() {
+  struct Shape { ods_layer_cfg c; bool tiled; };
+  const std::vector<Shape> shapes = {
+      {{256, 4, 2, 64, 512, 0, 0, 0, 0, 1e4f, 1e-6f}, false},      {{256, 4, 2, 64, 512, 0, 0, 0, 100, 1e4f, 1e-6f}, false},
+      {{4096, 32, 8, 128, 14336, 0, 0, 0, 0, 1e4f, 1e-6f}, true},  {{2048, 16, 1, 128, 5504, 0, 0, 0, 1024, 1e4f, 1e-6f}, false},
+      {{5120, 40, 40, 128, 13824, 0, 0, 0, 0, 1e4f, 1e-6f}, true}, {{1024, 16, 8, 64, 0, 128, 8, 768, 0, 1e4f, 1e-6f}, false},
+      {{8192, 8, 1, 128, 3584, 0, 0, 0, 0, 1e4f, 1e-6f}, true},    {{520, 6, 2, 64, 1000, 0, 0, 0, 40, 1e4f, 1e-6f}, false}};
+  auto check = [](const ods_block &blk, int B, int pages, int max_rows, int rows, int cus, bool every_row) {
+    const ods_batch b = batch_of(B, pages);
+    const ods_draft d = draft_of(rows, max_rows);
+    const size_t most = draft_ws_most(&blk, &b, &d, cus);
+    ods_state st = state(most);
+    const int n = num_ops(&blk);
+    CHECK(most >= draft_ws_bytes(&blk, 0, n, &b, &d, cus));
+    for (int B2 : {1, B / 2, B})
+      for (int m2 = 1; m2 <= max_rows; ++m2) {
+        if (B2 < 1) continue;
+        const ods_batch b2 = batch_of(B2, m2 % 2 ? pages : (pages + 1) / 2);
+        const ods_draft d2 = draft_of(std::max(1, (int)((int64_t)rows * m2 / max_rows)), m2);
+        CHECK(draft_ws_bytes(&blk, 0, n, &b2, &d2, cus) <= most);
+        if (m2 % 37 == 1) CHECK(validate_draft(&blk, 0, n, &b2, &d2, &st, cus) == ODS_OK);
+      }
+    for (int r = 1; r <= rows; r += every_row ? 1 : 97) {
+      const ods_draft d2 = draft_of(r, max_rows);
+      CHECK(draft_ws_bytes(&blk, 0, n, &b, &d2, cus) <= most);
+    }
+    CHECK(most == draft_ws_most(&blk, &b, &d, cus));
+  };
+  for (const Shape &s : shapes) {
+    const ods_layer L = layer(s.c, s.tiled);
+    const ods_block blk{1, &L};
+    for (int cus : {1, 256})
+      for (int pages : {1, 40, 256})
+        for (int max_rows : {1, 4, 9, 17, 64, 200, 256})
+          for (int B : {1, 32, 64, 600}) check(blk, B, pages, max_rows, std::min(B * max_rows, 3000), cus, false);
+    check(blk, 64, 40, 20, 1300, 256, true);
+    check(blk, 2, 8, 256, 512, 256, true);
+    check(blk, 600, 2, 256, 60000, 256, false);
+  }
+  std::vector<ods_layer> ls;  // layers of different shapes, the widest need not the last one's
+  for (int i : {2, 0, 5, 1}) ls.push_back(layer(shapes[i].c, shapes[i].tiled));
+  const ods_block blk{(int)ls.size(), ls.data()};
+  check(blk, 32, 256, 16, 512, 256, true);
+}
+
 int main() {
   check_cost_of_a_deep_block();
+  check_narrower_drafts();
   check_short_workspaces();
   printf("draft_sizes_check OK\n");
   return 0;

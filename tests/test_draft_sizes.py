@@ -6,6 +6,11 @@ import subprocess
 
 import pytest
 
+import workloads as W
+
+B = pytest.importorskip("paper_2609_14237_amd.binding")
+from test_draft_host import fake_batch, fake_block, fake_draft  # noqa: E402
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CXX = os.environ.get("CXX", "g++")
 
@@ -23,3 +28,15 @@ def test_sizes_of_drafted_ranges(tmp_path):
     r = subprocess.run([str(exe)], capture_output=True, text=True, env=env, timeout=600)
     assert r.returncode == 0, (r.stdout + r.stderr)[-4000:]
     assert "draft_sizes_check OK" in r.stdout
+
+
+@pytest.mark.parametrize("cfg,batch,pages", [
+    (W.LayerCfg(hidden=256, n_q=4, n_kv=2, head_dim=64, ffn=512), 32, 256),
+    (W.LayerCfg(hidden=256, n_q=4, n_kv=2, head_dim=64, ffn=512), 64, 40),
+    (W.BY_NAME["dense8b_b64"].layers[0], 32, 256)])
+def test_a_workspace_of_wide_trees_serves_narrow_ones(cfg, batch, pages):
+    """ods_draft_workspace_bytes never shrinks with the rows of a sequence."""
+    blk = fake_block([cfg])
+    sizes = [B.ods_draft_workspace_bytes(blk.c, fake_batch(batch=batch, max_pages=pages), fake_draft(rows=batch * m, max_rows=m))
+             for m in range(1, 257)]
+    assert sizes[0] > 0 and sizes == sorted(sizes)
