@@ -198,20 +198,23 @@ class DeviceDraft:
         """The host-visible sizes fit the block and the batch."""
         if self.row_off.shape != (batch.batch + 1,):
             raise ValueError(f"DeviceDraft: row_off {tuple(self.row_off.shape)} for a batch of {batch.batch}")
+        if batch.ctx_lens.numel() < batch.batch:
+            raise ValueError(f"DeviceDraft: ctx_lens {tuple(batch.ctx_lens.shape)} for a batch of {batch.batch}")
         if self.rope is not None and len(self.rope) != len(block.cfgs):
             raise ValueError(f"DeviceDraft: {len(self.rope)} ropes for {len(block.cfgs)} layers")
 
 
 class DeviceState:
     """Live buffers sized by ods_live_bytes and a workspace of ods_workspace_bytes; with `draft`, for its rows
-    (ods_draft_workspace_bytes)."""
+    (ods_draft_workspace_bytes). `rows`: what the buffers hold; a call on more is refused, since the library sees
+    addresses only."""
 
     def __init__(self, block: DeviceBlock, batch: DeviceBatch, device="cuda", fill=None,
                  draft: DeviceDraft | None = None):
         self.buffers = {}
-        rows = batch.batch if draft is None else draft.rows
+        self.rows = batch.batch if draft is None else draft.rows
         for i, name in enumerate(_b.BUFFERS):
-            nbytes = _b.ods_live_bytes(block.c, rows, i)
+            nbytes = _b.ods_live_bytes(block.c, self.rows, i)
             if nbytes == 0:
                 continue
             dt = _BUF_DTYPE.get(name, torch.bfloat16)
@@ -236,6 +239,11 @@ class DeviceState:
             n *= s
         return t[:n].view(*shape)
 
+    def check(self, who: str, rows: int) -> None:
+        """The live buffers hold `rows` rows."""
+        if rows > self.rows:
+            raise ValueError(f"{who}: {rows} rows, the state's buffers hold {self.rows}")
+
 
 def current_stream() -> int:
     # the handle alone: torch.cuda.current_stream() makes a Stream object first, 2.9 us
@@ -244,6 +252,7 @@ def current_stream() -> int:
 
 def run_partition(block: DeviceBlock, op_begin: int, op_end: int, batch: DeviceBatch, state: DeviceState,
                   stream: int | None = None) -> None:
+    state.check("run_partition", batch.batch)
     st = _b.ods_run_partition(block.c, op_begin, op_end, batch.c, state.c,
                               current_stream() if stream is None else stream)
     _b._check(st, f"ods_run_partition[{op_begin},{op_end})")
@@ -252,17 +261,20 @@ def run_partition(block: DeviceBlock, op_begin: int, op_end: int, batch: DeviceB
 def run_partition_scratch(block: DeviceBlock, op_begin: int, op_end: int, batch: DeviceBatch, state: DeviceState,
                           stream: int | None = None) -> None:
     """ods_run_partition_scratch: the same range on the library's own workspace (state.ws is not used)."""
+    state.check("run_partition_scratch", batch.batch)
     st = _b.ods_run_partition_scratch(block.c, op_begin, op_end, batch.c, state.c,
                                       current_stream() if stream is None else stream)
     _b._check(st, f"ods_run_partition_scratch[{op_begin},{op_end})")
 
 
 def attn_stage(block, layer, batch, state, stream=None) -> None:
+    state.check("attn_stage", batch.batch)
     st = _b.ods_attn_stage(block.c, layer, batch.c, state.c, current_stream() if stream is None else stream)
     _b._check(st, f"ods_attn_stage({layer})")
 
 
 def ffn_stage(block, layer, batch, state, stream=None) -> None:
+    state.check("ffn_stage", batch.batch)
     st = _b.ods_ffn_stage(block.c, layer, batch.c, state.c, current_stream() if stream is None else stream)
     _b._check(st, f"ods_ffn_stage({layer})")
 
@@ -274,6 +286,8 @@ class PartitionGraph:
     block, batch and state objects (and their buffers) alive while the graph is."""
 
     def __init__(self, block: DeviceBlock, op_begin: int, op_end: int, batch: DeviceBatch, state: DeviceState):
+        self.handle = None
+        state.check("PartitionGraph", batch.batch)
         st, h = _b.ods_partition_graph(block.c, op_begin, op_end, batch.c, state.c)
         _b._check(st, f"ods_partition_graph[{op_begin},{op_end})")
         self.handle = h
@@ -301,6 +315,7 @@ def run_draft(block: DeviceBlock, op_begin: int, op_end: int, batch: DeviceBatch
     """Operators [op_begin, op_end) for the drafted rows of a batch (ods_run_draft): ctx_lens counts the cached
     tokens, the drafted ones not among them."""
     draft.check(block, batch)
+    state.check("run_draft", draft.rows)
     st = _b.ods_run_draft(block.c, op_begin, op_end, batch.c, draft.c, state.c,
                           _stream_of("run_draft", stream, draft.row_off, batch.ctx_lens))
     _b._check(st, f"ods_run_draft[{op_begin},{op_end})")
@@ -311,9 +326,10 @@ class DraftGraph(PartitionGraph):
 
     def __init__(self, block: DeviceBlock, op_begin: int, op_end: int, batch: DeviceBatch, draft: DeviceDraft,
                  state: DeviceState):
-        draft.check(block, batch)
-        st, h = _b.ods_draft_graph(block.c, op_begin, op_end, batch.c, draft.c, state.c)
         self.handle = None
+        draft.check(block, batch)
+        state.check("DraftGraph", draft.rows)
+        st, h = _b.ods_draft_graph(block.c, op_begin, op_end, batch.c, draft.c, state.c)
         _b._check(st, f"ods_draft_graph[{op_begin},{op_end})")
         self.handle = h
         self._keep = (block, batch, draft, state)
