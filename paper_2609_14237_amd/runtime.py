@@ -24,6 +24,11 @@ def _ptr(t):
     return t.data_ptr()
 
 
+def _devices(*tensors) -> tuple:
+    """Indices of the devices that the tensors are on (-1: the host); None and what is no tensor has none."""
+    return tuple({t.get_device() for t in tensors if isinstance(t, torch.Tensor)})
+
+
 def _tile_shapes(cfg):
     """(out, in, gated, groups) of each projection weight, as ods_tile_weight takes them."""
     qkv = (cfg.n_q + 2 * cfg.n_kv) * cfg.head_dim
@@ -78,6 +83,27 @@ class DeviceBlock:
             L.pool_pages = pages[i] if pool is not None else 0
             L.weight_layout = _b.ODS_WEIGHTS_TILED if self.tiled else _b.ODS_WEIGHTS_ROWS
         self.c = ods_block(n, C.cast(self._layers, C.POINTER(ods_layer)))
+        self._pool_devices = [_devices(pool) for pool in self.pools]
+        self._op_devices = [_devices(pool, *w.values()) for w, pool in zip(self.weights, self.pools)]
+        self._devices = {d for on in self._op_devices for d in on}
+
+    def pool_devices(self, layer_begin: int, layer_end: int) -> set:
+        """Devices of the pools of layers [layer_begin, layer_end)."""
+        if len(self._devices) <= 1:  # the whole block's
+            return self._devices
+        return {d for on in self._pool_devices[max(layer_begin, 0):max(layer_end, 0)] for d in on}
+
+    def op_devices(self, op_begin: int, op_end: int) -> set:
+        """Devices of the layers that operators [op_begin, op_end) belong to."""
+        if len(self._devices) <= 1:
+            return self._devices
+        on, at = set(), 0
+        for cfg, devices in zip(self.cfgs, self._op_devices):
+            end = at + (14 if cfg.n_experts else 10)
+            if op_begin < end and at < op_end:
+                on.update(devices)
+            at = end
+        return on
 
     def num_ops(self) -> int:
         return _b.ods_block_num_ops(self.c)
@@ -106,6 +132,7 @@ class DeviceBatch:
             ring_pages = self.ring_table.shape[1]
         self.c = ods_batch(B, max_pages, _ptr(self.ctx_lens), _ptr(self.page_table), split_pages, ring_pages,
                            _ptr(self.ring_table))
+        self.devices = _devices(self.ctx_lens, self.page_table, self.ring_table)
 
     @property
     def batch(self) -> int:
@@ -116,15 +143,23 @@ _BUF_DTYPE = {"logits": torch.float32, "topk_w": torch.float32, "topk_ids": torc
               "perm": torch.int32, "slot_pos": torch.int32, "expert_off": torch.int32}
 
 
-def _stream_of(who: str, stream: int | None, *tensors: torch.Tensor | None) -> int:
-    """`stream`, or the current one, which has to be of the device the tensors are on."""
-    if stream is not None:
-        return stream
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"{who}: a tensor is on {t.device}, the current device is cuda:{device}")
-    return torch._C._cuda_getCurrentRawStream(device)
+def _stream_of(who: str, stream: int | None, *devices: int) -> int:
+    """`stream`, or the current one. What the call names is on one device: the current one, or, with a stream that the
+    caller names, the device of that stream, which is not looked at."""
+    if stream is None:
+        device = torch.cuda.current_device()
+        for d in devices:
+            if d != device:
+                raise ValueError(f"{who}: a tensor is on {_name(d)}, the current device is cuda:{device}")
+        return torch._C._cuda_getCurrentRawStream(device)
+    for d in devices:
+        if d != devices[0]:
+            raise ValueError(f"{who}: tensors are on {_name(devices[0])} and on {_name(d)}, a call takes one device")
+    return stream
+
+
+def _name(device: int) -> str:
+    return "the host" if device < 0 else f"cuda:{device}"
 
 
 class Rope:
@@ -166,7 +201,8 @@ def rope(r: Rope, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor | None =
     width = heads * r.c.head_dim  # the stride of a single row means nothing
     xs, ys = (t.stride(0) if rows > 1 else width for t in (x, y))
     _b._check(_b.ods_rope_rows(r.c, x.data_ptr(), xs, y.data_ptr(), ys, rows, heads, pos.data_ptr(),
-                               _stream_of("rope", stream, x, y, pos, r.freqs)), "ods_rope_rows")
+                               _stream_of("rope", stream, x.get_device(), y.get_device(), pos.get_device(),
+                                          r.freqs.get_device())), "ods_rope_rows")
     return y
 
 
@@ -189,6 +225,7 @@ class DeviceDraft:
         self._table = table
         self.c = ods_draft(depth.shape[0], max_rows, _ptr(self.row_off), _ptr(self.depth), _ptr(self.mask),
                            None if table is None else C.cast(table, C.POINTER(ods_rope)))
+        self.devices = _devices(self.row_off, self.depth, self.mask, *(r.freqs for r in self.rope or ()))
 
     @property
     def rows(self) -> int:
@@ -226,6 +263,7 @@ class DeviceState:
         self.ws_bytes = (_b.ods_workspace_bytes(block.c, batch.c) if draft is None
                          else _b.ods_draft_workspace_bytes(block.c, batch.c, draft.c))
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+        self.devices = _devices(self.ws)
         self.c = ods_state()
         for name, t in self.buffers.items():
             setattr(self.c, name, t.data_ptr())
@@ -317,7 +355,8 @@ def run_draft(block: DeviceBlock, op_begin: int, op_end: int, batch: DeviceBatch
     draft.check(block, batch)
     state.check("run_draft", draft.rows)
     st = _b.ods_run_draft(block.c, op_begin, op_end, batch.c, draft.c, state.c,
-                          _stream_of("run_draft", stream, draft.row_off, batch.ctx_lens))
+                          _stream_of("run_draft", stream, *block.op_devices(op_begin, op_end), *batch.devices, *draft.devices,
+                                     *state.devices))
     _b._check(st, f"ods_run_draft[{op_begin},{op_end})")
 
 
@@ -329,6 +368,7 @@ class DraftGraph(PartitionGraph):
         self.handle = None
         draft.check(block, batch)
         state.check("DraftGraph", draft.rows)
+        _stream_of("DraftGraph", None, *block.op_devices(op_begin, op_end), *batch.devices, *draft.devices, *state.devices)
         st, h = _b.ods_draft_graph(block.c, op_begin, op_end, batch.c, draft.c, state.c)
         _b._check(st, f"ods_draft_graph[{op_begin},{op_end})")
         self.handle = h
@@ -351,7 +391,8 @@ def kv_accept(block: DeviceBlock, batch: DeviceBatch, draft: DeviceDraft, path: 
             raise ValueError(f"kv_accept: {name} must be contiguous int32 {shape}, got {t.dtype} {tuple(t.shape)}")
     a, b = _layers(block, layers)
     st = _b.ods_kv_accept(block.c, a, b, batch.c, draft.c, path.data_ptr(), path.shape[1], path_len.data_ptr(),
-                          _ptr(ctx_out), _stream_of("kv_accept", stream, batch.ctx_lens, path, path_len, ctx_out))
+                          _ptr(ctx_out), _stream_of("kv_accept", stream, *block.pool_devices(a, b), *batch.devices, *draft.devices,
+                                                    *_devices(path, path_len, ctx_out)))
     _b._check(st, "ods_kv_accept")
 
 
@@ -361,7 +402,8 @@ def kv_copy_pages(block: DeviceBlock, pairs: torch.Tensor, layers=None, stream: 
     if pairs.dtype != torch.int32 or pairs.dim() != 2 or pairs.shape[1] != 2 or not pairs.is_contiguous():
         raise ValueError(f"kv_copy_pages: pairs must be contiguous int32 [n, 2], got {pairs.dtype} {tuple(pairs.shape)}")
     a, b = _layers(block, layers)
-    st = _b.ods_kv_copy_pages(block.c, a, b, pairs.data_ptr(), pairs.shape[0], _stream_of("kv_copy_pages", stream, pairs))
+    st = _b.ods_kv_copy_pages(block.c, a, b, pairs.data_ptr(), pairs.shape[0],
+                              _stream_of("kv_copy_pages", stream, *block.pool_devices(a, b), pairs.get_device()))
     _b._check(st, "ods_kv_copy_pages")
 
 
