@@ -146,8 +146,12 @@ hipError_t launch_copy_pages(const PoolSet &pools, int n_pools, const int32_t *p
   int64_t most = 0;  // 16-byte pieces of a page
   for (int i = 0; i < n_pools; ++i) most = std::max(most, pools.p[i].page_elems / 8);
   const int parts = (int)((most + 256 * kCopyLoads - 1) / (256 * kCopyLoads));
-  hipLaunchKernelGGL(copy_pages_kernel, dim3(n, parts, n_pools), dim3(256), 0, s, pools, (const int2 *)pairs);
-  return hipGetLastError();
+  for (int64_t at = 0; at < n; at += kMaxGridX) {
+    hipLaunchKernelGGL(copy_pages_kernel, dim3((int)std::min<int64_t>(n - at, kMaxGridX), parts, n_pools), dim3(256), 0, s, pools,
+                       (const int2 *)pairs + at);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_accept(const AcceptArgs &a, const PoolSet &pools, int n_pools, int max_kv, int32_t *ctx_out, hipStream_t s) {

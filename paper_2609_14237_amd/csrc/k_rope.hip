@@ -1,6 +1,8 @@
 // Rotary positions of arbitrary rows (ods_rope_rows): y = x turned to each
 // row's position, half or interleaved pairs, part of the head, frequencies
 // from a table of doubles.
+#include <algorithm>
+
 #include "kernels.hpp"
 #include "turn.hpp"
 
@@ -39,9 +41,13 @@ hipError_t launch_rope_rows(const ods_rope &r, const uint16_t *x, int64_t xs, ui
   const bool wide = turns_wide(r.rotary_dim, r.interleaved);
   const auto kern = r.interleaved ? (wide ? rope_rows_kernel<true, true> : rope_rows_kernel<false, true>)
                                   : (wide ? rope_rows_kernel<true, false> : rope_rows_kernel<false, false>);
-  hipLaunchKernelGGL(kern, dim3(rows), dim3(256), 0, s, x, xs, y, ys, heads, r.head_dim, r.rotary_dim, r.freqs, r.amplitude,
-                     pos);
-  return hipGetLastError();
+  for (int64_t at = 0; at < rows; at += kMaxGridX) {
+    const int n = (int)std::min<int64_t>(rows - at, kMaxGridX);
+    hipLaunchKernelGGL(kern, dim3(n), dim3(256), 0, s, x + at * xs, xs, y + at * ys, ys, heads, r.head_dim, r.rotary_dim, r.freqs,
+                       r.amplitude, pos + at);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace ods

@@ -67,6 +67,10 @@ hipError_t launch_gather_rows(const uint16_t *src, const int32_t *perm, const in
 hipError_t launch_moe_combine(const uint16_t *yp, const float *w, const int32_t *slot_pos, int B,
                               int k, int H, uint16_t *resid, hipStream_t s);
 
+// Workgroups of 256 threads along x of a launch: a dimension takes fewer than 2^32 threads, and what is above comes back as
+// a success of a few of them (2^24 + 5 rows: five turned). Longer calls take several launches.
+constexpr int kMaxGridX = 1 << 23;
+
 // y = the rows' heads turned to their positions (arguments checked by check_rope_rows).
 hipError_t launch_rope_rows(const ods_rope &r, const uint16_t *x, int64_t xs, uint16_t *y, int64_t ys, int rows,
                             int heads, const int32_t *pos, hipStream_t s);
