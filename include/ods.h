@@ -389,7 +389,8 @@ ods_status ods_rope_rows(const ods_rope *rope, const void *x, int64_t x_stride, 
  * A chain of one token with its bit set is the decode step of context ctx + 1.
  *
  *   rows      rows of the live buffers (what ods_live_bytes and the GEMMs take
- *             as the batch); rows from row_off[batch] on are padding, which
+ *             as the batch), 4096 * ODS_DRAFT_MAX_ROWS at most (past that
+ *             ODS_EUNSUPPORTED); rows from row_off[batch] on are padding, which
  *             rope, kv_append and attn_core leave as they were
  *   max_rows  most rows of one sequence, 1 .. ODS_DRAFT_MAX_ROWS; a sequence's
  *             rows past it are treated as padding

@@ -29,6 +29,9 @@ ods_status check_counts(const ods_batch *batch, const ods_draft *draft) {
     return set_error(ODS_EINVAL, "draft max_rows %d (need 1 .. %d)", draft->max_rows, ODS_DRAFT_MAX_ROWS);
   if (batch->batch > kMaxAttnBatch)
     return set_error(ODS_EUNSUPPORTED, "drafted rows support batch <= %d, got %d", kMaxAttnBatch, batch->batch);
+  // all that the sequences can have; the row-wise operators' launches hold fewer than 2^24 workgroups
+  if (draft->rows > kMaxAttnBatch * ODS_DRAFT_MAX_ROWS)
+    return set_error(ODS_EUNSUPPORTED, "draft rows %d (at most %d)", draft->rows, kMaxAttnBatch * ODS_DRAFT_MAX_ROWS);
   return ODS_OK;
 }
 

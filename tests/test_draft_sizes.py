@@ -9,7 +9,7 @@ import pytest
 import workloads as W
 
 B = pytest.importorskip("paper_2609_14237_amd.binding")
-from test_draft_host import fake_batch, fake_block, fake_draft  # noqa: E402
+from test_draft_host import fake_batch, fake_block, fake_draft, fake_state  # noqa: E402
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CXX = os.environ.get("CXX", "g++")
@@ -40,3 +40,16 @@ def test_a_workspace_of_wide_trees_serves_narrow_ones(cfg, batch, pages):
     sizes = [B.ods_draft_workspace_bytes(blk.c, fake_batch(batch=batch, max_pages=pages), fake_draft(rows=batch * m, max_rows=m))
              for m in range(1, 257)]
     assert sizes[0] > 0 and sizes == sorted(sizes)
+
+
+def test_rows_that_can_only_be_padding_are_refused():
+    """4096 sequences of 256 rows are 2^20; the row-wise operators' launches end at 2^24 workgroups."""
+    blk, most = fake_block([W.LayerCfg(hidden=64, n_q=1, n_kv=1, head_dim=64, ffn=64)]), 1 << 20
+    for rows in (most + 1, 1 << 24, 1 << 30):
+        for ops in ((0, 1), (2, 5), (5, 10)):
+            assert B.ods_run_draft(blk.c, *ops, fake_batch(), fake_draft(rows=rows, row_off=None), fake_state(resid=None, qkv=None),
+                                   None) == B.ODS_EUNSUPPORTED
+        assert B.ods_draft_workspace_bytes(blk.c, fake_batch(), fake_draft(rows=rows)) == 0
+        assert B.ods_kv_accept(blk.c, 0, 1, fake_batch(), fake_draft(rows=rows), None, 4, None, None, None) == B.ODS_EUNSUPPORTED
+    assert B.ods_run_draft(blk.c, 5, 10, fake_batch(), fake_draft(rows=most), fake_state(resid=None), None) == B.ODS_EINVAL
+    assert B.ods_draft_workspace_bytes(blk.c, fake_batch(), fake_draft(rows=most)) > 0
