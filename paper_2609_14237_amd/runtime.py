@@ -443,6 +443,8 @@ class KvPages:
 
     def resize(self, row: int, tokens: int) -> None:
         """Sequence `row` grows or shrinks to `tokens` tokens."""
+        if not 0 <= tokens < 1 << 31:  # the library would see its low 32 bits
+            raise ValueError(f"KvPages.resize: {tokens} tokens")
         pair = np.zeros(2, np.int32)
         st, n = _b.ods_pages_resize(self.c, self.table[row], int(self.tokens[row]), tokens, pair)
         _b._check(st, "ods_pages_resize")
