@@ -156,3 +156,33 @@ def test_tensors_that_are_not_on_the_device():
     with pytest.raises(ValueError, match="the host"):
         R.kv_accept(c.block, batch, c.draft, path, n)
     c.check(c.attend())
+
+
+@pytest.mark.parametrize("fill", [float("nan"), float("inf"), 1e30])
+def test_padding_rows_do_not_reach_others(fill):
+    """A padded batch through dense, windowed and MoE layers: whatever the rows behind the last sequence hold, the others'
+    results and the cache are the same, bit for bit."""
+    say("padding", fill)
+    from dataclasses import replace
+    import workloads as W
+    from workloads import gen
+    cfg = W.LayerCfg(hidden=256, n_q=4, n_kv=2, head_dim=64, ffn=512)
+    cfgs = [cfg, replace(cfg, window=40, ffn=0, n_experts=8, top_k=2, moe_ffn=128),
+            replace(cfg, ffn=0, n_experts=80, top_k=6, moe_ffn=64)]
+    weights = [{k: v.cuda() for k, v in gen.layer_weights(x, 1, l, "cpu", 1 / 16).items()} for l, x in enumerate(cfgs)]
+    c = Case([5, 60, 0, 200], [9, 16, 4, 1], 4, 2, 64, seed=1, pad=11).device()
+    real = c.R - 11
+    x = gen.activations(c.R, 256, 1, "cpu").cuda()
+    outs = []
+    for value in (0.0, fill):
+        pools = [c.pool.cuda() for _ in cfgs]
+        block = R.DeviceBlock(cfgs, weights, pools, c.P)
+        state = R.DeviceState(block, c.batch, fill=value, draft=c.draft)
+        state.view("resid", c.R, 256).copy_(x)[real:] = value
+        R.run_draft(block, 0, block.num_ops(), c.batch, c.draft, state)
+        torch.cuda.synchronize()
+        outs.append((state.view("resid", c.R, 256)[:real].clone(), pools))
+    assert torch.isfinite(outs[0][0]).all()
+    assert torch.equal(outs[0][0], outs[1][0])
+    for p, q in zip(outs[0][1], outs[1][1]):
+        assert torch.equal(p.view(torch.int16), q.view(torch.int16))
