@@ -400,7 +400,9 @@ ods_status ods_rope_rows(const ods_rope *rope, const void *x, int64_t x_stride, 
  *   rope      NULL: the layers' own rope_theta; or n_layers entries (host),
  *             each with the layer's head_dim
  * Slots past the page table (max_pages * 16 tokens) are neither written nor
- * attended. A window-only ring must also hold the drafted tokens:
+ * attended. Attention's launch is planned for the table's width, as if contexts
+ * filled it: a table no wider than the batch needs is a few us faster on short
+ * contexts. A window-only ring must also hold the drafted tokens:
  * ring_pages >= ceil((window + max_rows) / 16) + 1 (ODS_EINVAL otherwise).
  * batch <= 4096 as for attn_core; rows * n_q < 2^31, and batch * n_kv * query
  * tiles * window pages < 2^30 (ODS_EUNSUPPORTED otherwise). split_pages is not

@@ -69,7 +69,9 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
 // every K/V byte read. Bound by memory up to about 128 columns (64 sequences of
 // 9216 tokens, 4 rows of 32 heads on 8: 362 us, 6.9 TB/s; 16 rows 366), by the
 // matrix and vector units past that (64 sequences of 8192, 64 rows: 620 us, 0.89
-// PFLOP/s), by latency where there is little to read (one sequence of 3000, 16
+// PFLOP/s, the matrix cores busy for 45% of the cycles and the vector unit for 41%;
+// more rows take as many passes over K and V of that kind: 256 rows 2640 us), by
+// latency where there is little to read (one sequence of 3000, 16
 // rows: 17 us).
 //
 // Work split: a task is a (sequence, KV head, query tile), its units are tiles of
@@ -103,8 +105,13 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
 //                  8 r .. 8 r + 7, which is how S leaves P in registers, and one
 //                  16-byte read of a dim's slots in the dim-major V, so P never
 //                  moves.
-// P is rounded to bf16 for the product (the values it multiplies are bf16); its
-// sum, the maximum and the outputs are fp32.
+// P is rounded to bf16 for the product: the matrix cores multiply equal types, and
+// the values are bf16. A probability is off by 2^-8 of itself at most, an output by
+// 2^-8 of sum p |v| / sum p: no more than its own rounding to bf16 where the values
+// have one sign (over normal values the outputs are 0.0023 off the 64-bit ones in
+// the mean square, 0.0017 with fp32 probabilities). P in two bf16 halves would
+// double the products of V. Its sum, the maximum and the outputs before their
+// store are fp32.
 //
 // Tiles with a drafted token, a window edge, the end of the sequence or a page
 // outside the pool are masked score by score. In these a value that is not
@@ -679,8 +686,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   // A tile takes two phases: products (the last tile's values, then this one's scores; each operand is replaced from LDS
   // after its last use) and softmax, which also fetches a tile.
   //  - Softmax of tile t fetches into the slot of tile t - 1, whose last reads were made in products t - 1.
-  //  - Two or four waves meet once a tile, after its softmax; another workgroup of the compute unit fills the gaps. Products
-  //    of tile t read its keys first, so one tile fewer has to have landed (24 rows x 64 sequences: 123 us with the keys
+  //  - Two or four waves meet once a tile, after its softmax; where a compute unit runs two workgroups, the other fills the
+  //    gaps. Products of tile t read its keys first, so one tile fewer has to have landed (24 rows x 64 sequences: 123 us with the keys
   //    read a tile ahead, 112).
   //  - Eight waves have a compute unit to themselves. Their products read the next tile's keys, so that the reads run under
   //    the products: everyone's loads of t + 1 have landed before products t. The two waves of a SIMD run half a tile apart

@@ -133,21 +133,29 @@ TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_dra
   p.qt = 16;
   while (p.qt < nq && p.qt < 256) p.qt *= 2;
   p.max_qt = (int)((nq + p.qt - 1) / p.qt);
-  // tokens of a sequence a layer may read: the table's, or a window with the drafted rows
+  // Tokens of a sequence a layer may read: the table's, or a window with the drafted rows. The host sees no contexts, so a
+  // table wider than they need is planned for as if they filled it: right, but of the rules below no_cut needs a table of 864
+  // tokens at most (4 sequences of 128 tokens: 7.9 us up to 54 pages, 9.9 at 64, 10.7 at 2048), and a wide one reads past the
+  // caches what they would hold (64 sequences of 300 tokens, 4 rows: 18.9 us in 19 pages, 21.0 in 2048).
   int64_t tokens = (int64_t)kv_map(c, batch).cols * ODS_PAGE_TOKENS;
   if (c.window > 0) tokens = std::min(tokens, (int64_t)c.window + draft->max_rows + 64);
   const int64_t units = (int64_t)batch->batch * c.n_kv * p.max_qt * ((tokens + 31) / 32 + 1);
   p.units_ok = units < (int64_t)1 << 30;
-  p.min_tiles = 4;  // one sequence of 3000 tokens, us at 2, 4 and 6: 16 rows 17.3, 16.8, 17.0, 32 rows 24.7, 23.8, 24.1
+  // One sequence of 3000 tokens, us at 2, 4 and 6: 16 rows 17.3, 16.8, 17.0, 32 rows 24.7, 23.8, 24.1. Nearly level: what a
+  // shorter range saves in tiles its record costs.
+  p.min_tiles = 4;
   cus = std::max(cus, 1);
-  // 128 columns: a window makes the tasks nearly equal, so that they need no cutting or dealing, and two workgroups of four
-  // waves fill each other's gaps (32 sequences, window 1024: 42 us, one of eight waves 44; 64 of 2304 tokens each 112, 139).
-  // Contexts that differ are better dealt out to workgroups of eight (64 of 512 to 4096: 129 us, 139).
+  // 128 columns as four waves of 32: half the LDS reads of eight waves of 16, which read every tile once each. It pays
+  // where the tasks are nearly equal and need no dealing (64 sequences of 2304 tokens, 24 rows: 112 us with two workgroups a
+  // compute unit, eight waves 139), and a window makes them so (32 sequences, 1024 tokens of each: 42 to 45 us, eight waves
+  // 44). Contexts that differ are better dealt out to workgroups of eight (64 of 512 to 4096: 129 us, 139). A compute unit
+  // runs one such workgroup, with half its LDS, until per_cu below is 2.
   p.equal = p.qt == 128 && c.window > 0;
   // Workgroups per compute unit. Up to 16 columns are one wave's work, and two have room (64 sequences of up to 4096
   // tokens, 4 rows, us at 1, 2 and 4: D = 128 124, 121, 126; D = 64 at 4 and 8 68). The workgroups of two or four waves
-  // fit twice, which pays once a range is long (64 sequences of 2304 tokens, 16 rows: 102 us, one each 119; 8 of 2000 to 8000,
-  // 12 rows: 44 and 42). Eight waves have all the LDS.
+  // fit twice, which pays once a range is long, 64 units with both (64 sequences of 2304 tokens, 16 rows: 102 us, one each 119;
+  // 8 of 2000 to 8000, 12 rows: 44 and 42; behind a window of 1024 with 8 heads from 114 sequences on: 128 of them 129 us, 64
+  // with one each 83). Eight waves have all the LDS.
   const bool small = p.qt <= 64 || p.equal;
   int per_cu = p.qt <= 16 ? 256 / c.head_dim : 1;
   if (p.qt > 16 && small && units >= (int64_t)2 * cus * 64) per_cu = 2;
@@ -156,12 +164,13 @@ TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_dra
   // sequences of 9216 tokens, 4 rows: 362 us, through them 402; 64 ragged ones 129, 138). What fits may still be there
   // (16 sequences of 1000 to 2000 tokens, read again: 32 us, 34 past the caches), and query tiles read the same tiles again.
   p.stream = p.max_qt == 1 && units * 32 * c.head_dim * 4 > (int64_t)256 << 20;
-  // Joining a task of many ranges (one sequence: 18 us, by whole waves 23), or of few (64 ragged sequences cut into even
-  // ranges: 157 us, by quarters of a column 173).
   // One task a range, none long enough to be cut, whatever the contexts (4 short sequences: 7 us, with the second launch
-  // 10).
+  // 10). Longer tasks may still all be whole (32 behind a window of 1024: 36 tiles at most), or dealt out: then the
+  // second launch finds nothing to join, 3 to 4 us.
   const int64_t tasks = (int64_t)batch->batch * c.n_kv * p.max_qt;
   p.no_cut = tasks <= p.grid && (tokens + 31) / 32 + 1 <= p.min_tiles + kSplitTiles;
+  // Joining a task of many ranges by quarters of a column (one sequence: 18 us, by whole waves 23), or of few by whole waves
+  // (64 ragged sequences cut into even ranges: 157 us, by quarters 173).
   p.split_join = p.grid > 6 * (int64_t)batch->batch * c.n_kv * p.max_qt;
   return p;
 }

@@ -202,16 +202,16 @@ ods_status check_rope(const ods_rope *r, const char *who, bool need_freqs);
 ods_status check_rope_rows(const ods_rope *r, const void *x, int64_t xs, const void *y, int64_t ys, int rows, int heads,
                            const int32_t *pos);
 
-// Attention over drafted rows: query tile width and launch shape.
 // Tiles a range may have above an even share, so that no task is cut.
 constexpr int kSplitTiles = 24;
 
+// Attention over drafted rows: query tile width and launch shape.
 struct TreePlan {
   int qt;         // query vectors of a KV head that share a stream of tiles: 16, 32, 64, 128 or 256
   int max_qt;     // query tiles of the longest tree
   int grid;       // workgroups, one range each
   int min_tiles;  // fewest 32-token tiles in a range
-  bool equal;     // 128 columns as four waves of 32, two workgroups per compute unit
+  bool equal;     // 128 columns as four waves of 32, not eight of 16
   bool stream;    // K and V are read past the caches
   bool no_cut;    // no task can lie in two ranges: nothing to join
   bool split_join;  // records of a column are shared by four waves
