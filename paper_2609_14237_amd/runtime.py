@@ -66,6 +66,8 @@ class DeviceBlock:
     references those copies; pretiled=True takes weights tile_weights() already
     converted."""
 
+    WEIGHTS = ("g_attn", "w_qkv", "w_o", "g_ffn", "w_gate_up", "w_down", "w_router")
+
     def __init__(self, cfgs, weights, pools, pool_pages, tiled: bool = False, pretiled: bool = False):
         self.cfgs = list(cfgs)
         self.tiled = tiled or pretiled
@@ -77,14 +79,14 @@ class DeviceBlock:
         for i, (cfg, w, pool) in enumerate(zip(self.cfgs, self.weights, self.pools)):
             L = self._layers[i]
             L.cfg = layer_cfg(cfg)
-            for name in ("g_attn", "w_qkv", "w_o", "g_ffn", "w_gate_up", "w_down", "w_router"):
+            for name in self.WEIGHTS:
                 setattr(L, name, _ptr(w.get(name)))
             L.kv_pool = _ptr(pool)
             L.pool_pages = pages[i] if pool is not None else 0
             L.weight_layout = _b.ODS_WEIGHTS_TILED if self.tiled else _b.ODS_WEIGHTS_ROWS
         self.c = ods_block(n, C.cast(self._layers, C.POINTER(ods_layer)))
         self._pool_devices = [_devices(pool) for pool in self.pools]
-        self._op_devices = [_devices(pool, *w.values()) for w, pool in zip(self.weights, self.pools)]
+        self._op_devices = [_devices(pool, *map(w.get, self.WEIGHTS)) for w, pool in zip(self.weights, self.pools)]
         self._devices = {d for on in self._op_devices for d in on}
 
     def pool_devices(self, layer_begin: int, layer_end: int) -> set:

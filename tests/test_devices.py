@@ -67,6 +67,9 @@ def test_drafted_rows_of_two_devices():
     r.freqs = far(r.freqs)
     with pytest.raises(ValueError, match="device"):
         run(draft=draft_of(rope=[r]))
+    t = z(64, dt=torch.bfloat16)  # what a weight dictionary holds beside the weights is not looked at
+    with pytest.raises(B.OdsError):
+        run(block=R.DeviceBlock([CFG], [{"w_o": None, "lm_head": far(t)}], [t], 0))
     block, batch, draft = block_of(), batch_of(), draft_of()
     state = R.DeviceState(block, batch, device="cpu", draft=draft)
     state.devices = (3,)  # as made with device="cuda:3"
