@@ -366,6 +366,30 @@ ods_status ods_rope_freqs(const ods_rope *rope, double *freqs_host);
 ods_status ods_rope_rows(const ods_rope *rope, const void *x, int64_t x_stride, void *y, int64_t y_stride,
                          int32_t rows, int32_t heads, const int32_t *pos, hipStream_t stream);
 
+/* Gains of heads that are normalised before they turn: x * (mean(x^2) +
+ * eps)^-1/2 * gain over the head's head_dim values, in fp32, the result not
+ * rounded before the rotation. gain_q, gain_k: device bf16 [head_dim], for the
+ * query and the key heads. */
+typedef struct {
+  const void *gain_q, *gain_k;
+  float eps;            /* >= 0 */
+} ods_head_norm;
+
+/* y = the heads of x normalised and rotated, in one pass: ods_rope_rows for rows
+ * of n_q query heads and n_k key heads behind them. norm NULL: a rotation alone;
+ * norm->gain_q (gain_k) may be NULL where n_q (n_k) is 0.
+ * Positions of several axes (time, height, width of images and video): pos is
+ * device int32 [rows][n_axes], 1 <= n_axes <= ODS_ROPE_AXES, and pair i of the
+ * rotated ones turns by pos[r][axis[i]] * freqs[i]; axis is a device table of
+ * rotary_dim / 2 int32 in 0 .. n_axes - 1 (values outside are clamped), NULL with
+ * n_axes == 1. A row with a negative position on any axis is left alone.
+ * Values past the rotated ones are normalised and pass through. Errors as
+ * ods_rope_rows, and ODS_EINVAL for a norm or axes outside the above. */
+#define ODS_ROPE_AXES 8
+ods_status ods_head_rows(const ods_rope *rope, const ods_head_norm *norm, const int32_t *axis, int32_t n_axes,
+                         const void *x, int64_t x_stride, void *y, int64_t y_stride, int32_t rows, int32_t n_q,
+                         int32_t n_k, const int32_t *pos, hipStream_t stream);
+
 /* ---- Drafted rows: several tokens of a sequence in one step -----------------
  *
  * A step over a tree of drafted tokens per sequence (speculative decoding), a
@@ -408,12 +432,37 @@ ods_status ods_rope_rows(const ods_rope *rope, const void *x, int64_t x_stride, 
  * tiles * window pages < 2^30 (ODS_EUNSUPPORTED otherwise). split_pages is not
  * used. */
 #define ODS_DRAFT_MAX_ROWS 256
+
+/* Sequences that share the pages of a prefix (forks of one prompt): group g is
+ * sequences group_off[g] .. group_off[g + 1] - 1 of the batch, whose page tables
+ * name the same pages for their first tokens[g] tokens. In full-attention layers
+ * attn_core then reads those pages once for all drafted rows of the group, by
+ * the first sequence's table, and each sequence's other tokens by its own. What
+ * it computes is the same attention. Sequences in no group, groups of one, and
+ * sequences of fewer cached tokens than their group shares are read by
+ * themselves; what is shared is rounded down to 32 tokens. Sliding-window
+ * layers read each sequence's own window.
+ *   n_groups   0 .. batch, at most ODS_SHARED_GROUPS
+ *   group_off  device [n_groups + 1], ascending, in 0 .. batch
+ *   tokens     device [n_groups] */
+#define ODS_SHARED_GROUPS 4095
+typedef struct {
+  int32_t n_groups;
+  const int32_t *group_off;
+  const int32_t *tokens;
+} ods_shared;
+
+/*   norm      NULL, or n_layers entries (host): the rope operator normalises the q
+ *             and k heads before it turns them (ods_head_norm)
+ *   shared    NULL, or the batch's shared prefixes */
 typedef struct {
   int32_t rows, max_rows;
   const int32_t *row_off;
   const int32_t *depth;
   const uint64_t *mask;
   const ods_rope *rope;
+  const ods_head_norm *norm;
+  const ods_shared *shared;
 } ods_draft;
 
 /* An ods_state.ws_bytes that is enough for any operator range of this block, for
@@ -430,8 +479,9 @@ ods_status ods_run_draft(const ods_block *blk, int32_t op_begin, int32_t op_end,
                          const ods_draft *draft, ods_state *state, hipStream_t stream);
 
 /* ods_partition_graph for drafted rows: the pointers of draft (the entries of
- * draft->rope included) and rows, max_rows are held as of this call; row_off,
- * depth, mask and freqs are read at each launch. */
+ * draft->rope, norm and shared included) and rows, max_rows, n_groups are held as
+ * of this call; row_off, depth, mask, freqs, gains, group_off and tokens are read
+ * at each launch. */
 ods_status ods_draft_graph(const ods_block *blk, int32_t op_begin, int32_t op_end, const ods_batch *batch,
                            const ods_draft *draft, ods_state *state, hipGraphExec_t *exec);
 
@@ -503,6 +553,82 @@ ods_status ods_kv_copy_pages(const ods_block *blk, int32_t layer_begin, int32_t 
 ods_status ods_kv_accept(const ods_block *blk, int32_t layer_begin, int32_t layer_end, const ods_batch *batch,
                          const ods_draft *draft, const int32_t *path, int32_t path_cols, const int32_t *path_len,
                          int32_t *ctx_out, hipStream_t stream);
+
+/* Groups of adjacent sequences that share leading pages, for ods_shared (host
+ * only): rows of table [rows][max_pages] whose first entries are the same. A row
+ * joins the group before it while that does not lower the pages the group saves
+ * ((its rows - 1) * its common pages); only whole pages of `tokens` (host [rows],
+ * each sequence's cached tokens) count. Writes group_off [rows + 1] and
+ * group_tokens [rows] (their first *n_groups + 1 and *n_groups entries): together
+ * the groups hold all rows, those that share nothing in groups of 0 tokens.
+ * ODS_EINVAL for null pointers, negative sizes or token counts past the table. */
+ods_status ods_pages_shared(const int32_t *table, int32_t rows, int32_t max_pages, const int32_t *tokens,
+                            int32_t *group_off, int32_t *group_tokens, int32_t *n_groups);
+
+/* ---- Verification of drafted tokens ------------------------------------------
+ *
+ * The accepted path of each sequence's tree and the token after it, so that what
+ * is kept is distributed as if it had been drawn from the target model alone
+ * (rejection sampling of drafts: Leviathan et al. 2023, arxiv 2211.17192; of
+ * several drafts after one token, each tested on what the ones before left:
+ * Miao et al. 2024, arxiv 2305.09781). Random numbers are inputs.
+ *
+ * Row 0 of a sequence is the token its last step ended with, which is always
+ * kept; row j > 0 holds tokens[j], a draft of what follows row parent[j] (an
+ * index below j inside the sequence). target row i holds the target's
+ * probabilities of the token after row i, proposal row i the draft's, from which
+ * the children of row i were drawn independently. From row i = 0 on:
+ *   W = target[i], Z = 1; for the children c of i in ascending order, x = tokens[c]:
+ *     c is kept, and i = c, if W(x) > 0 and accept_u[c] * Z * proposal[i](x) < W(x);
+ *     else W = max(W - Z * proposal[i], 0) and Z = the sum of W.
+ * proposal NULL: the drafted tokens are plain guesses (the likeliest ones, say),
+ * as if proposal[i](x) were 1: c is kept if accept_u[c] * Z < W(x), else W(x) = 0
+ * and Z = Z - the W(x) that was there.
+ * When no child is kept the token after the path is the first t with
+ * W(0) + .. + W(t) > next_u[b] * (the sum of W); where rounding leaves none, the
+ * last t with W(t) > 0; where W holds nothing, the same of target[i]; where that
+ * holds nothing, -1. Probabilities are fp32 or bf16 and all of this is computed
+ * in fp64. Probabilities that are negative or not finite count as 0. A row whose
+ * token is outside [0, vocab), or whose parent is not a row before it, is passed
+ * over. A path ends early at path_cols rows: the token after it is drawn from
+ * that row's target.
+ *
+ *   vocab            1 .. ODS_VERIFY_MAX_VOCAB; row r of target starts at target + r * target_stride
+ *                    values (stride >= vocab), of proposal likewise
+ *   tokens, parent   device int32 [rows]
+ *   accept_u         device fp32 [rows], in [0, 1) (row 0's is not used)
+ *   next_u           device fp32 [batch], in [0, 1)
+ *   path             device [batch][path_cols]: the kept rows as ods_kv_accept takes
+ *                    them, -1 behind them; path_cols 1 .. ODS_DRAFT_MAX_ROWS
+ *   path_len, next_token  device int32 [batch]; 0 and -1 for a sequence without rows
+ *   ws               at least ods_verify_workspace_bytes() bytes
+ * Arrays of this struct need the alignment of their values only, ws 16 bytes. */
+#define ODS_VERIFY_MAX_VOCAB (1 << 24)
+typedef enum { ODS_PROBS_F32 = 0, ODS_PROBS_BF16 = 1 } ods_probs;
+
+typedef struct {
+  int32_t vocab;
+  int32_t dtype;         /* ods_probs, of target and proposal */
+  const void *target;
+  int64_t target_stride;
+  const void *proposal;
+  int64_t proposal_stride;
+  const int32_t *tokens, *parent;
+  const float *accept_u, *next_u;
+  int32_t path_cols;
+  int32_t *path, *path_len, *next_token;
+  void *ws;
+  size_t ws_bytes;
+} ods_verify;
+
+/* Workspace of a verification of up to `batch` sequences over up to `vocab`
+ * tokens (0 on invalid arguments). */
+size_t ods_verify_workspace_bytes(int32_t batch, int32_t vocab);
+
+/* Enqueue the verification of the draft's rows (rows, max_rows and row_off are
+ * read; batch as of its ods_batch). batch == 0 returns ODS_OK with nothing
+ * enqueued. */
+ods_status ods_draft_verify(int32_t batch, const ods_draft *draft, const ods_verify *verify, hipStream_t stream);
 
 /* Message for the last non-OK status returned on this thread ("" if none). */
 const char *ods_last_error(void);

@@ -21,6 +21,10 @@ ODS_WEIGHTS_ROWS, ODS_WEIGHTS_TILED = 0, 1
 
 ODS_ROPE_PLAIN, ODS_ROPE_LINEAR, ODS_ROPE_BASE, ODS_ROPE_ROTATIONS, ODS_ROPE_INDEX = 0, 1, 2, 3, 4
 DRAFT_MAX_ROWS = 256  # ODS_DRAFT_MAX_ROWS
+ROPE_AXES = 8  # ODS_ROPE_AXES
+SHARED_GROUPS = 4095  # ODS_SHARED_GROUPS
+VERIFY_MAX_VOCAB = 1 << 24  # ODS_VERIFY_MAX_VOCAB
+ODS_PROBS_F32, ODS_PROBS_BF16 = 0, 1
 
 BUFFERS = ("resid", "xn", "qkv", "o", "hn", "gu", "act", "logits", "topk_w", "topk_ids", "perm",
            "slot_pos", "expert_off", "xp", "gu_p", "act_p", "yp")
@@ -65,9 +69,25 @@ class ods_rope(C.Structure):
                 ("turns_lo", C.c_double), ("amplitude", C.c_float), ("freqs", C.c_void_p)]
 
 
+class ods_head_norm(C.Structure):
+    _fields_ = [("gain_q", C.c_void_p), ("gain_k", C.c_void_p), ("eps", C.c_float)]
+
+
+class ods_shared(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("group_off", C.c_void_p), ("tokens", C.c_void_p)]
+
+
 class ods_draft(C.Structure):
     _fields_ = [("rows", C.c_int32), ("max_rows", C.c_int32), ("row_off", C.c_void_p), ("depth", C.c_void_p),
-                ("mask", C.c_void_p), ("rope", C.POINTER(ods_rope))]
+                ("mask", C.c_void_p), ("rope", C.POINTER(ods_rope)), ("norm", C.POINTER(ods_head_norm)),
+                ("shared", C.POINTER(ods_shared))]
+
+
+class ods_verify(C.Structure):
+    _fields_ = [("vocab", C.c_int32), ("dtype", C.c_int32), ("target", C.c_void_p), ("target_stride", C.c_int64),
+                ("proposal", C.c_void_p), ("proposal_stride", C.c_int64), ("tokens", C.c_void_p), ("parent", C.c_void_p),
+                ("accept_u", C.c_void_p), ("next_u", C.c_void_p), ("path_cols", C.c_int32), ("path", C.c_void_p),
+                ("path_len", C.c_void_p), ("next_token", C.c_void_p), ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
 
 
 class ods_pages(C.Structure):
@@ -102,6 +122,8 @@ SIGNATURES = {
     "ods_rope_freqs": (C.c_int, [C.POINTER(ods_rope), C.c_void_p]),
     "ods_rope_rows": (C.c_int, [C.POINTER(ods_rope), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32,
                                 C.c_void_p, C.c_void_p]),
+    "ods_head_rows": (C.c_int, [C.POINTER(ods_rope), C.POINTER(ods_head_norm), C.c_void_p, C.c_int32, C.c_void_p, C.c_int64,
+                                C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p]),
     "ods_draft_workspace_bytes": (C.c_size_t, [C.POINTER(ods_block), C.POINTER(ods_batch), C.POINTER(ods_draft)]),
     "ods_run_draft": (C.c_int, [C.POINTER(ods_block), C.c_int32, C.c_int32, C.POINTER(ods_batch), C.POINTER(ods_draft),
                                 C.POINTER(ods_state), C.c_void_p]),
@@ -114,9 +136,12 @@ SIGNATURES = {
     "ods_pages_release": (C.c_int, [C.POINTER(ods_pages), C.c_void_p, C.c_int32]),
     "ods_pages_compact": (C.c_int, [C.POINTER(ods_pages), C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
                                     C.c_void_p]),
+    "ods_pages_shared": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "ods_kv_copy_pages": (C.c_int, [C.POINTER(ods_block), C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]),
     "ods_kv_accept": (C.c_int, [C.POINTER(ods_block), C.c_int32, C.c_int32, C.POINTER(ods_batch), C.POINTER(ods_draft),
                                 C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ods_verify_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
+    "ods_draft_verify": (C.c_int, [C.c_int32, C.POINTER(ods_draft), C.POINTER(ods_verify), C.c_void_p]),
 }
 
 
@@ -237,6 +262,13 @@ def ods_rope_rows(rope: ods_rope, x: int, x_stride: int, y: int, y_stride: int, 
     return lib.ods_rope_rows(C.byref(rope), x, x_stride, y, y_stride, rows, heads, pos, stream)
 
 
+def ods_head_rows(rope: ods_rope, norm, axis, n_axes: int, x: int, x_stride: int, y: int, y_stride: int, rows: int, n_q: int,
+                  n_k: int, pos: int, stream: int) -> int:
+    """norm: ods_head_norm or None; axis: address of the pairs' axes or None."""
+    return lib.ods_head_rows(C.byref(rope), None if norm is None else C.byref(norm), axis, n_axes, x, x_stride, y, y_stride,
+                             rows, n_q, n_k, pos, stream)
+
+
 def ods_draft_workspace_bytes(blk: ods_block, batch: ods_batch, draft: ods_draft) -> int:
     return lib.ods_draft_workspace_bytes(C.byref(blk), C.byref(batch), C.byref(draft))
 
@@ -282,6 +314,15 @@ def ods_pages_compact(pages: ods_pages, table, pairs):
     return st, n.value
 
 
+def ods_pages_shared(table, tokens, group_off, group_tokens):
+    """(status, n_groups). table: int32 numpy [rows, max_pages]; tokens [rows]; group_off [rows + 1], group_tokens [rows]
+    (written)."""
+    n = C.c_int32(0)
+    st = lib.ods_pages_shared(_np(table), table.shape[0], table.shape[1], _np(tokens), _np(group_off), _np(group_tokens),
+                              C.addressof(n))
+    return st, n.value
+
+
 def ods_kv_copy_pages(blk: ods_block, layer_begin: int, layer_end: int, pairs: int, n_pairs: int, stream: int) -> int:
     return lib.ods_kv_copy_pages(C.byref(blk), layer_begin, layer_end, pairs, n_pairs, stream)
 
@@ -290,3 +331,11 @@ def ods_kv_accept(blk: ods_block, layer_begin: int, layer_end: int, batch: ods_b
                   path_cols: int, path_len: int, ctx_out, stream: int) -> int:
     return lib.ods_kv_accept(C.byref(blk), layer_begin, layer_end, C.byref(batch), C.byref(draft), path, path_cols,
                              path_len, ctx_out, stream)
+
+
+def ods_verify_workspace_bytes(batch: int, vocab: int) -> int:
+    return lib.ods_verify_workspace_bytes(batch, vocab)
+
+
+def ods_draft_verify(batch: int, draft: ods_draft, verify: ods_verify, stream: int) -> int:
+    return lib.ods_draft_verify(batch, C.byref(draft), C.byref(verify), stream)

@@ -1,6 +1,7 @@
 // Rotary positions of arbitrary rows (ods_rope_rows): y = x turned to each
 // row's position, half or interleaved pairs, part of the head, frequencies
-// from a table of doubles.
+// from a table of doubles. The same of heads that are normalised first, and of
+// positions with several axes (ods_head_rows).
 #include <algorithm>
 
 #include "kernels.hpp"
@@ -33,7 +34,55 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(const uint16_t *x, int64
   }
 }
 
+// `per` rows a block (kHeadRows at most): rows of few heads share the block's angles and lanes.
+constexpr int kHeadRows = 8;
+template <int KIND>
+__global__ __launch_bounds__(256) void head_rows_kernel(const HeadRowsArgs a, int rows, int per) {
+  __shared__ __align__(16) float cs[kHeadRows * 128], sn[kHeadRows * 128];
+  __shared__ __align__(16) float exchange[KIND == kAny ? 2048 : 4];
+  __shared__ int go[kHeadRows];
+  const int64_t row0 = (int64_t)blockIdx.x * per;
+  const int n = (int)min((int64_t)per, rows - row0), np = a.turn.rdim / 2;
+  const int32_t *pos = a.pos + row0 * a.n_axes;
+  if (threadIdx.x < n) {
+    bool all = true;
+    for (int i = 0; i < a.n_axes; ++i) all = all && pos[threadIdx.x * a.n_axes + i] >= 0;
+    go[threadIdx.x] = all;
+  }
+  for (int t = threadIdx.x; t < n * np; t += 256) {
+    const int r = t / np, i = t - r * np;
+    const int axis = a.axis ? min(max(a.axis[i], 0), a.n_axes - 1) : 0;
+    float c, s;
+    turn_by((double)pos[r * a.n_axes + axis] * a.freqs[i], c, s);
+    cs[t] = c * a.amp;
+    sn[t] = s * a.amp;
+  }
+  __syncthreads();
+  turn_heads<KIND>(
+      a.turn, n, [&](int r) { return a.x + (row0 + r) * a.xs; }, [&](int r) { return a.y + (row0 + r) * a.ys; },
+      [&](int r) { return go[r] != 0; }, cs, sn, exchange);
+}
+
 }  // namespace
+
+hipError_t launch_head_rows(const HeadRowsArgs &args, int rows, hipStream_t s) {
+  if (rows <= 0 || args.turn.heads <= 0) return hipSuccess;
+  const HeadKind kind = head_kind(args.turn.rdim, args.turn.interleaved);
+  const auto kern = kind == kHalves ? head_rows_kernel<kHalves> : kind == kPairs ? head_rows_kernel<kPairs> : head_rows_kernel<kAny>;
+  const int of_row = args.turn.heads << head_lanes_log2(head_items(kind, args.turn.D, args.turn.rdim));
+  const int per = std::min(kHeadRows, std::max(1, 512 / of_row));
+  HeadRowsArgs a = args;
+  const int64_t most = (int64_t)kMaxGridX * per;  // rows of a launch
+  for (int64_t at = 0; at < rows; at += most) {
+    const int n = (int)std::min<int64_t>(rows - at, most);
+    a.x = args.x + at * a.xs;
+    a.y = args.y + at * a.ys;
+    a.pos = args.pos + at * a.n_axes;
+    hipLaunchKernelGGL(kern, dim3((n + per - 1) / per), dim3(256), 0, s, a, n, per);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 hipError_t launch_rope_rows(const ods_rope &r, const uint16_t *x, int64_t xs, uint16_t *y, int64_t ys, int rows,
                             int heads, const int32_t *pos, hipStream_t s) {

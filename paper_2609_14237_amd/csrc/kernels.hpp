@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "plan.hpp"
+#include "turn.hpp"
 
 namespace ods {
 
@@ -75,6 +76,20 @@ constexpr int kMaxGridX = 1 << 23;
 hipError_t launch_rope_rows(const ods_rope &r, const uint16_t *x, int64_t xs, uint16_t *y, int64_t ys, int rows,
                             int heads, const int32_t *pos, hipStream_t s);
 
+// The same of heads that are normalised first, and of positions of several axes (arguments checked by check_head_rows).
+struct HeadRowsArgs {
+  HeadTurn turn;
+  const uint16_t *x;
+  int64_t xs;
+  uint16_t *y;
+  int64_t ys;
+  const int32_t *pos, *axis;
+  int n_axes;
+  const double *freqs;
+  float amp;
+};
+hipError_t launch_head_rows(const HeadRowsArgs &a, int rows, hipStream_t s);
+
 // Drafted rows of one layer: B sequences, `rows` rows of the buffers.
 struct DraftArgs {
   uint16_t *qkv;
@@ -88,10 +103,16 @@ struct DraftArgs {
   const double *freqs;  // null: the layer's own theta, whole head, half layout
   int rdim, interleaved;
   float amp, theta;
+  const uint16_t *gain_q, *gain_k;  // null: heads are turned as they are
+  float eps;
+  ods_shared shared;   // n_groups 0: none
+  int batch, base;     // sequences of the call, of which B from `base` on are a launch's
 };
 hipError_t launch_draft_rope_append(const DraftArgs &a, bool do_rope, bool do_append, hipStream_t s);
 // ws: tree_ws_bytes(plan, D).
 hipError_t launch_tree_attention(const DraftArgs &a, const TreePlan &plan, void *ws, hipStream_t s);
+// The same with shared prefixes. ws: shared_ws_bytes(plan, ...).
+hipError_t launch_shared_attention(const DraftArgs &a, const SharedPlan &plan, void *ws, hipStream_t s);
 
 // Pools of several layers, handed to one launch by value.
 constexpr int kPoolSet = 32;
@@ -112,5 +133,8 @@ hipError_t launch_copy_pages(const PoolSet &pools, int n_pools, const int32_t *p
 // ctx_out: NULL or where the new contexts go; launch_accept_ctx for one that is a.ctx_lens, after all of launch_accept.
 hipError_t launch_accept(const AcceptArgs &a, const PoolSet &pools, int n_pools, int max_kv, int32_t *ctx_out, hipStream_t s);
 hipError_t launch_accept_ctx(const AcceptArgs &a, int32_t *ctx_out, hipStream_t s);
+
+// Accepted paths and the tokens after them (arguments checked by check_verify).
+hipError_t launch_verify(int batch, const ods_draft &draft, const ods_verify &v, hipStream_t s);
 
 }  // namespace ods

@@ -173,6 +173,12 @@ DraftArgs draft_args(const ods_block *blk, int layer, const ods_batch *batch, co
     const ods_rope &r = draft->rope[layer];
     a.freqs = r.freqs; a.rdim = r.rotary_dim; a.interleaved = r.interleaved; a.amp = r.amplitude;
   }
+  if (draft->norm) {
+    const ods_head_norm &n = draft->norm[layer];
+    a.gain_q = (const uint16_t *)n.gain_q; a.gain_k = (const uint16_t *)n.gain_k; a.eps = n.eps;
+  }
+  a.batch = batch->batch;
+  if (takes_shared(c, draft)) a.shared = *draft->shared;
   return a;
 }
 
@@ -307,11 +313,43 @@ ods_status ods_graph_destroy(hipGraphExec_t exec) {
 
 ods_status ods_rope_rows(const ods_rope *rope, const void *x, int64_t x_stride, void *y, int64_t y_stride,
                          int32_t rows, int32_t heads, const int32_t *pos, hipStream_t stream) {
-  const ods_status rc = check_rope_rows(rope, x, x_stride, y, y_stride, rows, heads, pos);
+  const ods_status rc = check_rope_rows("ods_rope_rows", rope, x, x_stride, y, y_stride, rows, heads, pos);
   if (rc != ODS_OK) return rc;
   const hipError_t e = launch_rope_rows(*rope, (const uint16_t *)x, x_stride, (uint16_t *)y, y_stride, rows, heads, pos,
                                         stream);
   if (e != hipSuccess) return set_error(ODS_EHIP, "ods_rope_rows: %s", hipGetErrorString(e));
+  clear_error();
+  return ODS_OK;
+}
+
+ods_status ods_head_rows(const ods_rope *rope, const ods_head_norm *norm, const int32_t *axis, int32_t n_axes,
+                         const void *x, int64_t x_stride, void *y, int64_t y_stride, int32_t rows, int32_t n_q,
+                         int32_t n_k, const int32_t *pos, hipStream_t stream) {
+  const ods_status rc = check_head_rows(rope, norm, axis, n_axes, x, x_stride, y, y_stride, rows, n_q, n_k, pos);
+  if (rc != ODS_OK) return rc;
+  HeadRowsArgs a{};
+  a.turn.heads = n_q + n_k; a.turn.n_q = n_q; a.turn.D = rope->head_dim; a.turn.rdim = rope->rotary_dim;
+  a.turn.interleaved = rope->interleaved;
+  if (norm) {
+    a.turn.gain_q = (const uint16_t *)norm->gain_q; a.turn.gain_k = (const uint16_t *)norm->gain_k; a.turn.eps = norm->eps;
+  }
+  a.x = (const uint16_t *)x; a.xs = x_stride;
+  a.y = (uint16_t *)y; a.ys = y_stride;
+  a.pos = pos; a.axis = axis; a.n_axes = n_axes;
+  a.freqs = rope->freqs; a.amp = rope->amplitude;
+  const hipError_t e = launch_head_rows(a, rows, stream);
+  if (e != hipSuccess) return set_error(ODS_EHIP, "ods_head_rows: %s", hipGetErrorString(e));
+  clear_error();
+  return ODS_OK;
+}
+
+ods_status ods_draft_verify(int32_t batch, const ods_draft *draft, const ods_verify *verify, hipStream_t stream) {
+  const ods_status rc = check_verify(batch, draft, verify);
+  if (rc != ODS_OK) return rc;
+  if (batch > 0) {
+    const hipError_t e = launch_verify(batch, *draft, *verify, stream);
+    if (e != hipSuccess) return set_error(ODS_EHIP, "ods_draft_verify: %s", hipGetErrorString(e));
+  }
   clear_error();
   return ODS_OK;
 }
@@ -341,9 +379,11 @@ ods_status ods_run_draft(const ods_block *blk, int32_t op_begin, int32_t op_end,
     }
     const OpRef op = op_at(blk, step.begin);
     const DraftArgs a = draft_args(blk, op.layer, batch, draft, st);
-    const hipError_t e =
-        step.attn ? launch_tree_attention(a, tree_plan(blk->layers[op.layer].cfg, batch, draft, cus), st->ws, stream)
-                  : launch_draft_rope_append(a, step.rope, step.append, stream);
+    const ods_layer_cfg &c = blk->layers[op.layer].cfg;
+    const hipError_t e = !step.attn ? launch_draft_rope_append(a, step.rope, step.append, stream)
+                         : takes_shared(c, draft)
+                             ? launch_shared_attention(a, shared_plan(c, batch, draft, cus), st->ws, stream)
+                             : launch_tree_attention(a, tree_plan(c, batch, draft, cus), st->ws, stream);
     const char *what = step.rope && step.append ? "rope+kv_append" : op_kind_name(op.kind);
     if (trace)
       fprintf(stderr, "[ods] layer %d drafted %s B=%d rows=%d -> %s\n", op.layer, what, a.B, a.rows, hipGetErrorString(e));

@@ -79,9 +79,8 @@ ods_status check_rope(const ods_rope *r, const char *who, bool need_freqs) {
   return ODS_OK;
 }
 
-ods_status check_rope_rows(const ods_rope *r, const void *x, int64_t xs, const void *y, int64_t ys, int rows, int heads,
-                           const int32_t *pos) {
-  const char *who = "ods_rope_rows";
+ods_status check_rope_rows(const char *who, const ods_rope *r, const void *x, int64_t xs, const void *y, int64_t ys, int rows,
+                           int heads, const int32_t *pos) {
   ods_status rc = check_rope(r, who, true);
   if (rc != ODS_OK) return rc;
   if (rows < 0 || heads < 0) return set_error(ODS_EINVAL, "%s: rows %d, heads %d", who, rows, heads);
@@ -103,6 +102,27 @@ ods_status check_rope_rows(const ods_rope *r, const void *x, int64_t xs, const v
     if (xs != ys || gap < width || gap > xs - width) return set_error(ODS_EINVAL, "%s: x and y overlap", who);
   }
   return ODS_OK;
+}
+
+ods_status check_head_norm(const ods_head_norm *n, const char *who, bool q, bool k) {
+  if (!(n->eps >= 0.f) || !std::isfinite(n->eps)) return set_error(ODS_EINVAL, "%s: eps must be finite and not negative", who);
+  ods_status rc = ODS_OK;
+  if (q && (rc = check_ptr(n->gain_q, who, "gain_q")) != ODS_OK) return rc;
+  if (k && (rc = check_ptr(n->gain_k, who, "gain_k")) != ODS_OK) return rc;
+  return ODS_OK;
+}
+
+ods_status check_head_rows(const ods_rope *r, const ods_head_norm *norm, const int32_t *axis, int n_axes, const void *x,
+                           int64_t xs, const void *y, int64_t ys, int rows, int n_q, int n_k, const int32_t *pos) {
+  const char *who = "ods_head_rows";
+  if (rows < 0 || n_q < 0 || n_k < 0 || n_q > INT32_MAX - n_k)
+    return set_error(ODS_EINVAL, "%s: rows %d, heads %d + %d", who, rows, n_q, n_k);
+  if (n_axes < 1 || n_axes > ODS_ROPE_AXES) return set_error(ODS_EINVAL, "%s: n_axes %d (need 1 .. %d)", who, n_axes, ODS_ROPE_AXES);
+  if (n_axes > 1 && !axis) return set_error(ODS_EINVAL, "%s: %d axes without a table", who, n_axes);
+  if ((uintptr_t)axis & 3u) return set_error(ODS_EINVAL, "%s: axis is not 4-byte aligned", who);
+  ods_status rc = check_rope_rows(who, r, x, xs, y, ys, rows, n_q + n_k, pos);
+  if (rc != ODS_OK || !norm) return rc;
+  return check_head_norm(norm, who, n_q > 0, n_k > 0);
 }
 
 // ---------------------------------------------------------------- drafted ranges
@@ -180,6 +200,33 @@ size_t tree_ws_bytes(const TreePlan &p, int D) {
   return (size_t)p.grid * kTreeDescBytes + (size_t)2 * p.grid * p.qt * (D + 2) * sizeof(float);
 }
 
+SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus) {
+  SharedPlan s;
+  s.tail = tree_plan(c, batch, draft, cus);
+  // The host knows no group's rows: a tile as wide as the mean group's columns, more tiles for larger groups.
+  TreePlan &p = s.prefix;
+  const int group = c.n_q / c.n_kv, groups = std::max(draft->shared->n_groups, 1);
+  const int64_t columns = (int64_t)draft->rows * group;
+  p.qt = 16;
+  while (p.qt < columns / groups && p.qt < 256) p.qt *= 2;
+  p.max_qt = 2;  // more than one: the kernel asks each group
+  const int64_t tiles = ((int64_t)batch->max_pages * ODS_PAGE_TOKENS + 31) / 32;
+  const int64_t tasks = c.n_kv * (columns / p.qt + groups), units = tasks * tiles;
+  p.units_ok = units < (int64_t)1 << 30;
+  p.min_tiles = 4;
+  p.equal = p.qt == 128;
+  const int per_cu = p.qt <= 16 ? 256 / c.head_dim : p.qt <= 128 ? 2 : 1;
+  p.grid = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)std::max(cus, 1) * per_cu, (units + p.min_tiles - 1) / p.min_tiles));
+  p.stream = false;
+  p.no_cut = false;
+  p.split_join = p.grid > 6 * tasks;
+  return s;
+}
+
+size_t shared_ws_bytes(const SharedPlan &p, int rows, int n_q, int D) {
+  return shared_state_bytes(rows, n_q, D) + std::max(tree_ws_bytes(p.prefix, D), tree_ws_bytes(p.tail, D));
+}
+
 ods_batch row_batch(const ods_batch *batch, const ods_draft *draft) {
   ods_batch b = *batch;
   b.batch = draft->rows;
@@ -194,7 +241,10 @@ size_t draft_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_
   for (int g = op_begin; g < op_end; ++g) {
     const OpRef op = op_at(blk, g);
     const ods_layer_cfg &c = blk->layers[op.layer].cfg;
-    if (op.kind == K_ATTN_CORE) w = std::max(w, tree_ws_bytes(tree_plan(c, batch, draft, cus), c.head_dim));
+    if (op.kind != K_ATTN_CORE) continue;
+    w = std::max(w, takes_shared(c, draft)
+                        ? shared_ws_bytes(shared_plan(c, batch, draft, cus), draft->rows, c.n_q, c.head_dim)
+                        : tree_ws_bytes(tree_plan(c, batch, draft, cus), c.head_dim));
   }
   return w;
 }
@@ -203,25 +253,48 @@ size_t draft_ws_most(const ods_block *blk, const ods_batch *batch, const ods_dra
   size_t w = std::max<size_t>(256, rows_ws_most(blk, draft->rows));
   for (int l = 0; l < blk->n_layers; ++l) {
     const ods_layer_cfg &c = blk->layers[l].cfg;
+    const bool shared = takes_shared(c, draft);
+    size_t records = 0;
     auto take = [&](int max_rows) {
       ods_draft d = *draft;
       d.max_rows = max_rows;
-      w = std::max(w, tree_ws_bytes(tree_plan(c, batch, &d, cus), c.head_dim));
+      records = std::max(records, tree_ws_bytes(tree_plan(c, batch, &d, cus), c.head_dim));
     };
+    // Prefixes: the records of every tile width, on as many compute units.
+    for (int qt = 16; shared && qt <= 256; qt *= 2) {
+      TreePlan p{};
+      p.qt = qt;
+      p.grid = std::max(cus, 1) * (qt <= 16 ? 256 / c.head_dim : qt <= 128 ? 2 : 1);
+      records = std::max(records, tree_ws_bytes(p, c.head_dim));
+    }
     // A query tile's width times the grid may be more for a narrower tree, of which more workgroups share a compute unit; of
     // the trees of one width the longest needs most.
     for (int qt = 16; qt <= 256; qt *= 2)
       if (qt / (c.n_q / c.n_kv) >= 1) take(std::min(draft->max_rows, qt / (c.n_q / c.n_kv)));
     take(draft->max_rows);
+    w = std::max(w, records + (shared ? shared_state_bytes(draft->rows, c.n_q, c.head_dim) : 0));
   }
   return w;
 }
 
+namespace {
+
+ods_status check_shared(const ods_shared *s, const ods_batch *batch) {
+  if (!s) return ODS_OK;
+  if (s->n_groups < 0 || s->n_groups > batch->batch)
+    return set_error(ODS_EINVAL, "shared n_groups %d of %d sequences", s->n_groups, batch->batch);
+  if (s->n_groups > ODS_SHARED_GROUPS)
+    return set_error(ODS_EUNSUPPORTED, "shared n_groups %d (at most %d)", s->n_groups, ODS_SHARED_GROUPS);
+  return ODS_OK;
+}
+
+}  // namespace
+
 ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch,
                              const ods_draft *draft) {
   if (!batch || !draft) return set_error(ODS_EINVAL, "null batch or draft");
-  const ods_status rc = check_counts(batch, draft);
-  if (rc != ODS_OK) return rc;
+  ods_status rc = check_counts(batch, draft);
+  if (rc != ODS_OK || (rc = check_shared(draft->shared, batch)) != ODS_OK) return rc;
   for (int g = op_begin; g < op_end; ++g) {
     const OpRef op = op_at(blk, g);
     const ods_layer_cfg &c = blk->layers[op.layer].cfg;
@@ -229,6 +302,8 @@ ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, con
       return set_error(ODS_EUNSUPPORTED, "layer %d: draft rows * n_q exceeds 2^31", op.layer);
     if (op.kind == K_ATTN_CORE && !tree_plan(c, batch, draft, 1).units_ok)
       return set_error(ODS_EUNSUPPORTED, "layer %d: batch * n_kv * query tiles * window pages exceeds 2^30", op.layer);
+    if (op.kind == K_ATTN_CORE && takes_shared(c, draft) && !shared_plan(c, batch, draft, 1).prefix.units_ok)
+      return set_error(ODS_EUNSUPPORTED, "layer %d: n_kv * query tiles of the groups * pages exceeds 2^30", op.layer);
   }
   return ODS_OK;
 }
@@ -266,10 +341,14 @@ ods_status validate_draft(const ods_block *blk, int op_begin, int op_end, const 
         return set_error(ODS_EINVAL, "layer %d: rope of head_dim %d for heads of %d", layer, draft->rope[layer].head_dim,
                          c.head_dim);
     }
+    if (s.rope && draft->norm && (rc = check_head_norm(&draft->norm[layer], who, true, true)) != ODS_OK) return rc;
     if ((s.append || s.attn) && (rc = check_table(L, layer, batch, draft)) != ODS_OK) return rc;
     if (s.attn) {
       if ((rc = check_ptr(draft->mask, who, "mask")) != ODS_OK || (rc = check_ptr(st->o, who, "o")) != ODS_OK ||
           (rc = check_ptr(st->ws, who, "ws")) != ODS_OK)
+        return rc;
+      if (takes_shared(c, draft) && ((rc = check_ptr(draft->shared->group_off, who, "shared group_off")) != ODS_OK ||
+                                     (rc = check_ptr(draft->shared->tokens, who, "shared tokens")) != ODS_OK))
         return rc;
       if (need == 0) need = draft_ws_bytes(blk, op_begin, op_end, batch, draft, cus);
       if (st->ws_bytes < need) return set_error(ODS_ENOMEM, "workspace %zu bytes < required %zu", st->ws_bytes, need);

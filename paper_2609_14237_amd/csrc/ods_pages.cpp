@@ -140,6 +140,40 @@ ods_status ods_pages_release(ods_pages *p, int32_t *row, int32_t max_pages) {
   return ODS_OK;
 }
 
+ods_status ods_pages_shared(const int32_t *table, int32_t rows, int32_t max_pages, const int32_t *tokens,
+                            int32_t *group_off, int32_t *group_tokens, int32_t *n_groups) {
+  const char *who = "ods_pages_shared";
+  if (!table || !tokens || !group_off || !group_tokens || !n_groups) return set_error(ODS_EINVAL, "%s: null pointer", who);
+  if (rows < 0 || max_pages < 1) return set_error(ODS_EINVAL, "%s: rows %d, max_pages %d", who, rows, max_pages);
+  for (int32_t r = 0; r < rows; ++r)
+    if (tokens[r] < 0 || pages_of(tokens[r]) > max_pages)
+      return set_error(ODS_EINVAL, "%s: row %d of %d tokens in %d pages", who, r, tokens[r], max_pages);
+  int32_t n = 0;
+  group_off[0] = 0;
+  for (int32_t r = 0; r < rows;) {
+    const int32_t *first = table + (int64_t)r * max_pages;
+    int64_t common = tokens[r] / ODS_PAGE_TOKENS;  // whole pages of the rows so far
+    int32_t end = r + 1;
+    for (; end < rows; ++end) {
+      const int32_t *row = table + (int64_t)end * max_pages;
+      const int64_t most = std::min<int64_t>(common, tokens[end] / ODS_PAGE_TOKENS);
+      int64_t same = 0;
+      while (same < most && row[same] >= 0 && row[same] == first[same]) ++same;
+      const int64_t saved = (end - r - 1) * common, then = (end - r) * same;
+      if (then == 0 || then < saved) break;
+      common = same;
+    }
+    const int32_t of_group = end - r > 1 ? (int32_t)(common * ODS_PAGE_TOKENS) : 0;
+    if (of_group == 0 && n > 0 && group_tokens[n - 1] == 0) --n;  // with the row before, which shares nothing either
+    group_tokens[n] = of_group;
+    group_off[++n] = end;
+    r = end;
+  }
+  *n_groups = n;
+  clear_error();
+  return ODS_OK;
+}
+
 ods_status ods_pages_compact(ods_pages *p, int32_t *table, int32_t rows, int32_t max_pages, int32_t *pairs,
                              int32_t max_pairs, int32_t *n_pairs) {
   const char *who = "ods_pages_compact";

@@ -198,9 +198,13 @@ void plan_launch(const ods_block *blk, int op_begin, int op_end, int i, const od
 // Fields of an ods_rope outside the documented ranges; `who` names it in the message. Its freqs pointer only
 // with need_freqs.
 ods_status check_rope(const ods_rope *r, const char *who, bool need_freqs);
-// Arguments of ods_rope_rows.
-ods_status check_rope_rows(const ods_rope *r, const void *x, int64_t xs, const void *y, int64_t ys, int rows, int heads,
+// Arguments of ods_rope_rows, or of a call that takes the same rows.
+ods_status check_rope_rows(const char *who, const ods_rope *r, const void *x, int64_t xs, const void *y, int64_t ys, int rows, int heads,
                            const int32_t *pos);
+
+// Arguments of ods_head_rows.
+ods_status check_head_rows(const ods_rope *r, const ods_head_norm *norm, const int32_t *axis, int n_axes, const void *x,
+                           int64_t xs, const void *y, int64_t ys, int rows, int n_q, int n_k, const int32_t *pos);
 
 // Tiles a range may have above an even share, so that no task is cut.
 constexpr int kSplitTiles = 24;
@@ -220,6 +224,21 @@ struct TreePlan {
 constexpr int kTreeDescBytes = 32;
 TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus);
 size_t tree_ws_bytes(const TreePlan &p, int D);
+
+// The same where groups of sequences share a prefix: two launches, over the groups' prefixes (their query tiles are of all
+// the group's rows) and over what each sequence has beyond. Between them a state of every row and query head.
+struct SharedPlan {
+  TreePlan prefix, tail;
+};
+// Whether a layer's attention takes the draft's groups.
+inline bool takes_shared(const ods_layer_cfg &c, const ods_draft *draft) {
+  return draft->shared && draft->shared->n_groups > 0 && c.window == 0;
+}
+SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus);
+inline size_t shared_state_bytes(int rows, int n_q, int D) {  // of sums, then of (maximum, denominator)
+  return ((size_t)rows * n_q * (D + 2) * sizeof(float) + 15) / 16 * 16;
+}
+size_t shared_ws_bytes(const SharedPlan &p, int rows, int n_q, int D);
 
 inline bool is_kv_op(OpKind k) { return k == K_ROPE || k == K_KV_APPEND || k == K_ATTN_CORE; }
 // One step of a drafted range: a run [begin, end) of operators that only see rows (ods_run_partition on
@@ -241,6 +260,14 @@ ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, con
 // Every check ods_run_draft makes before it enqueues anything.
 ods_status validate_draft(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, const ods_draft *draft,
                           const ods_state *st, int cus);
+// Arguments of ods_draft_verify, and where its workspace's parts are.
+ods_status check_verify(int batch, const ods_draft *draft, const ods_verify *v);
+constexpr int kVerifyChunk = 1024;  // values of the vocabulary whose sum is kept
+struct VerifyWs {
+  size_t head, list, sums, bytes;  // offsets: per sequence 16 bytes, ODS_DRAFT_MAX_ROWS doubles, chunks doubles
+  int chunks;
+};
+VerifyWs verify_ws(int batch, int vocab);
 // Checks of the page operators (block, layer range, pools).
 ods_status check_pools(const ods_block *blk, int layer_begin, int layer_end, const char *who);
 ods_status check_accept(const ods_block *blk, int layer_begin, int layer_end, const ods_batch *batch,

@@ -98,6 +98,123 @@ __device__ __forceinline__ void turn_row_by_values(const uint16_t *src, uint16_t
   }
 }
 
+// ---------------------------------------------------------------- heads normalised before they turn
+//
+// y = R(pos) (x inv gain), inv = (mean(x^2) + eps)^-1/2 over the head, rounded once, at the end. A head lies on L
+// neighbouring lanes of one wave (L a power of two, 32 at most), so its sum of squares is a reduction over lanes and a value
+// is read once and written once.
+struct HeadTurn {
+  int heads, n_q, D, rdim, interleaved;
+  const uint16_t *gain_q, *gain_k;  // null: no norm
+  float eps;
+};
+
+enum HeadKind {
+  kHalves,  // half layout, rdim % 16 == 0: an item is 16 bytes of first values and the 16 of their mates, or 16 that pass through
+  kPairs,   // interleaved, rdim % 8 == 0: an item is four pairs
+  kAny      // else an item is 8 values, whose mates come from the neighbouring lanes by way of LDS
+};
+__host__ __device__ inline HeadKind head_kind(int rdim, int interleaved) {
+  return rdim % (interleaved ? 8 : 16) != 0 ? kAny : interleaved ? kPairs : kHalves;
+}
+__host__ __device__ inline int head_items(HeadKind kind, int D, int rdim) {
+  return kind == kHalves ? rdim / 16 + (D - rdim) / 8 : D / 8;
+}
+// log2 of the lanes of a head
+__host__ __device__ inline int head_lanes_log2(int items) {
+  int log = 0;
+  while (1 << log < items) ++log;
+  return log;
+}
+
+// Heads of `rows` rows by the 256 threads of a block; src(r) and dst(r) are a row's first value (they may be the same), go(r)
+// whether it is done at all. Row r's cosines start at cs + r * rdim / 2. exchange: 2048 floats of LDS, kAny only.
+template <int KIND, typename Src, typename Dst, typename Go>
+__device__ __forceinline__ void turn_heads(const HeadTurn &p, int rows, Src src, Dst dst, Go go, const float *cs, const float *sn,
+                                           float *exchange) {
+  constexpr int U = 2;  // items of a thread in flight
+  const int np = p.rdim / 2, turned = np / 8, items = head_items((HeadKind)KIND, p.D, p.rdim);
+  const int log = head_lanes_log2(items), lanes = 1 << log, total = rows * p.heads << log;
+  const float inv_d = 1.f / (float)p.D;
+  for (int t0 = 0; t0 < total; t0 += 256 * U) {
+    u32x4 a[U], b[U];
+    int row[U], head[U], at[U];  // at: first dim of the item, -1: none
+    bool pair[U];                // kHalves: the item has mates
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * 256 + (int)threadIdx.x, h = min(t >> log, rows * p.heads - 1), i = t & (lanes - 1);
+      row[u] = h / p.heads;
+      head[u] = h - row[u] * p.heads;
+      pair[u] = KIND == kHalves && i < turned;
+      at[u] = t >= total || i >= items || !go(row[u]) ? -1 : KIND != kHalves || i < turned ? i * 8 : p.rdim + (i - turned) * 8;
+      a[u] = b[u] = u32x4{0u, 0u, 0u, 0u};
+      if (at[u] < 0) continue;
+      const uint16_t *x = src(row[u]) + head[u] * p.D + at[u];
+      a[u] = *(const u32x4 *)x;
+      if (pair[u]) b[u] = *(const u32x4 *)(x + np);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[8], w[8];  // the item's values, and their mates (kHalves)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[2 * k] = bf_lo(a[u][k]);
+        v[2 * k + 1] = bf_hi(a[u][k]);
+        w[2 * k] = bf_lo(b[u][k]);
+        w[2 * k + 1] = bf_hi(b[u][k]);
+      }
+      if (p.gain_q || p.gain_k) {
+        float sum = sumsq8(a[u]);
+        if (KIND == kHalves) sum += sumsq8(b[u]);
+        for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, o, kWave);
+        const float inv = rsqrtf(sum * inv_d + p.eps);
+        const uint16_t *g = (head[u] < p.n_q ? p.gain_q : p.gain_k) + max(at[u], 0);
+        const u32x4 ga = *(const u32x4 *)g;
+        const u32x4 gb = pair[u] ? *(const u32x4 *)(g + np) : ga;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          v[2 * k] *= inv * bf_lo(ga[k]);
+          v[2 * k + 1] *= inv * bf_hi(ga[k]);
+          w[2 * k] *= inv * bf_lo(gb[k]);
+          w[2 * k + 1] *= inv * bf_hi(gb[k]);
+        }
+      }
+      const float *c = cs + row[u] * np, *s = sn + row[u] * np;
+      if (KIND == kHalves && pair[u]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) turn2(v[k], w[k], c[at[u] + k], s[at[u] + k]);
+      } else if (KIND == kPairs && at[u] >= 0 && at[u] < p.rdim) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) turn2(v[2 * k], v[2 * k + 1], c[at[u] / 2 + k], s[at[u] / 2 + k]);
+      } else if (KIND == kAny) {
+        float *mine = exchange + threadIdx.x * 8;
+        *(f32x4 *)mine = f32x4{v[0], v[1], v[2], v[3]};
+        *(f32x4 *)(mine + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        // A wave's LDS operations are done in order: the writes above and those of the next item need no wait, only to stay
+        // where they are.
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("" ::: "memory");
+        const float *first = exchange + (threadIdx.x & ~(lanes - 1)) * 8;  // the head's dim 0
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int d = at[u] + k;
+          if (at[u] < 0 || d >= p.rdim) continue;
+          const bool low = p.interleaved ? !(d & 1) : d < np;
+          const int j = p.interleaved ? d >> 1 : low ? d : d - np;
+          const float mate = first[p.interleaved ? d ^ 1 : low ? d + np : d - np];
+          v[k] = low ? v[k] * c[j] - mate * s[j] : v[k] * c[j] + mate * s[j];
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_wave_barrier();
+      }
+      if (at[u] < 0) continue;
+      uint16_t *y = dst(row[u]) + head[u] * p.D + at[u];
+      *(u32x4 *)y = u32x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+      if (pair[u]) *(u32x4 *)(y + np) = u32x4{pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7])};
+    }
+  }
+}
+
 // Whether turn_row takes it.
 __host__ __device__ inline bool turns_wide(int rdim, int interleaved) { return rdim % (interleaved ? 8 : 16) == 0; }
 

@@ -9,7 +9,8 @@ import numpy as np
 import torch
 
 from . import binding as _b
-from .binding import ods_batch, ods_block, ods_draft, ods_layer, ods_layer_cfg, ods_pages, ods_rope, ods_state
+from .binding import (ods_batch, ods_block, ods_draft, ods_head_norm, ods_layer, ods_layer_cfg, ods_pages, ods_rope,
+                      ods_shared, ods_state, ods_verify)
 
 
 def layer_cfg(cfg) -> ods_layer_cfg:
@@ -168,14 +169,19 @@ class Rope:
     """Rotary positions with their device table of frequencies (ods_rope): theta, the rotated part of the head
     (rotary_dim, default all), pair layout, and scaling for long contexts: "plain", "linear", "base", "rotations" or
     "index" (include/ods.h has the formulas). `turns` is (turns_hi, turns_lo) of the last two, by default (4, 1) and
-    (32, 1)."""
+    (32, 1).
+
+    Positions of several axes (time, height, width): `sections` has the pairs of each axis, rotary_dim / 2 in all, dealt
+    out in `order` "blocks" (the first pairs are the first axis's) or "cyclic" (one pair each in turn, while an axis has
+    some left). A pair keeps the frequency of its place in the head, or, with own_freqs, every axis has the frequencies
+    of a rotary part of its own size."""
 
     SCALINGS = {"plain": _b.ODS_ROPE_PLAIN, "linear": _b.ODS_ROPE_LINEAR, "base": _b.ODS_ROPE_BASE,
                 "rotations": _b.ODS_ROPE_ROTATIONS, "index": _b.ODS_ROPE_INDEX}
 
     def __init__(self, head_dim: int, theta: float = 10000.0, rotary_dim: int | None = None, interleaved: bool = False,
                  scaling: str = "plain", factor: float = 1.0, orig_ctx: float = 8192.0, turns=None,
-                 amplitude: float = 1.0, device="cuda"):
+                 amplitude: float = 1.0, device="cuda", sections=None, order: str = "blocks", own_freqs: bool = False):
         if scaling not in self.SCALINGS:
             raise ValueError(f"scaling {scaling!r}: one of {', '.join(self.SCALINGS)}")
         hi, lo = turns if turns is not None else ((32.0, 1.0) if scaling == "index" else (4.0, 1.0))
@@ -184,35 +190,111 @@ class Rope:
                           amplitude, None)
         host = np.zeros(max(rdim // 2, 1), np.float64)
         _b._check(_b.ods_rope_freqs(self.c, host), "ods_rope_freqs")
+        self.axes, self.axis = 1, None
+        if sections is not None:
+            sections = [int(n) for n in sections]
+            if order not in ("blocks", "cyclic"):
+                raise ValueError(f"Rope: order {order!r}: blocks or cyclic")
+            if min(sections, default=-1) < 0 or sum(sections) != rdim // 2 or len(sections) > _b.ROPE_AXES:
+                raise ValueError(f"Rope: sections {sections} of {rdim // 2} pairs (at most {_b.ROPE_AXES} axes)")
+            self.axes = len(sections)
+            axis = _deal(sections, order)
+            if own_freqs:
+                part = ods_rope.from_buffer_copy(self.c)
+                for a, n in enumerate(sections):
+                    own = np.zeros(max(n, 1), np.float64)
+                    part.rotary_dim = 2 * n
+                    if n:
+                        _b._check(_b.ods_rope_freqs(part, own), "ods_rope_freqs")
+                        host[:rdim // 2][axis == a] = own
+            self.axis = torch.from_numpy(axis).to(device)
         self.freqs = torch.from_numpy(host).to(device)
         self.c.freqs = self.freqs.data_ptr()
 
 
-def rope(r: Rope, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor | None = None, stream: int | None = None):
+def _deal(sections, order: str) -> np.ndarray:
+    """Axis of every pair, int32."""
+    if order == "blocks":
+        return np.repeat(np.arange(len(sections), dtype=np.int32), sections)
+    left, axis = list(sections), []
+    while any(left):
+        for a, n in enumerate(left):
+            if n:
+                axis.append(a)
+                left[a] = n - 1
+    return np.array(axis, np.int32)
+
+
+class HeadNorm:
+    """Heads normalised before they turn (ods_head_norm): x / rms(x) * gain over a head. gain_q, gain_k: bf16 [head_dim]
+    for the query heads, the first n_q of a row (default: all of them), and for the key heads behind them."""
+
+    def __init__(self, gain_q: torch.Tensor, gain_k: torch.Tensor | None = None, n_q: int | None = None, eps: float = 1e-6):
+        for name, g in (("gain_q", gain_q), ("gain_k", gain_k)):
+            if g is not None and (g.dtype != torch.bfloat16 or g.dim() != 1 or g.shape != gain_q.shape):
+                raise ValueError(f"HeadNorm: {name} is bf16 [head_dim], got {g.dtype} {tuple(g.shape)}")
+        self.gain_q = gain_q.contiguous()
+        self.gain_k = None if gain_k is None else gain_k.contiguous()
+        self.n_q = n_q
+        self.head_dim = gain_q.shape[0]
+        self.c = ods_head_norm(_ptr(self.gain_q), _ptr(self.gain_k), eps)
+        self.devices = _devices(self.gain_q, self.gain_k)
+
+
+def rope(r: Rope, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor | None = None, stream: int | None = None,
+         norm: HeadNorm | None = None):
     """Rotate x [rows, heads, head_dim] (bf16; the last two dims contiguous, rows at any stride of 8) to positions
-    pos [rows] (int32; rows with a negative one are left alone) into out (default x, in place); returns out."""
+    pos [rows] (int32; rows with a negative one are left alone) into out (default x, in place); returns out. With `norm`
+    the heads are normalised first, in the same pass. A Rope with sections takes pos [rows, axes]."""
     y = x if out is None else out
     for t in (x, y):
         if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[2] != r.c.head_dim:
             raise ValueError(f"rope takes bf16 [rows, heads, {r.c.head_dim}], got {t.dtype} {tuple(t.shape)}")
         if t.numel() and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != r.c.head_dim)):
             raise ValueError("rope: the heads of a row must be contiguous")
-    if x.shape != y.shape or pos.dtype != torch.int32 or pos.shape != x.shape[:1] or not pos.is_contiguous():
+    places = x.shape[:1] if r.axis is None else (x.shape[0], r.axes)
+    if x.shape != y.shape or pos.dtype != torch.int32 or pos.shape != places or not pos.is_contiguous():
         raise ValueError(f"rope: x {tuple(x.shape)}, out {tuple(y.shape)}, pos {pos.dtype} {tuple(pos.shape)}")
     rows, heads = x.shape[:2]
     width = heads * r.c.head_dim  # the stride of a single row means nothing
     xs, ys = (t.stride(0) if rows > 1 else width for t in (x, y))
+    if norm is not None or r.axis is not None:
+        n_q = heads if norm is None or norm.n_q is None else norm.n_q
+        if norm is not None and (norm.head_dim != r.c.head_dim or not 0 <= n_q <= heads or (n_q < heads and norm.gain_k is None)):
+            raise ValueError(f"rope: a norm of heads of {norm.head_dim}, {n_q} with gain_q, for {heads} of {r.c.head_dim}")
+        on = _devices(x, y, pos, r.freqs, r.axis) + (norm.devices if norm is not None else ())
+        _b._check(_b.ods_head_rows(r.c, None if norm is None else norm.c, _ptr(r.axis), r.axes, x.data_ptr(), xs, y.data_ptr(),
+                                   ys, rows, n_q, heads - n_q, pos.data_ptr(), _stream_of("rope", stream, *on)),
+                  "ods_head_rows")
+        return y
     _b._check(_b.ods_rope_rows(r.c, x.data_ptr(), xs, y.data_ptr(), ys, rows, heads, pos.data_ptr(),
                                _stream_of("rope", stream, x.get_device(), y.get_device(), pos.get_device(),
                                           r.freqs.get_device())), "ods_rope_rows")
     return y
 
 
+class SharedPrefix:
+    """Groups of a batch's sequences that share the pages of a prefix (ods_shared): group g is sequences
+    group_off[g] .. group_off[g + 1] - 1, whose tables name the same pages for their first tokens[g] tokens. Device int32
+    [groups + 1] and [groups]; KvPages.shared() finds them. Both may be rewritten between calls; their lengths stay."""
+
+    def __init__(self, group_off: torch.Tensor, tokens: torch.Tensor):
+        if group_off.dtype != torch.int32 or tokens.dtype != torch.int32 or tokens.dim() != 1 or group_off.shape != (len(tokens) + 1,):
+            raise ValueError(f"SharedPrefix: int32 group_off [groups + 1] and tokens [groups], got {group_off.dtype} "
+                             f"{tuple(group_off.shape)} and {tokens.dtype} {tuple(tokens.shape)}")
+        self.group_off, self.tokens = group_off.contiguous(), tokens.contiguous()
+        self.c = ods_shared(len(tokens), _ptr(self.group_off), _ptr(self.tokens))
+        self.devices = _devices(self.group_off, self.tokens)
+
+
 class DeviceDraft:
     """ods_draft: drafted rows of a batch. row_off [B + 1] and depth [rows] int32, mask [rows, ceil(max_rows / 64)]
-    int64 (bit patterns; a 1-D tensor is one word per row). `rope`: None for the layers' own, or one Rope per layer."""
+    int64 (bit patterns; a 1-D tensor is one word per row). `rope`: None for the layers' own, or one Rope per layer.
+    `norm`: None, or one HeadNorm per layer, of whose gains the layer's q and k heads take one each. `shared`: None, or the
+    prefixes that groups of the batch's sequences share."""
 
-    def __init__(self, row_off: torch.Tensor, depth: torch.Tensor, mask: torch.Tensor, max_rows: int, rope=None):
+    def __init__(self, row_off: torch.Tensor, depth: torch.Tensor, mask: torch.Tensor, max_rows: int, rope=None, norm=None,
+                 shared: SharedPrefix | None = None):
         words = (max_rows + 63) // 64
         mask = mask if mask.dim() == 2 else mask.reshape(-1, words)
         if row_off.dtype != torch.int32 or depth.dtype != torch.int32 or mask.dtype != torch.int64:
@@ -225,9 +307,18 @@ class DeviceDraft:
         if self.rope is not None:
             table = (ods_rope * len(self.rope))(*(r.c for r in self.rope))
         self._table = table
+        self.norm, self.shared = None if norm is None else list(norm), shared
+        gains = None
+        if self.norm is not None:
+            gains = (ods_head_norm * len(self.norm))(*(n.c for n in self.norm))
+        self._gains = gains
         self.c = ods_draft(depth.shape[0], max_rows, _ptr(self.row_off), _ptr(self.depth), _ptr(self.mask),
-                           None if table is None else C.cast(table, C.POINTER(ods_rope)))
-        self.devices = _devices(self.row_off, self.depth, self.mask, *(r.freqs for r in self.rope or ()))
+                           None if table is None else C.cast(table, C.POINTER(ods_rope)),
+                           None if gains is None else C.cast(gains, C.POINTER(ods_head_norm)),
+                           None if shared is None else C.pointer(shared.c))
+        self.devices = _devices(self.row_off, self.depth, self.mask, *(r.freqs for r in self.rope or ()),
+                                *(g for n in self.norm or () for g in (n.gain_q, n.gain_k)),
+                                *((shared.group_off, shared.tokens) if shared is not None else ()))
 
     @property
     def rows(self) -> int:
@@ -241,6 +332,11 @@ class DeviceDraft:
             raise ValueError(f"DeviceDraft: ctx_lens {tuple(batch.ctx_lens.shape)} for a batch of {batch.batch}")
         if self.rope is not None and len(self.rope) != len(block.cfgs):
             raise ValueError(f"DeviceDraft: {len(self.rope)} ropes for {len(block.cfgs)} layers")
+        if self.norm is not None and len(self.norm) != len(block.cfgs):
+            raise ValueError(f"DeviceDraft: {len(self.norm)} norms for {len(block.cfgs)} layers")
+        for n, cfg in zip(self.norm or (), block.cfgs):
+            if n.head_dim != cfg.head_dim:
+                raise ValueError(f"DeviceDraft: a norm of heads of {n.head_dim} for a layer's of {cfg.head_dim}")
 
 
 class DeviceState:
@@ -466,6 +562,15 @@ class KvPages:
         _b._check(_b.ods_pages_release(self.c, self.table[row]), "ods_pages_release")
         self.tokens[row] = 0
 
+    def shared(self) -> tuple:
+        """Groups of adjacent rows that share leading pages: (group_off [groups + 1], tokens [groups]) int32 numpy, for
+        SharedPrefix (ods_pages_shared)."""
+        rows = len(self.tokens)
+        off, tokens = np.zeros(rows + 1, np.int32), np.zeros(max(rows, 1), np.int32)
+        st, n = _b.ods_pages_shared(self.table, self.tokens, off, tokens)
+        _b._check(st, "ods_pages_shared")
+        return off[:n + 1].copy(), tokens[:n].copy()
+
     def compact(self, max_pairs: int | None = None) -> int:
         """Move the highest held pages into the lowest free ones; returns how many."""
         n = int(self.c.pool_pages) if max_pairs is None else max_pairs
@@ -480,3 +585,53 @@ class KvPages:
         out = [np.array(c, np.int32).reshape(-1, 2) for c in self._copies]
         self._copies = []
         return out
+
+
+# ---------------------------------------------------------------- verification of drafted tokens
+
+class DraftVerifier:
+    """Accepted paths of drafted tokens and the tokens after them (ods_draft_verify), for batches of up to `batch`
+    sequences: `path` [batch, path_cols], `path_len` [batch] (what kv_accept takes) and `next` [batch], int32, with the
+    workspace of a vocabulary. A run writes the rows of its batch; runs on one verifier are ordered by the caller."""
+
+    DTYPES = {torch.float32: _b.ODS_PROBS_F32, torch.bfloat16: _b.ODS_PROBS_BF16}
+
+    def __init__(self, batch: int, path_cols: int, vocab: int, device="cuda"):
+        nbytes = _b.ods_verify_workspace_bytes(batch, vocab)
+        if nbytes == 0 or not 1 <= path_cols <= _b.DRAFT_MAX_ROWS:
+            raise ValueError(f"DraftVerifier: batch {batch}, path_cols {path_cols}, vocab {vocab}")
+        self.batch, self.path_cols, self.vocab = batch, path_cols, vocab
+        self.path = torch.full((batch, path_cols), -1, dtype=torch.int32, device=device)
+        self.path_len = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.next = torch.full((batch,), -1, dtype=torch.int32, device=device)
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+    def run(self, draft: DeviceDraft, tokens: torch.Tensor, parent: torch.Tensor, target: torch.Tensor,
+            accept_u: torch.Tensor, next_u: torch.Tensor, proposal: torch.Tensor | None = None,
+            stream: int | None = None) -> None:
+        """tokens, parent int32 [rows]; target and proposal [rows, vocab] probabilities, fp32 or bf16, rows at any stride
+        (proposal None: the tokens are guesses); accept_u [rows] and next_u [batch of this call] fp32 in [0, 1)."""
+        rows, B = draft.rows, draft.row_off.shape[0] - 1
+        if B > self.batch:
+            raise ValueError(f"DraftVerifier: {B} sequences, made for {self.batch}")
+        for name, t, dtype, shape in (("tokens", tokens, torch.int32, (rows,)), ("parent", parent, torch.int32, (rows,)),
+                                      ("accept_u", accept_u, torch.float32, (rows,)), ("next_u", next_u, torch.float32, (B,))):
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+                raise ValueError(f"DraftVerifier: {name} must be contiguous {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+        for name, t in (("target", target), ("proposal", proposal)):
+            if t is None:
+                continue
+            if t.dtype not in self.DTYPES or t.dtype != target.dtype or t.dim() != 2 or t.shape != target.shape or t.shape[0] != rows:
+                raise ValueError(f"DraftVerifier: {name} is fp32 or bf16 [{rows}, vocab], target and proposal alike, got "
+                                 f"{t.dtype} {tuple(t.shape)}")
+            if t.stride(1) != 1 and t.shape[1] > 1:
+                raise ValueError(f"DraftVerifier: the values of a row of {name} must be contiguous")
+        vocab = target.shape[1]
+        if not 1 <= vocab <= self.vocab:
+            raise ValueError(f"DraftVerifier: {vocab} tokens, made for {self.vocab}")
+        stride = lambda t: 0 if t is None else max(t.stride(0), vocab) if rows <= 1 else t.stride(0)  # noqa: E731
+        v = ods_verify(vocab, self.DTYPES[target.dtype], _ptr(target), stride(target), _ptr(proposal), stride(proposal),
+                       _ptr(tokens), _ptr(parent), _ptr(accept_u), _ptr(next_u), self.path_cols, _ptr(self.path),
+                       _ptr(self.path_len), _ptr(self.next), _ptr(self.ws), self.ws.numel())
+        on = _devices(draft.row_off, tokens, parent, target, proposal, accept_u, next_u, self.ws)
+        _b._check(_b.ods_draft_verify(B, draft.c, v, _stream_of("DraftVerifier", stream, *on)), "ods_draft_verify")
