@@ -445,7 +445,7 @@ ods_status ods_head_rows(const ods_rope *rope, const ods_head_norm *norm, const 
  *   n_groups   0 .. batch, at most ODS_SHARED_GROUPS
  *   group_off  device [n_groups + 1], ascending, in 0 .. batch
  *   tokens     device [n_groups] */
-#define ODS_SHARED_GROUPS 4095
+#define ODS_SHARED_GROUPS 1024
 typedef struct {
   int32_t n_groups;
   const int32_t *group_off;
@@ -560,7 +560,8 @@ ods_status ods_kv_accept(const ods_block *blk, int32_t layer_begin, int32_t laye
  * ((its rows - 1) * its common pages); only whole pages of `tokens` (host [rows],
  * each sequence's cached tokens) count. Writes group_off [rows + 1] and
  * group_tokens [rows] (their first *n_groups + 1 and *n_groups entries): together
- * the groups hold all rows, those that share nothing in groups of 0 tokens.
+ * the groups hold all rows, those that share nothing in groups of 0 tokens, or as
+ * many of the first rows as ODS_SHARED_GROUPS groups take.
  * ODS_EINVAL for null pointers, negative sizes or token counts past the table. */
 ods_status ods_pages_shared(const int32_t *table, int32_t rows, int32_t max_pages, const int32_t *tokens,
                             int32_t *group_off, int32_t *group_tokens, int32_t *n_groups);

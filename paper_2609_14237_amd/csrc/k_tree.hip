@@ -66,6 +66,50 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
     vb[(e >> log_d) * blk + (e & (D - 1)) * kPage + slot] = v[e];
 }
 
+// Sequences per launch: what LDS has room for beside the tiles. Larger batches take several launches, one after the other
+// on the same records.
+constexpr int kTreeBatch = 2048;
+
+template <int D, int NQ, int QW, bool STREAM>
+hipError_t go_tree(DraftArgs a, const TreePlan &plan, void *ws, hipStream_t s) {
+  using Shape = TreeShape<D, NQ, QW>;
+  static std::atomic<uint64_t> lds_set{0};  // devices whose LDS limit is raised
+  auto lds = [](int B) { return ((3 * (size_t)B + 1) * 4 + 15) / 16 * 16 + (size_t)Shape::kSlots * Shape::kTileBytes; };
+  const auto kern = tree_attention_kernel<D, NQ, QW, STREAM>;
+  if (hipError_t e = ensure_lds_limit((const void *)kern, lds(kTreeBatch), lds_set); e != hipSuccess) return e;
+  static_assert(sizeof(TreeDesc) <= kTreeDescBytes, "descriptor size");
+  TreeDesc *desc = (TreeDesc *)ws;
+  float2 *ml = (float2 *)((uint8_t *)ws + (size_t)kTreeDescBytes * plan.grid);
+  float *acc = (float *)(ml + (size_t)2 * plan.grid * plan.qt);
+  TreeOut out{};
+  out.rec_acc = acc;
+  out.rec_ml = ml;
+  out.desc = desc;
+  const float scale = (float)(1.4426950408889634 / sqrt((double)D));
+  const int B = a.B;
+  for (int b0 = 0; b0 < B; b0 += kTreeBatch) {
+    a.B = B - b0 < kTreeBatch ? B - b0 : kTreeBatch;
+    const int64_t tasks = (int64_t)a.B * a.n_kv * plan.max_qt;
+    const int by_task = tasks <= plan.grid, blocks = by_task ? (int)tasks : plan.grid;
+    hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * QW), lds(a.B), s, a, plan.min_tiles, plan.max_qt, by_task, (int)plan.no_cut, scale,
+                       out);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (!plan.no_cut) {
+      if (plan.split_join)
+        hipLaunchKernelGGL((tree_join_kernel<D, true>), dim3(blocks, plan.qt), dim3(256), 0, s, a, plan.qt, plan.max_qt,
+                           by_task, acc, ml, desc);
+      else
+        hipLaunchKernelGGL((tree_join_kernel<D, false>), dim3(blocks, plan.qt / 16), dim3(256), 0, s, a, plan.qt, plan.max_qt,
+                           by_task, acc, ml, desc);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    a.row_off += a.B;
+    a.ctx_lens += a.B;
+    a.table += (int64_t)a.B * a.cols;
+  }
+  return hipSuccess;
+}
+
 }  // namespace
 
 hipError_t launch_draft_rope_append(const DraftArgs &a, bool do_rope, bool do_append, hipStream_t s) {
@@ -74,7 +118,24 @@ hipError_t launch_draft_rope_append(const DraftArgs &a, bool do_rope, bool do_ap
 }
 
 hipError_t launch_tree_attention(const DraftArgs &a, const TreePlan &plan, void *ws, hipStream_t s) {
-  return plan.stream ? launch_part<kWhole, true>(a, plan, ws, TreeState{}, s) : launch_part<kWhole, false>(a, plan, ws, TreeState{}, s);
+  auto of = [&](auto d, auto stream) {
+    constexpr int D = decltype(d)::value;
+    constexpr bool STREAM = decltype(stream)::value;
+    switch (plan.qt) {
+      case 16: return go_tree<D, 16, 1, STREAM>(a, plan, ws, s);
+      case 32: return go_tree<D, 16, 2, STREAM>(a, plan, ws, s);
+      case 64: return go_tree<D, 16, 4, STREAM>(a, plan, ws, s);
+      case 128:
+        if (plan.equal) return go_tree<D, 32, 4, STREAM>(a, plan, ws, s);
+        return go_tree<D, 16, 8, STREAM>(a, plan, ws, s);
+      case 256: return go_tree<D, 32, 8, STREAM>(a, plan, ws, s);
+    }
+    return hipErrorInvalidValue;
+  };
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  if (plan.stream) return a.D == 128 ? of(D128(), std::true_type()) : of(D64(), std::true_type());
+  return a.D == 128 ? of(D128(), std::false_type()) : of(D64(), std::false_type());
 }
 
 }  // namespace ods

@@ -201,30 +201,51 @@ size_t tree_ws_bytes(const TreePlan &p, int D) {
 }
 
 SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus) {
-  SharedPlan s;
-  s.tail = tree_plan(c, batch, draft, cus);
-  // The host knows no group's rows: a tile as wide as the mean group's columns, more tiles for larger groups.
-  TreePlan &p = s.prefix;
+  SharedPlan p;
+  const TreePlan tail = tree_plan(c, batch, draft, cus);
   const int group = c.n_q / c.n_kv, groups = std::max(draft->shared->n_groups, 1);
-  const int64_t columns = (int64_t)draft->rows * group;
-  p.qt = 16;
-  while (p.qt < columns / groups && p.qt < 256) p.qt *= 2;
-  p.max_qt = 2;  // more than one: the kernel asks each group
-  const int64_t tiles = ((int64_t)batch->max_pages * ODS_PAGE_TOKENS + 31) / 32;
-  const int64_t tasks = c.n_kv * (columns / p.qt + groups), units = tasks * tiles;
-  p.units_ok = units < (int64_t)1 << 30;
+  const int64_t columns = (int64_t)draft->rows * group, nq = (int64_t)draft->max_rows * group;
+  // The host knows no group's rows: the mean group's decide.
+  p.waves = 4;
+  p.qtt = nq > 64 ? 128 : 64;
+  p.qtp = p.qtt == 128 || columns / groups > 64 ? 128 : 64;
+  if (columns / groups >= 1024 && std::max(batch->batch, groups) <= kSharedSmall) {
+    p.waves = 8;
+    p.qtp = 256;
+    p.qtt = nq > 128 ? 256 : 128;
+  }
+  p.max_qt = (int)((nq + p.qtt - 1) / p.qtt);
+  const int64_t tiles = ((int64_t)batch->max_pages * ODS_PAGE_TOKENS + 31) / 32 + 1;
+  const int64_t of_tails = (int64_t)batch->batch * c.n_kv * p.max_qt;
+  const int64_t tasks = c.n_kv * (columns / p.qtp + groups) + of_tails;
+  p.units_ok = tasks * tiles < (int64_t)1 << 30;
   p.min_tiles = 4;
-  p.equal = p.qt == 128;
-  const int per_cu = p.qt <= 16 ? 256 / c.head_dim : p.qt <= 128 ? 2 : 1;
-  p.grid = (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)std::max(cus, 1) * per_cu, (units + p.min_tiles - 1) / p.min_tiles));
-  p.stream = false;
-  p.no_cut = false;
-  p.split_join = p.grid > 6 * tasks;
-  return s;
+  const int per_cu = p.waves == 4 ? 2 : 1;
+  p.grid = (int)std::max<int64_t>(2, std::min<int64_t>((int64_t)std::max(cus, 1) * per_cu, tasks * tiles / p.min_tiles));
+  p.tile_cost = 1.f;
+  p.stream = tail.stream;
+  return p;
 }
 
-size_t shared_ws_bytes(const SharedPlan &p, int rows, int n_q, int D) {
-  return shared_state_bytes(rows, n_q, D) + std::max(tree_ws_bytes(p.prefix, D), tree_ws_bytes(p.tail, D));
+SharedWs shared_ws(const SharedPlan &p, int batch, int rows, int n_q, int n_kv, int D) {
+  SharedWs w;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 15) / 16 * 16;
+    return here;
+  };
+  for (int i = 0; i < 2; ++i) {
+    w.state[i] = take((size_t)rows * n_q * D * sizeof(float));
+    w.state_ml[i] = take((size_t)rows * n_q * 2 * sizeof(float));
+  }
+  w.prefix = take((size_t)rows * n_q * 2 * sizeof(int32_t));
+  w.desc = take((size_t)batch * n_kv * p.max_qt * kTreeDescBytes);
+  const size_t records = (size_t)2 * p.grid * std::max(p.qtp, p.qtt);
+  w.rec_ml = take(records * 2 * sizeof(float));
+  w.rec_acc = take(records * D * sizeof(float));
+  w.bytes = at;
+  return w;
 }
 
 ods_batch row_batch(const ods_batch *batch, const ods_draft *draft) {
@@ -243,7 +264,7 @@ size_t draft_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_
     const ods_layer_cfg &c = blk->layers[op.layer].cfg;
     if (op.kind != K_ATTN_CORE) continue;
     w = std::max(w, takes_shared(c, draft)
-                        ? shared_ws_bytes(shared_plan(c, batch, draft, cus), draft->rows, c.n_q, c.head_dim)
+                        ? shared_ws(shared_plan(c, batch, draft, cus), batch->batch, draft->rows, c.n_q, c.n_kv, c.head_dim).bytes
                         : tree_ws_bytes(tree_plan(c, batch, draft, cus), c.head_dim));
   }
   return w;
@@ -253,26 +274,25 @@ size_t draft_ws_most(const ods_block *blk, const ods_batch *batch, const ods_dra
   size_t w = std::max<size_t>(256, rows_ws_most(blk, draft->rows));
   for (int l = 0; l < blk->n_layers; ++l) {
     const ods_layer_cfg &c = blk->layers[l].cfg;
-    const bool shared = takes_shared(c, draft);
     size_t records = 0;
     auto take = [&](int max_rows) {
       ods_draft d = *draft;
       d.max_rows = max_rows;
       records = std::max(records, tree_ws_bytes(tree_plan(c, batch, &d, cus), c.head_dim));
     };
-    // Prefixes: the records of every tile width, on as many compute units.
-    for (int qt = 16; shared && qt <= 256; qt *= 2) {
-      TreePlan p{};
-      p.qt = qt;
-      p.grid = std::max(cus, 1) * (qt <= 16 ? 256 / c.head_dim : qt <= 128 ? 2 : 1);
-      records = std::max(records, tree_ws_bytes(p, c.head_dim));
-    }
     // A query tile's width times the grid may be more for a narrower tree, of which more workgroups share a compute unit; of
     // the trees of one width the longest needs most.
     for (int qt = 16; qt <= 256; qt *= 2)
       if (qt / (c.n_q / c.n_kv) >= 1) take(std::min(draft->max_rows, qt / (c.n_q / c.n_kv)));
     take(draft->max_rows);
-    w = std::max(w, records + (shared ? shared_state_bytes(draft->rows, c.n_q, c.head_dim) : 0));
+    w = std::max(w, records);
+    if (!takes_shared(c, draft)) continue;
+    // The most of every part: 256 columns of records for every compute unit, and as many tail tiles as the narrowest would make.
+    SharedPlan p{};
+    p.grid = 2 * std::max(cus, 1);
+    p.qtp = p.qtt = 128;
+    p.max_qt = (int)(((int64_t)draft->max_rows * (c.n_q / c.n_kv) + 63) / 64);
+    w = std::max(w, shared_ws(p, batch->batch, draft->rows, c.n_q, c.n_kv, c.head_dim).bytes);
   }
   return w;
 }
@@ -302,8 +322,8 @@ ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, con
       return set_error(ODS_EUNSUPPORTED, "layer %d: draft rows * n_q exceeds 2^31", op.layer);
     if (op.kind == K_ATTN_CORE && !tree_plan(c, batch, draft, 1).units_ok)
       return set_error(ODS_EUNSUPPORTED, "layer %d: batch * n_kv * query tiles * window pages exceeds 2^30", op.layer);
-    if (op.kind == K_ATTN_CORE && takes_shared(c, draft) && !shared_plan(c, batch, draft, 1).prefix.units_ok)
-      return set_error(ODS_EUNSUPPORTED, "layer %d: n_kv * query tiles of the groups * pages exceeds 2^30", op.layer);
+    if (op.kind == K_ATTN_CORE && takes_shared(c, draft) && !shared_plan(c, batch, draft, 1).units_ok)
+      return set_error(ODS_EUNSUPPORTED, "layer %d: n_kv * query tiles of groups and trees * pages exceeds 2^30", op.layer);
   }
   return ODS_OK;
 }

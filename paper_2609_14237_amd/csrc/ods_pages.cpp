@@ -150,7 +150,7 @@ ods_status ods_pages_shared(const int32_t *table, int32_t rows, int32_t max_page
       return set_error(ODS_EINVAL, "%s: row %d of %d tokens in %d pages", who, r, tokens[r], max_pages);
   int32_t n = 0;
   group_off[0] = 0;
-  for (int32_t r = 0; r < rows;) {
+  for (int32_t r = 0; r < rows && n < ODS_SHARED_GROUPS;) {
     const int32_t *first = table + (int64_t)r * max_pages;
     int64_t common = tokens[r] / ODS_PAGE_TOKENS;  // whole pages of the rows so far
     int32_t end = r + 1;

@@ -225,20 +225,32 @@ constexpr int kTreeDescBytes = 32;
 TreePlan tree_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus);
 size_t tree_ws_bytes(const TreePlan &p, int D);
 
-// The same where groups of sequences share a prefix: two launches, over the groups' prefixes (their query tiles are of all
-// the group's rows) and over what each sequence has beyond. Between them a state of every row and query head.
+// The same where groups of sequences share a prefix: one launch over the groups' prefixes (query tiles of all the group's
+// rows) and over what each sequence has beyond (the tail), whose results a second one joins.
 struct SharedPlan {
-  TreePlan prefix, tail;
+  int waves;        // of a workgroup: 4, or 8
+  int qtp, qtt;     // query tiles of prefixes and tails: 16 or 32 columns a wave
+  int max_qt;       // query tiles of the longest tree
+  int grid, min_tiles;
+  float tile_cost;  // time of a prefix tile, of a tail tile's
+  bool stream;      // tails are read past the caches
+  bool units_ok;
 };
+constexpr int kSharedBatch = 2048;  // sequences of a launch: what LDS has room for beside the tiles
+constexpr int kSharedSmall = 512;   // with workgroups of 8 waves, and as many groups
 // Whether a layer's attention takes the draft's groups.
 inline bool takes_shared(const ods_layer_cfg &c, const ods_draft *draft) {
   return draft->shared && draft->shared->n_groups > 0 && c.window == 0;
 }
 SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus);
-inline size_t shared_state_bytes(int rows, int n_q, int D) {  // of sums, then of (maximum, denominator)
-  return ((size_t)rows * n_q * (D + 2) * sizeof(float) + 15) / 16 * 16;
-}
-size_t shared_ws_bytes(const SharedPlan &p, int rows, int n_q, int D);
+// Where the workspace's parts are, in bytes.
+struct SharedWs {
+  size_t state[2], state_ml[2];  // of prefix and tail: sums and (maximum, denominator) of every row and query head
+  size_t prefix, desc;           // descriptors of the prefixes' query tiles and of the tail tasks
+  size_t rec_ml, rec_acc;        // two records a range
+  size_t bytes;
+};
+SharedWs shared_ws(const SharedPlan &p, int batch, int rows, int n_q, int n_kv, int D);
 
 inline bool is_kv_op(OpKind k) { return k == K_ROPE || k == K_KV_APPEND || k == K_ATTN_CORE; }
 // One step of a drafted range: a run [begin, end) of operators that only see rows (ods_run_partition on

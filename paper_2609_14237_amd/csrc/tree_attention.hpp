@@ -70,9 +70,8 @@ namespace {
 // see it) and added only to the columns that see it.
 
 // Parts: a sequence is one problem (kWhole), or two where its group shares a prefix. kPrefix: a "sequence" is a group, its
-// columns are those of all the group's drafted rows, its tokens the shared ones, none of them masked; what comes out is a
-// state per (row, query head): sums, maximum and denominator, in fp32. kTail: a sequence's tokens behind the shared ones;
-// its first piece begins with the state instead of zeros, so the join sees nothing of the prefix.
+// columns are those of all the group's drafted rows, its tokens the shared ones, none of them masked. kTail: a sequence's
+// tokens behind those its group shares. What either computes of a row and query head is joined by shared_join_kernel.
 enum TreePart { kWhole, kPrefix, kTail };
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -138,37 +137,6 @@ __device__ __forceinline__ void drop_nonfinite(uint32_t &w) {
   if ((w & 0x7f800000u) == 0x7f800000u) w &= 0x0000ffffu;
 }
 
-// Tokens that a group of sequences [s0, s1) shares: whole tiles, fewer than the table holds, and none in a group of one.
-__device__ __forceinline__ int shared_tokens(int s0, int s1, int tokens, int cols) {
-  return s1 - s0 < 2 ? 0 : max(0, min(tokens, cols * kPage - 1)) / kTile * kTile;
-}
-
-// Group g as a sequence of its shared tokens; s0: the sequence whose table it is read by.
-__device__ __forceinline__ DraftSeq group_seq(const DraftArgs &a, int g, int &s0) {
-  s0 = min(max(a.shared.group_off[g], 0), a.batch);
-  const int s1 = min(max(a.shared.group_off[g + 1], s0), a.batch);
-  const int r0 = a.row_off[s0], e = a.row_off[s1];
-  DraftSeq s;
-  s.r0 = r0;
-  s.n = r0 < 0 || r0 >= a.rows || e <= r0 ? 0 : min(e, a.rows) - r0;
-  s.ctx = s.cap = shared_tokens(s0, s1, a.shared.tokens[g], a.cols);
-  s.end = s.n == 0 ? 0 : s.ctx;
-  return s;
-}
-
-// Tokens of sequence b (of the batch) that its group's state covers; offs: group_off, in LDS.
-__device__ __forceinline__ int covered_tokens(const DraftArgs &a, const int *offs, int b, const DraftSeq &s) {
-  int g = 0, hi = a.shared.n_groups;
-  while (hi - g > 1) {
-    const int mid = (g + hi) >> 1;
-    if (offs[mid] <= b) g = mid; else hi = mid;
-  }
-  const int s0 = max(offs[g], 0), s1 = min(offs[g + 1], a.batch);
-  if (b < s0 || b >= s1) return 0;
-  const int p = shared_tokens(s0, s1, a.shared.tokens[g], a.cols);
-  return s.ctx >= p && s.end > p ? p : 0;
-}
-
 // A task that begins in a range and ends in a later one.
 struct TreeDesc {
   int pieces;      // ranges it lies in (0: none such)
@@ -176,6 +144,26 @@ struct TreeDesc {
   int r0;          // first drafted row of its sequence
   int col0, cols;  // first column of its query tile, columns of the sequence
   int head;        // KV head
+  int key;         // kTail: first column of its group's rows (of all drafted rows), -1: its group shares nothing
+};
+
+// What a workgroup knows of its sequences, in LDS.
+struct TreeSeqs {
+  int count;
+  int *pre;          // [count + 1] units before (of whole tasks: tasks before)
+  int *first, *n;    // first tile (kPrefix: the sequence whose table counts), tiles
+  int *r0, *rows;    // kPrefix: rows of the group
+  int *key;          // kTail: as TreeDesc::key
+};
+
+// Where results that are joined go.
+struct TreeOut {
+  float *rec_acc;    // records: sums [..][stride][D], maximum and denominator [..][stride]
+  float2 *rec_ml;
+  TreeDesc *desc;    // of each range, or of each task of the batch
+  float *state_acc;  // of tasks in one piece: sums [rows * n_q][D], maximum and denominator [rows * n_q]
+  float2 *state_ml;
+  int2 *prefix;      // kPrefix: (pieces, record) of a query tile, at [head][its first column of all drafted rows]
 };
 
 // Outputs of a sequence that is left alone; `threads` of them.
@@ -197,22 +185,21 @@ struct TreeShape {
   static constexpr int kPerWave = kChunks / QW;
 };
 
-// STREAM: K and V go past the caches. state_acc, state_ml [rows * n_q][D] and [rows * n_q]: written by kPrefix, read by kTail.
-template <int D, int NQ, int QW, bool STREAM, TreePart PART>
-__global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) void tree_attention_kernel(
-    const DraftArgs a, const int min_tiles, const int max_qt, const int by_task,
-    const int no_cut, const float scale_log2, float *__restrict__ rec_acc,
-    float2 *__restrict__ rec_ml, TreeDesc *__restrict__ desc, float *__restrict__ state_acc, float2 *__restrict__ state_ml) {
+// Range r of G of a launch's tasks; `block`: its number among all ranges that leave records of RS columns. The sequences of
+// kPrefix and kTail are known already, seqs.pre holding the tasks of each.
+// STREAM: K and V go past the caches.
+template <int D, int NQ, int QW, bool STREAM, TreePart PART, int RS>
+__device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &seqs, uint8_t *const slots, const int r, const int G,
+                                          const int block, const int min_tiles, const int max_qt, const int by_task,
+                                          const int no_cut, const float scale_log2, const TreeOut &out) {
   using Shape = TreeShape<D, NQ, QW>;
   constexpr int KK = D / 32, NB = D / 16, CB = NQ / 16, QT = Shape::QT;
   constexpr int NS = Shape::kSlots, LPT = Shape::kPerWave, THREADS = 64 * QW;
   constexpr int PB = kPage * D * 2;  // bytes of one page block of a head
   constexpr int DEAL = NQ == 16 ? 4 : 1;  // most whole tasks of a range; wider waves have no registers left for a list
-  extern __shared__ __align__(16) int smem[];
-  const int B = PART == kPrefix ? a.shared.n_groups : a.B, group = a.n_q / a.n_kv;
-  // of a sequence: units before, first tile (kPrefix: 0, and here the sequence whose table counts), tiles
-  int *s_pre = smem, *s_first = smem + B + 1, *s_n = s_first + B;
-  uint8_t *const slots = (uint8_t *)smem + ((3 * B + 1) * 4 + 15) / 16 * 16;
+  const int B = seqs.count, group = a.n_q / a.n_kv;
+  int *const s_pre = seqs.pre, *const s_first = seqs.first, *const s_n = seqs.n;
+  TreeDesc *const desc = out.desc;
   __shared__ int s_tot[QW][3], s_ids[THREADS], s_ord[THREADS], s_list[DEAL][4], s_most;
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -234,9 +221,8 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
     return i;
   };
 
-  const int r = blockIdx.x, G = gridDim.x;
-  if (!by_task && tid == 0) desc[r].pieces = 0;
-  if (no_cut)  // no second launch
+  if (PART == kWhole && !by_task && tid == 0) desc[r].pieces = 0;
+  if (PART == kWhole && no_cut)  // no second launch
     for (int b = r; b < B; b += G) zero_left_alone(a, b, THREADS);
   int total = 0, all_tasks = 0, most = 0, S, each;
   bool whole = false, dealt = false;  // ranges are lists of whole tasks; dealt out by length
@@ -246,23 +232,19 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
     const int per = (B + THREADS - 1) / THREADS;
     const int b0 = min(B, tid * per), b1 = min(B, b0 + per);
     int loc = 0, tasks = 0;
-    int *const offs = (int *)slots;
-    if (PART == kTail) {
-      for (int i = tid; i <= a.shared.n_groups; i += THREADS) offs[i] = a.shared.group_off[i];
-      __syncthreads();
-    }
     for (int b = b0; b < b1; ++b) {
-      int first, n, s0;
-      const DraftSeq s = PART == kPrefix ? group_seq(a, b, s0) : draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
-      tiles_of(s, a.window, first, n);
-      if (PART == kTail && n > 0) {
-        first = covered_tokens(a, offs, a.base + b, s) / kTile;
-        n -= first;
+      int first, n, of_seq;
+      if (PART == kWhole) {
+        const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
+        tiles_of(s, a.window, first, n);
+        s_first[b] = first;
+        s_n[b] = n;
+        of_seq = n == 0 ? 0 : a.n_kv * ((s.n * group + QT - 1) / QT);
+        s_pre[b] = of_seq;
+      } else {
+        n = s_n[b];
+        of_seq = s_pre[b];
       }
-      s_first[b] = PART == kPrefix ? s0 : first;
-      s_n[b] = n;
-      const int of_seq = n == 0 ? 0 : a.n_kv * ((s.n * group + QT - 1) / QT);
-      s_pre[b] = of_seq;
       loc += n * of_seq;
       tasks += of_seq;
       most = max(most, n);
@@ -326,12 +308,11 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   if (whole) {
     if (tid < each) {
       const int k = deal(r, tid), i = k < all_tasks ? find(k) : 0, b = dealt ? s_ord[i] : i;
-      int s0;
-      const DraftSeq s = PART == kPrefix ? group_seq(a, b, s0) : draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
+      const int rows = PART == kPrefix ? seqs.rows[b] : draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring).n;
       s_list[tid][0] = b;
       s_list[tid][1] = k - s_pre[i];
       s_list[tid][2] = k < all_tasks ? s_n[b] : 0;
-      s_list[tid][3] = (k - s_pre[i]) / max(1, (s.n * group + QT - 1) / QT);
+      s_list[tid][3] = (k - s_pre[i]) / max(1, (rows * group + QT - 1) / QT);
     }
     __syncthreads();
     n_w = 0;
@@ -438,7 +419,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   };
 
   // ---- the task being accumulated
-  int cb_seq, ct, c_n, c_first, c_qts, item = 0;  // sequence, task in it, its tiles; where in the list
+  int cb_seq, ct, c_n, c_first, c_qts, c_key = -1, item = 0;  // sequence, task in it, its tiles; where in the list
   int tile;                                                                          // next tile of the task
   DraftSeq seq;
   bool busy;                          // this wave has columns in it
@@ -455,16 +436,22 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   auto task_id = [&]() { return ((int64_t)cb_seq * a.n_kv + head) * max_qt + qt; };
   auto load_seq = [&]() {
     c_n = uniform(s_n[cb_seq]);
-    c_first = PART == kPrefix ? 0 : uniform(s_first[cb_seq]);
-    int s0;
-    const DraftSeq s = PART == kPrefix ? group_seq(a, cb_seq, s0)
-                                       : draft_seq((ConstInts)a.row_off, (ConstInts)a.ctx_lens, cb_seq, a.rows, a.max_rows, a.cols, a.ring);
-    seq.r0 = uniform(s.r0);
-    seq.n = uniform(s.n);
+    if (PART == kPrefix) {
+      c_first = 0;
+      seq.r0 = uniform(seqs.r0[cb_seq]);
+      seq.n = uniform(seqs.rows[cb_seq]);
+      seq.ctx = seq.end = seq.cap = c_n * kTile;
+    } else {
+      c_first = uniform(s_first[cb_seq]);
+      const DraftSeq s = draft_seq((ConstInts)a.row_off, (ConstInts)a.ctx_lens, cb_seq, a.rows, a.max_rows, a.cols, a.ring);
+      seq.r0 = uniform(s.r0);
+      seq.n = uniform(s.n);
+      seq.ctx = uniform(s.ctx);
+      seq.end = uniform(s.end);
+      seq.cap = s.cap;
+    }
+    if (PART == kTail) c_key = uniform(seqs.key[cb_seq]);
     c_qts = max_qt > 1 ? (seq.n * group + QT - 1) / QT : 1;
-    seq.ctx = uniform(s.ctx);
-    seq.end = uniform(s.end);
-    seq.cap = PART == kPrefix ? uniform(s.cap) : s.cap;
   };
   auto open_task = [&]() {
     head = max_qt > 1 ? ct / c_qts : ct;
@@ -486,14 +473,6 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
       l[cb] = 0.f;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) acc[cb][nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (PART == kTail && c_first > 0 && tile == 0) {  // on top of the shared tokens
-        const int64_t at = (int64_t)(seq.r0 + j) * a.n_q + head * group + c - j * group;
-        const float2 ml = state_ml[at];
-        m[cb] = ml.x;
-        l[cb] = rq == 0 ? ml.y : 0.f;  // close_task adds the lane quads
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) acc[cb][nb] = *(const f32x4 *)(state_acc + at * D + nb * 16 + rq * 4);
-      }
     }
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) p[cb] = u32x4{0u, 0u, 0u, 0u};  // the first products add nothing
@@ -506,7 +485,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   // Output or record of the task's piece [seg_first, last tile so far]; `whole`: the piece is all of the task.
   auto close_task = [&](bool whole) {
     const int cols = seq.n * group;
-    const int rec = 2 * r + (first_piece ? 0 : 1);
+    const int rec = 2 * block + (first_piece ? 0 : 1);
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       float sum = l[cb];
@@ -515,11 +494,11 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
       const int at = col0 + cb * 16 + hl, c = qt * QT + at;
       if (c >= cols) continue;
       const int j = row_of(c);
-      if (PART == kPrefix && whole) {
+      if (whole && (PART == kPrefix || (PART == kTail && c_key >= 0))) {
         const int64_t to = (int64_t)(seq.r0 + j) * a.n_q + head * group + c - j * group;
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(state_acc + to * D + nb * 16 + rq * 4) = acc[cb][nb];
-        if (rq == 0) state_ml[to] = make_float2(m[cb], sum);
+        for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(out.state_acc + to * D + nb * 16 + rq * 4) = acc[cb][nb];
+        if (rq == 0) out.state_ml[to] = make_float2(m[cb], sum);
       } else if (whole) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         uint16_t *dst = a.o + ((int64_t)(seq.r0 + j) * a.n_q + head * group + c - j * group) * D + rq * 4;
@@ -531,12 +510,21 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
           *(u32x2 *)(dst + nb * 16) = w;
         }
       } else {
-        float *dst = rec_acc + ((int64_t)rec * QT + at) * D + rq * 4;
+        float *dst = out.rec_acc + ((int64_t)rec * RS + at) * D + rq * 4;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(dst + nb * 16) = acc[cb][nb];
-        if (rq == 0) rec_ml[(int64_t)rec * QT + at] = make_float2(m[cb], sum);
+        if (rq == 0) out.rec_ml[(int64_t)rec * RS + at] = make_float2(m[cb], sum);
       }
     }
+  };
+
+  // The task that began in this range lies in `pieces` ranges. By one thread.
+  auto describe = [&](int pieces) {
+    const int rec = 2 * block + (first_piece ? 0 : 1);
+    if (PART == kPrefix)
+      out.prefix[((int64_t)head * a.rows + seq.r0) * group + qt * QT] = make_int2(pieces, rec);
+    else
+      desc[PART == kTail || by_task ? task_id() : r] = TreeDesc{pieces, rec, seq.r0, qt * QT, seq.n * group, head, c_key};
   };
 
   // ---- the phases of a tile
@@ -797,7 +785,11 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
       if (PING && wave < 4) meet(All(), true);  // the halves change tasks together
       if (QW > 1) values(std::false_type(), nullptr);
       close_task(seg_first == 0);
-      if (by_task && tid == 0 && seg_first == 0) desc[task_id()].pieces = 1;
+      if (PART == kWhole) {
+        if (by_task && tid == 0 && seg_first == 0) desc[task_id()].pieces = 1;
+      } else if (tid == 0 && seg_first == 0) {
+        describe(1);
+      }
       first_piece = false;
       tile = 0;
       if (t < n_w) {
@@ -826,10 +818,23 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
     close_task(false);
     if (tid == 0 && seg_first == 0) {  // ... that began in it: this range names the records to join
       const int begin = uniform(s_pre[cb_seq]) + ct * c_n, end = begin + c_n;
-      desc[by_task ? task_id() : r] =
-          TreeDesc{(end - 1) / S - r + 1, 2 * r + (first_piece ? 0 : 1), seq.r0, qt * QT, seq.n * group, head};
+      describe((end - 1) / S - r + 1);
     }
   }
+}
+
+template <int D, int NQ, int QW, bool STREAM>
+__global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) void tree_attention_kernel(
+    const DraftArgs a, const int min_tiles, const int max_qt, const int by_task, const int no_cut, const float scale_log2,
+    const TreeOut out) {
+  extern __shared__ __align__(16) int smem[];
+  TreeSeqs seqs{};
+  seqs.count = a.B;
+  seqs.pre = smem;  // units before, first tile, tiles of a sequence
+  seqs.first = smem + a.B + 1;
+  seqs.n = seqs.first + a.B;
+  tree_work<D, NQ, QW, STREAM, kWhole, NQ * QW>(a, seqs, (uint8_t *)smem + ((3 * a.B + 1) * 4 + 15) / 16 * 16, blockIdx.x, gridDim.x,
+                                                blockIdx.x, min_tiles, max_qt, by_task, no_cut, scale_log2, out);
 }
 
 // Joins the records of tasks that lie in several ranges: o[d] = sum_i
@@ -840,13 +845,11 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
 // (many tasks of two or three). Block x is task x of the batch, or, where there
 // are more tasks than ranges, the task that begins in range x. Also writes the
 // zeros of sequences that are left alone.
-// PREFIX: the joined sums are a state, not yet divided.
-template <int D, bool SPLIT, bool PREFIX>
+template <int D, bool SPLIT>
 __global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const int QT, const int max_qt, const int by_task,
                                                         const float *__restrict__ rec_acc,
                                                         const float2 *__restrict__ rec_ml,
-                                                        const TreeDesc *__restrict__ desc, float *__restrict__ state_acc,
-                                                        float2 *__restrict__ state_ml) {
+                                                        const TreeDesc *__restrict__ desc) {
   constexpr int LPR = D / 4, RPW = kWave / LPR;                 // lanes per record, records a wave reads at once
   constexpr int NC = SPLIT ? 1 : 4, G = SPLIT ? 4 * RPW : RPW;  // columns of a wave, records of a column at once
   constexpr int PRE = SPLIT ? 4 : 2;                            // trips in flight
@@ -854,7 +857,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int group = a.n_q / a.n_kv;
   const TreeDesc e = desc[blockIdx.x];
-  bool zero = !PREFIX && blockIdx.y == 0;
+  bool zero = blockIdx.y == 0;
   int b0 = blockIdx.x, step = gridDim.x;
   if (by_task) {  // the descriptor of a task without units was not written
     b0 = blockIdx.x / (a.n_kv * max_qt);
@@ -942,91 +945,12 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const DraftArgs a, const
     }
     const int col = e.col0 + at0 + c;
     if (lane >= LPR || col >= e.cols) continue;
-    if (PREFIX) {
-      const int64_t to = (int64_t)(e.r0 + col / group) * a.n_q + e.head * group + col % group;
-      *(f32x4 *)(state_acc + to * D + d) = v;
-      if (d == 0) state_ml[to] = make_float2(top, l);
-      continue;
-    }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     u32x2 out;
     out[0] = pack_pair(v[0] * inv, v[1] * inv);
     out[1] = pack_pair(v[2] * inv, v[3] * inv);
     *(u32x2 *)(a.o + ((int64_t)(e.r0 + col / group) * a.n_q + e.head * group + col % group) * D + d) = out;
   }
-}
-
-// Sequences per launch: what LDS has room for beside the tiles. Larger batches take several launches, one after the other
-// on the same records.
-constexpr int kTreeBatch = 2048;
-
-// Workspace of a launch: descriptors, then records, as tree_ws_bytes counts them.
-struct TreeState {
-  float *acc;
-  float2 *ml;
-};
-
-template <int D, int NQ, int QW, bool STREAM, TreePart PART>
-hipError_t go_tree(DraftArgs a, const TreePlan &plan, void *ws, const TreeState &state, hipStream_t s) {
-  using Shape = TreeShape<D, NQ, QW>;
-  static std::atomic<uint64_t> lds_set{0};  // devices whose LDS limit is raised
-  auto lds = [](int B) { return ((3 * (size_t)B + 1) * 4 + 15) / 16 * 16 + (size_t)Shape::kSlots * Shape::kTileBytes; };
-  static_assert(PART != kTail || Shape::kSlots * Shape::kTileBytes >= (ODS_SHARED_GROUPS + 1) * 4, "group offsets in the tiles' place");
-  const auto kern = tree_attention_kernel<D, NQ, QW, STREAM, PART>;
-  if (hipError_t e = ensure_lds_limit((const void *)kern, lds(kTreeBatch), lds_set); e != hipSuccess) return e;
-  static_assert(sizeof(TreeDesc) <= kTreeDescBytes, "descriptor size");
-  TreeDesc *desc = (TreeDesc *)ws;
-  float2 *ml = (float2 *)((uint8_t *)ws + (size_t)kTreeDescBytes * plan.grid);
-  float *acc = (float *)(ml + (size_t)2 * plan.grid * plan.qt);
-  const float scale = (float)(1.4426950408889634 / sqrt((double)D));
-  const int all = PART == kPrefix ? a.shared.n_groups : a.B;
-  for (int b0 = 0; b0 < all; b0 += kTreeBatch) {
-    const int n = all - b0 < kTreeBatch ? all - b0 : kTreeBatch;
-    (PART == kPrefix ? a.shared.n_groups : a.B) = n;
-    a.base = b0;
-    const int64_t tasks = (int64_t)n * a.n_kv * plan.max_qt;
-    const int by_task = PART != kPrefix && tasks <= plan.grid, blocks = by_task ? (int)tasks : plan.grid;
-    hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * QW), lds(n), s, a, plan.min_tiles, plan.max_qt, by_task, (int)plan.no_cut, scale, acc,
-                       ml, desc, state.acc, state.ml);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (!plan.no_cut) {
-      if (plan.split_join)
-        hipLaunchKernelGGL((tree_join_kernel<D, true, PART == kPrefix>), dim3(blocks, plan.qt), dim3(256), 0, s, a, plan.qt,
-                           plan.max_qt, by_task, acc, ml, desc, state.acc, state.ml);
-      else
-        hipLaunchKernelGGL((tree_join_kernel<D, false, PART == kPrefix>), dim3(blocks, plan.qt / 16), dim3(256), 0, s, a, plan.qt,
-                           plan.max_qt, by_task, acc, ml, desc, state.acc, state.ml);
-      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
-    if (PART == kPrefix) {
-      a.shared.group_off += n;
-      a.shared.tokens += n;
-    } else {
-      a.row_off += n;
-      a.ctx_lens += n;
-      a.table += (int64_t)n * a.cols;
-    }
-  }
-  return hipSuccess;
-}
-
-// The shapes of a plan.
-template <TreePart PART, bool STREAM>
-hipError_t launch_part(const DraftArgs &a, const TreePlan &plan, void *ws, const TreeState &state, hipStream_t s) {
-  auto of = [&](auto d) {
-    constexpr int D = decltype(d)::value;
-    switch (plan.qt) {
-      case 16: return go_tree<D, 16, 1, STREAM, PART>(a, plan, ws, state, s);
-      case 32: return go_tree<D, 16, 2, STREAM, PART>(a, plan, ws, state, s);
-      case 64: return go_tree<D, 16, 4, STREAM, PART>(a, plan, ws, state, s);
-      case 128:
-        if (plan.equal) return go_tree<D, 32, 4, STREAM, PART>(a, plan, ws, state, s);
-        return go_tree<D, 16, 8, STREAM, PART>(a, plan, ws, state, s);
-      case 256: return go_tree<D, 32, 8, STREAM, PART>(a, plan, ws, state, s);
-    }
-    return hipErrorInvalidValue;
-  };
-  return a.D == 128 ? of(std::integral_constant<int, 128>()) : of(std::integral_constant<int, 64>());
 }
 
 }  // namespace
