@@ -445,7 +445,7 @@ ods_status ods_head_rows(const ods_rope *rope, const ods_head_norm *norm, const 
  *   n_groups   0 .. batch, at most ODS_SHARED_GROUPS
  *   group_off  device [n_groups + 1], ascending, in 0 .. batch
  *   tokens     device [n_groups] */
-#define ODS_SHARED_GROUPS 1024
+#define ODS_SHARED_GROUPS 512
 typedef struct {
   int32_t n_groups;
   const int32_t *group_off;

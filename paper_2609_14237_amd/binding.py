@@ -22,7 +22,7 @@ ODS_WEIGHTS_ROWS, ODS_WEIGHTS_TILED = 0, 1
 ODS_ROPE_PLAIN, ODS_ROPE_LINEAR, ODS_ROPE_BASE, ODS_ROPE_ROTATIONS, ODS_ROPE_INDEX = 0, 1, 2, 3, 4
 DRAFT_MAX_ROWS = 256  # ODS_DRAFT_MAX_ROWS
 ROPE_AXES = 8  # ODS_ROPE_AXES
-SHARED_GROUPS = 1024  # ODS_SHARED_GROUPS
+SHARED_GROUPS = 512  # ODS_SHARED_GROUPS
 VERIFY_MAX_VOCAB = 1 << 24  # ODS_VERIFY_MAX_VOCAB
 ODS_PROBS_F32, ODS_PROBS_BF16 = 0, 1
 

@@ -15,11 +15,13 @@ namespace {
 // LDS: five integers of a group, four of a sequence, three to end lists.
 inline size_t shared_meta_bytes(int groups, int B) { return ((5 * (size_t)groups + 4 * (size_t)B + 4) * 4 + 15) / 16 * 16; }
 
-template <int D, int NQP, int NQT, int QW, bool STREAM>
-__global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) void shared_attention_kernel(
-    const DraftArgs a, const int min_tiles, const int max_qt, const float tile_cost, const float scale_log2, const TreeOut prefix_out,
-    const TreeOut tail_out) {
-  constexpr int THREADS = 64 * QW, QTP = NQP * QW, QTT = NQT * QW, RS = QTP > QTT ? QTP : QTT;
+// A workgroup has KW waves. Prefix ranges are one workgroup's work; tail ranges of up to 32 columns (WT: waves of a range)
+// are one wave's each: with few columns a tile is a chain of latencies, and such chains side by side reach the memory's rate.
+template <int D, int NQP, int NQT, int WT, int KW>
+__global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) void shared_attention_kernel(
+    const DraftArgs a, const SharedCost cost, const int max_qt, const float scale_log2, const TreeOut prefix_out, const TreeOut tail_out) {
+  constexpr int THREADS = 64 * KW, QTP = NQP * KW, QTT = NQT * WT, RPB = KW / WT;  // RPB: tail ranges of a workgroup
+  constexpr int TILE = TreeShape<D, NQP, KW>::kTileBytes, NS = TreeShape<D, NQP, KW>::kSlots;
   extern __shared__ __align__(16) int smem[];
   const int N = a.shared.n_groups, B = a.B, group = a.n_q / a.n_kv, tid = threadIdx.x;
   TreeSeqs p{}, t{};
@@ -35,7 +37,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   t.n = t.first + B;
   t.key = t.n + B;
   uint8_t *const slots = (uint8_t *)smem + ((5 * N + 4 * B + 3) * 4 + 15) / 16 * 16;
-  __shared__ int s_units[QW][2];
+  __shared__ int s_sums[KW][4];
 
   // Groups, as far as their sequences are this launch's; the rows and tokens of the sequences.
   for (int g = tid; g <= N; g += THREADS) {
@@ -60,7 +62,7 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
     t.key[b] = s.r0;
   }
   __syncthreads();
-  int units[2] = {0, 0};
+  int sums[4] = {0, 0, 0, 0};  // units and tasks of prefixes, of tails
   for (int b = tid; b < B; b += THREADS) {
     const int rows = t.pre[b], ctx = t.first[b], end = t.n[b], r0 = t.key[b];
     int g = 0, hi = N;  // the last group that begins at b or before
@@ -76,44 +78,60 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
     t.key[b] = covered ? p.r0[g] * group : -1;
     t.n[b] = end == 0 ? 0 : (end - 1) / kTile + 1 - t.first[b];
     t.pre[b] = end == 0 ? 0 : a.n_kv * ((rows * group + QTT - 1) / QTT);
-    units[1] += t.n[b] * t.pre[b];
+    sums[2] += t.n[b] * t.pre[b];
+    sums[3] += t.pre[b];
   }
-  for (int g = tid; g < N; g += THREADS) units[0] += p.n[g] * p.pre[g];
-  for (int i = 0; i < 2; ++i) {
-    const int sum = wave_scan(units[i], [](int x, int y) { return x + y; });
-    if ((tid & 63) == 63) s_units[tid >> 6][i] = sum;
+  for (int g = tid; g < N; g += THREADS) {
+    sums[0] += p.n[g] * p.pre[g];
+    sums[1] += p.pre[g];
+  }
+  for (int i = 0; i < 4; ++i) {
+    const int sum = wave_scan(sums[i], [](int x, int y) { return x + y; });
+    if ((tid & 63) == 63) s_sums[tid >> 6][i] = sum;
   }
   __syncthreads();
-  units[0] = units[1] = 0;
-  for (int w = 0; w < QW; ++w)
-    for (int i = 0; i < 2; ++i) units[i] += s_units[w][i];
+  for (int i = 0; i < 4; ++i) {
+    sums[i] = 0;
+    for (int w = 0; w < KW; ++w) sums[i] += s_sums[w][i];
+  }
   const int G = gridDim.x, r = blockIdx.x;
-  const float cost = (float)units[0] * tile_cost, all = cost + (float)units[1];
-  int of_prefix = units[0] == 0 ? 0 : max(1, min(G - 1, (int)((float)G * cost / all + 0.5f)));
-  of_prefix = __builtin_amdgcn_readfirstlane(of_prefix);
-  if (r < of_prefix)
-    tree_work<D, NQP, QW, false, kPrefix, RS>(a, p, slots, r, of_prefix, r, min_tiles, 2, 0, 0, scale_log2, prefix_out);
-  else
-    tree_work<D, NQT, QW, STREAM, kTail, RS>(a, t, slots, r - of_prefix, G - of_prefix, r, min_tiles, max_qt, 1, 0, scale_log2, tail_out);
+  for (int b = r; b < B; b += G) {  // what no range writes: zeros of sequences left alone, tasks that are none
+    zero_left_alone(a, b, THREADS);
+    for (int i = tid; i < a.n_kv * max_qt; i += THREADS)
+      if (t.n[b] == 0 || i % max_qt >= t.pre[b] / a.n_kv) tail_out.desc[(int64_t)b * a.n_kv * max_qt + i].pieces = 0;
+  }
+  const float of_p = (float)sums[0] * cost.prefix_tile + (float)sums[1] * cost.prefix_task;
+  const float of_t = (float)sums[2] * cost.tail_tile + (float)sums[3] * cost.tail_task;
+  int split = sums[0] == 0 ? 0 : max(1, min(G - 1, (int)((float)G * of_p / (of_p + of_t) + 0.5f)));
+  split = __builtin_amdgcn_readfirstlane(split);
+  if (r < split) {
+    tree_work<D, NQP, KW, NS, false, kPrefix, 1>(a, p, slots, r, split, cost.prefix_least, cost.prefix_slack, 2, 0, 0, scale_log2, prefix_out);
+  } else {
+    constexpr int NT = NS / RPB > 0 ? NS / RPB : 1;
+    static_assert(NT * RPB * TILE <= NS * TILE, "tiles of the tail ranges");
+    const int of_wave = RPB > 1 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
+    // Tails that are read once and are more than the last-level cache holds (256 MB) go past the caches, where prefixes are to
+    // stay.
+    const bool past = max_qt == 1 && (float)sums[2] * (float)TILE > 256e6f;
+    tree_work<D, NQT, WT, NT, false, kTail, RPB>(a, t, slots, (r - split) * RPB + of_wave, (G - split) * RPB, cost.tail_least, cost.tail_slack, max_qt, 1, 0,
+                                                  scale_log2, tail_out, past);
+  }
 }
 
 // One wave per column of a tail task: the pieces of its prefix task, then its own. Bound by latency where there are few
-// columns (the descriptors, then all records at once), by memory where there are many. Also writes the zeros of sequences
-// that are left alone.
+// columns (the two descriptors, then all records at once), by memory where there are many.
 template <int D>
-__global__ __launch_bounds__(256) void shared_join_kernel(const DraftArgs a, const int qtp, const int qtt, const int stride, const int max_qt,
-                                                          const TreeOut prefix_out, const TreeOut tail_out) {
+__global__ __launch_bounds__(256) void shared_join_kernel(const DraftArgs a, const int qtp, const int qtt, const TreeOut prefix_out,
+                                                          const TreeOut tail_out) {
   constexpr int LPR = D / 4, RPW = kWave / LPR, PRE = 4;  // lanes per record, records a wave reads at once, trips in flight
-  const int lane = threadIdx.x & 63, at = blockIdx.y * 4 + (threadIdx.x >> 6);
-  const int group = a.n_q / a.n_kv, task = blockIdx.x, qt = task % max_qt, b = task / max_qt / a.n_kv;
-  const TreeDesc e = tail_out.desc[task];  // of a task without units: what an earlier call left
-  if (task % (max_qt * a.n_kv) == 0 && blockIdx.y == 0) zero_left_alone(a, b, 256);
-  const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
-  const int col = qt * qtt + at;
-  if (s.end == 0 || at >= qtt || col >= s.n * group || (e.pieces == 1 && e.key < 0)) return;
-  const int row = s.r0 + col / group, head = e.head;
+  const int lane = threadIdx.x & 63, at = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = a.n_q / a.n_kv;
+  const TreeDesc e = tail_out.desc[blockIdx.x];
+  const int col = e.col0 + at;
+  if (e.pieces == 0 || at >= qtt || col >= e.cols || (e.pieces == 1 && e.key < 0)) return;
+  const int row = e.r0 + col / group, head = e.head;
   const int64_t to = (int64_t)row * a.n_q + head * group + col % group;
-  const int rel = e.key < 0 ? 0 : s.r0 * group + col - e.key, first = rel / qtp * qtp;
+  const int rel = e.key < 0 ? 0 : e.r0 * group + col - e.key, first = rel / qtp * qtp;
   const int2 p = e.key < 0 ? make_int2(0, 0) : prefix_out.prefix[(int64_t)head * a.rows * group + e.key + first];
   const int pieces = p.x + e.pieces;
   const int d = (lane % LPR) * 4, sub = lane / LPR;
@@ -129,7 +147,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(const DraftArgs a, con
       const TreeOut &from = shared ? prefix_out : tail_out;
       const int n = shared ? p.x : e.pieces, j = shared ? i : i - p.x, rec = shared ? p.y : e.rec;
       // whole tasks left a state of the row and head; pieces a record in each of their ranges
-      const int64_t idx = n == 1 ? to : (int64_t)(j == 0 ? rec : (rec & ~1) + 2 * j) * stride + (shared ? rel - first : at);
+      const int64_t idx = n == 1 ? to : (int64_t)(j == 0 ? rec : (rec & ~1) + 2 * j) * (shared ? qtp : qtt) + (shared ? rel - first : at);
       ml[k] = (n == 1 ? from.state_ml : from.rec_ml)[idx];
       x[k] = *(const f32x4 *)((n == 1 ? from.state_acc : from.rec_acc) + idx * D + d);
     }
@@ -167,39 +185,37 @@ __global__ __launch_bounds__(256) void shared_join_kernel(const DraftArgs a, con
   *(u32x2 *)(a.o + to * D + d) = out;
 }
 
-template <int D, int NQP, int NQT, int QW, bool STREAM>
+template <int D, int NQP, int NQT, int WT, int KW>
 hipError_t go_shared(DraftArgs a, const SharedPlan &plan, void *ws, hipStream_t s) {
-  using Shape = TreeShape<D, NQP, QW>;
+  using Shape = TreeShape<D, NQP, KW>;
   static std::atomic<uint64_t> lds_set{0};  // devices whose LDS limit is raised
+  if (plan.waves != KW || plan.qtp != NQP * KW || plan.qtt != NQT * WT) return hipErrorInvalidValue;  // what the workspace is cut for
   const size_t tiles = (size_t)Shape::kSlots * Shape::kTileBytes;
-  const auto kern = shared_attention_kernel<D, NQP, NQT, QW, STREAM>;
-  const int most = QW == 8 ? kSharedSmall : kSharedBatch;
-  const size_t limit = tiles + shared_meta_bytes(QW == 8 ? kSharedSmall : ODS_SHARED_GROUPS, most);
-  if (hipError_t e = ensure_lds_limit((const void *)kern, limit, lds_set); e != hipSuccess) return e;
+  const auto kern = shared_attention_kernel<D, NQP, NQT, WT, KW>;
+  if (hipError_t e = ensure_lds_limit((const void *)kern, tiles + shared_meta_bytes(ODS_SHARED_GROUPS, kSharedBatch), lds_set); e != hipSuccess)
+    return e;
   static_assert(sizeof(TreeDesc) <= kTreeDescBytes, "descriptor size");
-  const int N = a.shared.n_groups;
   const SharedWs w = shared_ws(plan, a.batch, a.rows, a.n_q, a.n_kv, D);
-  auto at = [&](size_t offset) { return (uint8_t *)ws + offset; };
-  TreeOut prefix{}, tail{};
-  prefix.rec_acc = tail.rec_acc = (float *)at(w.rec_acc);
-  prefix.rec_ml = tail.rec_ml = (float2 *)at(w.rec_ml);
-  prefix.state_acc = (float *)at(w.state[0]);
-  tail.state_acc = (float *)at(w.state[1]);
-  prefix.state_ml = (float2 *)at(w.state_ml[0]);
-  tail.state_ml = (float2 *)at(w.state_ml[1]);
-  prefix.prefix = (int2 *)at(w.prefix);
-  tail.desc = (TreeDesc *)at(w.desc);
+  TreeOut out[2] = {};  // prefix, tail
+  for (int i = 0; i < 2; ++i) {
+    auto at = [&](size_t offset) { return (uint8_t *)ws + offset; };
+    out[i].rec_acc = (float *)at(w.rec_acc[i]);
+    out[i].rec_ml = (float2 *)at(w.rec_ml[i]);
+    out[i].state_acc = (float *)at(w.state[i]);
+    out[i].state_ml = (float2 *)at(w.state_ml[i]);
+    out[i].prefix = (int2 *)at(w.prefix);
+    out[i].desc = (TreeDesc *)at(w.desc);
+  }
   const float scale = (float)(1.4426950408889634 / sqrt((double)D));
-  const int B = a.B, stride = plan.qtp > plan.qtt ? plan.qtp : plan.qtt;
-  const int columns = a.max_rows * (a.n_q / a.n_kv) < plan.qtt ? a.max_rows * (a.n_q / a.n_kv) : plan.qtt;
-  for (int b0 = 0; b0 < B; b0 += most) {  // a group on both sides of a border is two, each of which reads the prefix
-    a.B = B - b0 < most ? B - b0 : most;
+  const int B = a.B, most = a.max_rows * (a.n_q / a.n_kv), columns = most < plan.qtt ? most : plan.qtt;
+  for (int b0 = 0; b0 < B; b0 += kSharedBatch) {  // a group on both sides of a border is two, each of which reads the prefix
+    a.B = B - b0 < kSharedBatch ? B - b0 : kSharedBatch;
     a.base = b0;
-    hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * QW), tiles + shared_meta_bytes(N, a.B), s, a, plan.min_tiles, plan.max_qt,
-                       plan.tile_cost, scale, prefix, tail);
+    hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * KW), tiles + shared_meta_bytes(a.shared.n_groups, a.B), s, a, plan.cost,
+                       plan.max_qt, scale, out[0], out[1]);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(shared_join_kernel<D>, dim3(a.B * a.n_kv * plan.max_qt, (columns + 3) / 4), dim3(256), 0, s, a, plan.qtp, plan.qtt,
-                       stride, plan.max_qt, prefix, tail);
+                       out[0], out[1]);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     a.row_off += a.B;
     a.ctx_lens += a.B;
@@ -211,18 +227,22 @@ hipError_t go_shared(DraftArgs a, const SharedPlan &plan, void *ws, hipStream_t 
 }  // namespace
 
 hipError_t launch_shared_attention(const DraftArgs &a, const SharedPlan &plan, void *ws, hipStream_t s) {
-  auto of = [&](auto d, auto stream) {
+  auto of = [&](auto d) {
     constexpr int D = decltype(d)::value;
-    constexpr bool STREAM = decltype(stream)::value;
-    if (plan.waves == 8)
-      return plan.qtt == 256 ? go_shared<D, 32, 32, 8, STREAM>(a, plan, ws, s) : go_shared<D, 32, 16, 8, STREAM>(a, plan, ws, s);
-    if (plan.qtt == 128) return go_shared<D, 32, 32, 4, STREAM>(a, plan, ws, s);
-    return plan.qtp == 128 ? go_shared<D, 32, 16, 4, STREAM>(a, plan, ws, s) : go_shared<D, 16, 16, 4, STREAM>(a, plan, ws, s);
+    if (plan.waves == 8) switch (plan.qtt) {
+        case 16: return go_shared<D, 32, 16, 1, 8>(a, plan, ws, s);
+        case 32: return go_shared<D, 32, 32, 1, 8>(a, plan, ws, s);
+        case 128: return go_shared<D, 32, 16, 8, 8>(a, plan, ws, s);
+        case 256: return go_shared<D, 32, 32, 8, 8>(a, plan, ws, s);
+      }
+    else switch (plan.qtt) {
+        case 16: return plan.qtp == 64 ? go_shared<D, 16, 16, 1, 4>(a, plan, ws, s) : go_shared<D, 32, 16, 1, 4>(a, plan, ws, s);
+        case 64: return go_shared<D, 32, 16, 4, 4>(a, plan, ws, s);
+        case 128: return go_shared<D, 32, 32, 4, 4>(a, plan, ws, s);
+      }
+    return hipErrorInvalidValue;
   };
-  using D64 = std::integral_constant<int, 64>;
-  using D128 = std::integral_constant<int, 128>;
-  if (plan.stream) return a.D == 128 ? of(D128(), std::true_type()) : of(D64(), std::true_type());
-  return a.D == 128 ? of(D128(), std::false_type()) : of(D64(), std::false_type());
+  return a.D == 128 ? of(std::integral_constant<int, 128>()) : of(std::integral_constant<int, 64>());
 }
 
 }  // namespace ods

@@ -202,28 +202,40 @@ size_t tree_ws_bytes(const TreePlan &p, int D) {
 
 SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus) {
   SharedPlan p;
-  const TreePlan tail = tree_plan(c, batch, draft, cus);
   const int group = c.n_q / c.n_kv, groups = std::max(draft->shared->n_groups, 1);
   const int64_t columns = (int64_t)draft->rows * group, nq = (int64_t)draft->max_rows * group;
-  // The host knows no group's rows: the mean group's decide.
-  p.waves = 4;
-  p.qtt = nq > 64 ? 128 : 64;
-  p.qtp = p.qtt == 128 || columns / groups > 64 ? 128 : 64;
-  if (columns / groups >= 1024 && std::max(batch->batch, groups) <= kSharedSmall) {
-    p.waves = 8;
-    p.qtp = 256;
-    p.qtt = nq > 128 ? 256 : 128;
-  }
+  // The host knows no group's rows: the mean group's decide. Workgroups of eight waves have a compute unit to themselves and
+  // share each K/V byte among 256 columns, which is fastest where the prefixes' products are nearly all there is (128
+  // sequences of 4 rows, 4096 columns, over 32768 tokens: 309 us, with four waves 379). Two of four waves overlap the products
+  // of one with the loads of the other (64 sequences over 8192 tokens, 256 columns: 38 us, with eight waves 42).
+  const int64_t mean = columns / groups;
+  p.waves = mean >= 1024 ? 8 : 4;
+  // Tails of 16 columns (32 with eight waves) are one wave's ranges; wider ones a workgroup's (seven groups, up to 32 columns,
+  // four waves: 96 us, with ranges of a wave 98).
+  if (p.waves == 8)
+    p.qtt = nq <= 16 ? 16 : nq <= 32 ? 32 : nq <= 128 ? 128 : 256;
+  else
+    p.qtt = nq <= 16 ? 16 : nq <= 64 ? 64 : 128;
+  p.qtp = p.waves == 8 ? 256 : p.qtt == 16 && mean <= 64 ? 64 : 128;
   p.max_qt = (int)((nq + p.qtt - 1) / p.qtt);
   const int64_t tiles = ((int64_t)batch->max_pages * ODS_PAGE_TOKENS + 31) / 32 + 1;
-  const int64_t of_tails = (int64_t)batch->batch * c.n_kv * p.max_qt;
-  const int64_t tasks = c.n_kv * (columns / p.qtp + groups) + of_tails;
+  const int64_t tasks = c.n_kv * (columns / p.qtp + groups) + (int64_t)batch->batch * c.n_kv * p.max_qt;
   p.units_ok = tasks * tiles < (int64_t)1 << 30;
-  p.min_tiles = 4;
-  const int per_cu = p.waves == 4 ? 2 : 1;
-  p.grid = (int)std::max<int64_t>(2, std::min<int64_t>((int64_t)std::max(cus, 1) * per_cu, tasks * tiles / p.min_tiles));
-  p.tile_cost = 1.f;
-  p.stream = tail.stream;
+  p.grid = (int)std::max<int64_t>(2, std::min<int64_t>((int64_t)std::max(cus, 1) * (p.waves == 4 ? 2 : 1), tasks * tiles / 4));
+  // Of a prefix tile, measured as what splits the grid best (64 sequences over 8192 tokens, us at 0.5, 0.75 and 0.9 of a
+  // prefix tile for a tile of eight tail waves: 42, 38 and 42; seven groups, a tile of a whole workgroup at 0.7, 1.0 and 1.3:
+  // 104, 103 and 96; eight waves, 128 sequences over 32768, at 0.3, 0.4 and 0.6: 377, 309 and 312).
+  const bool of_wave = p.qtt == 16 || (p.waves == 8 && p.qtt == 32);
+  p.cost.prefix_tile = 1.f;
+  p.cost.prefix_task = 4.f;
+  p.cost.tail_tile = p.waves == 8 ? (of_wave ? 0.4f : 0.8f) : of_wave ? 0.75f : 1.3f;
+  p.cost.tail_task = of_wave ? 0.3f : 1.f;
+  // A prefix range leaves a record of up to 66 KB (8 sequences over 2000 tokens, at least 4, 8 and 16 tiles: 23.4, 20.6 and
+  // 22.5 us), a tail range of a wave one of 8 KB (2 and 3 tiles: 20.0 and 19.1).
+  p.cost.prefix_least = 8;
+  p.cost.tail_least = of_wave ? 3 : 4;
+  p.cost.prefix_slack = 6;
+  p.cost.tail_slack = of_wave ? 1 : 8;
   return p;
 }
 
@@ -241,9 +253,11 @@ SharedWs shared_ws(const SharedPlan &p, int batch, int rows, int n_q, int n_kv, 
   }
   w.prefix = take((size_t)rows * n_q * 2 * sizeof(int32_t));
   w.desc = take((size_t)batch * n_kv * p.max_qt * kTreeDescBytes);
-  const size_t records = (size_t)2 * p.grid * std::max(p.qtp, p.qtt);
-  w.rec_ml = take(records * 2 * sizeof(float));
-  w.rec_acc = take(records * D * sizeof(float));
+  for (int i = 0; i < 2; ++i) {
+    const size_t records = (size_t)2 * p.grid * (i == 0 ? p.qtp : p.qtt <= 32 ? p.waves * p.qtt : p.qtt);
+    w.rec_ml[i] = take(records * 2 * sizeof(float));
+    w.rec_acc[i] = take(records * D * sizeof(float));
+  }
   w.bytes = at;
   return w;
 }
@@ -287,11 +301,12 @@ size_t draft_ws_most(const ods_block *blk, const ods_batch *batch, const ods_dra
     take(draft->max_rows);
     w = std::max(w, records);
     if (!takes_shared(c, draft)) continue;
-    // The most of every part: 256 columns of records for every compute unit, and as many tail tiles as the narrowest would make.
+    // The most of every part: the widest tiles, and as many of the tails' as the narrowest would make.
     SharedPlan p{};
-    p.grid = 2 * std::max(cus, 1);
-    p.qtp = p.qtt = 128;
-    p.max_qt = (int)(((int64_t)draft->max_rows * (c.n_q / c.n_kv) + 63) / 64);
+    p.grid = std::max(cus, 2);
+    p.waves = 8;
+    p.qtp = p.qtt = 256;
+    p.max_qt = (int)(((int64_t)draft->max_rows * (c.n_q / c.n_kv) + 127) / 128);
     w = std::max(w, shared_ws(p, batch->batch, draft->rows, c.n_q, c.n_kv, c.head_dim).bytes);
   }
   return w;

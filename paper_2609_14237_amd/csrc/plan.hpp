@@ -227,17 +227,21 @@ size_t tree_ws_bytes(const TreePlan &p, int D);
 
 // The same where groups of sequences share a prefix: one launch over the groups' prefixes (query tiles of all the group's
 // rows) and over what each sequence has beyond (the tail), whose results a second one joins.
+// Expected times, in one unit, of a tile of 32 tokens and of a task besides its tiles, by one workgroup; fewest tiles of a
+// range.
+struct SharedCost {
+  float prefix_tile, prefix_task, tail_tile, tail_task;
+  int prefix_least, tail_least, prefix_slack, tail_slack;
+};
 struct SharedPlan {
-  int waves;        // of a workgroup: 4, or 8
-  int qtp, qtt;     // query tiles of prefixes and tails: 16 or 32 columns a wave
-  int max_qt;       // query tiles of the longest tree
-  int grid, min_tiles;
-  float tile_cost;  // time of a prefix tile, of a tail tile's
-  bool stream;      // tails are read past the caches
+  int waves;     // of a workgroup: 4, two workgroups to a compute unit, or 8
+  int qtp, qtt;  // columns of the query tiles of prefixes (16 or 32 a wave) and of tails
+  int max_qt;    // query tiles of the longest tree
+  int grid;      // workgroups
+  SharedCost cost;
   bool units_ok;
 };
-constexpr int kSharedBatch = 2048;  // sequences of a launch: what LDS has room for beside the tiles
-constexpr int kSharedSmall = 512;   // with workgroups of 8 waves, and as many groups
+constexpr int kSharedBatch = 512;  // sequences of a launch: what LDS has room for beside the tiles and the groups
 // Whether a layer's attention takes the draft's groups.
 inline bool takes_shared(const ods_layer_cfg &c, const ods_draft *draft) {
   return draft->shared && draft->shared->n_groups > 0 && c.window == 0;
@@ -247,7 +251,7 @@ SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods
 struct SharedWs {
   size_t state[2], state_ml[2];  // of prefix and tail: sums and (maximum, denominator) of every row and query head
   size_t prefix, desc;           // descriptors of the prefixes' query tiles and of the tail tasks
-  size_t rec_ml, rec_acc;        // two records a range
+  size_t rec_ml[2], rec_acc[2];  // two records a range
   size_t bytes;
 };
 SharedWs shared_ws(const SharedPlan &p, int batch, int rows, int n_q, int n_kv, int D);

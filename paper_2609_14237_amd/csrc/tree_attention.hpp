@@ -185,25 +185,31 @@ struct TreeShape {
   static constexpr int kPerWave = kChunks / QW;
 };
 
-// Range r of G of a launch's tasks; `block`: its number among all ranges that leave records of RS columns. The sequences of
-// kPrefix and kTail are known already, seqs.pre holding the tasks of each.
-// STREAM: K and V go past the caches.
-template <int D, int NQ, int QW, bool STREAM, TreePart PART, int RS>
-__device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &seqs, uint8_t *const slots, const int r, const int G,
-                                          const int block, const int min_tiles, const int max_qt, const int by_task,
-                                          const int no_cut, const float scale_log2, const TreeOut &out) {
+// Range r of G of a launch's tasks, by QW waves. The sequences of kPrefix and kTail are known already, seqs.pre holding the
+// tasks of each. Ranges are whole tasks where the longest is at most `slack` tiles more than an even share. WPB > 1: a workgroup is that many waves of one range each (QW is 1), with tiles of their own.
+// K and V go past the caches with STREAM (kTail: with `past`).
+template <int D, int NQ, int QW, int NS, bool STREAM, TreePart PART, int WPB>
+__device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &seqs, uint8_t *const all_slots, const int r, const int G,
+                                          const int min_tiles, const int slack, const int max_qt, const int by_task, const int no_cut,
+                                          const float scale_log2, const TreeOut &out, const bool past = false) {
+  static_assert(WPB == 1 || QW == 1, "waves of a range, or ranges of a wave");
   using Shape = TreeShape<D, NQ, QW>;
   constexpr int KK = D / 32, NB = D / 16, CB = NQ / 16, QT = Shape::QT;
-  constexpr int NS = Shape::kSlots, LPT = Shape::kPerWave, THREADS = 64 * QW;
+  constexpr int LPT = Shape::kPerWave, THREADS = 64 * QW * WPB;
+  constexpr bool EARLY = PART == kTail && QW == 1;  // a tile's slot is filled again as soon as the tile is in registers
   constexpr int PB = kPage * D * 2;  // bytes of one page block of a head
-  constexpr int DEAL = NQ == 16 ? 4 : 1;  // most whole tasks of a range; wider waves have no registers left for a list
+  constexpr int DEAL = PART == kWhole && NQ == 16 ? 4 : 1;  // most whole tasks of a range; wider waves have no registers left for a list
   const int B = seqs.count, group = a.n_q / a.n_kv;
   int *const s_pre = seqs.pre, *const s_first = seqs.first, *const s_n = seqs.n;
   TreeDesc *const desc = out.desc;
-  __shared__ int s_tot[QW][3], s_ids[THREADS], s_ord[THREADS], s_list[DEAL][4], s_most;
+  __shared__ int s_tot[QW * WPB][3], s_ids[THREADS], s_ord[DEAL > 1 ? THREADS : 1], s_lists[WPB][DEAL][4], s_most;
 
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int of_block = __builtin_amdgcn_readfirstlane(tid >> 6), wave = WPB > 1 ? 0 : of_block;
+  const int at_list = WPB > 1 ? lane : tid;  // among the threads of the range
+  const bool lead = at_list == 0;
+  uint8_t *const slots = all_slots + (WPB > 1 ? of_block * NS * Shape::kTileBytes : 0);
+  auto &s_list = s_lists[WPB > 1 ? of_block : 0];
   const int hl = lane & 15, rq = lane >> 4;
   const int col0 = NQ * wave;  // this wave's columns of a query tile
   // c / group and c % group of a column, c < 2^13: exact, (c + 1/2) / group is 1/32 off an integer at least
@@ -226,6 +232,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
     for (int b = r; b < B; b += G) zero_left_alone(a, b, THREADS);
   int total = 0, all_tasks = 0, most = 0, S, each;
   bool whole = false, dealt = false;  // ranges are lists of whole tasks; dealt out by length
+  int cut = 0, tile0 = 0;             // or each is a piece of one task, of about `cut` tiles; its first tile
   // Task of round j of range x.
   auto deal = [&](int x, int j) { return j & 1 ? (j + 1) * G - 1 - x : j * G + x; };
   {
@@ -252,12 +259,12 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
     auto plus = [](int x, int y) { return x + y; };
     const int inc = wave_scan(loc, plus), inc_tasks = wave_scan(tasks, plus);
     most = wave_scan(most, [](int x, int y) { return max(x, y); });
-    if (lane == 63) s_tot[wave][0] = inc, s_tot[wave][1] = inc_tasks, s_tot[wave][2] = most;
+    if (lane == 63) s_tot[of_block][0] = inc, s_tot[of_block][1] = inc_tasks, s_tot[of_block][2] = most;
     __syncthreads();
     int run = inc - loc, run_tasks = inc_tasks - tasks;
     most = 0;
-    for (int w = 0; w < QW; ++w) {
-      if (w < wave) run += s_tot[w][0], run_tasks += s_tot[w][1];
+    for (int w = 0; w < QW * WPB; ++w) {
+      if (w < of_block) run += s_tot[w][0], run_tasks += s_tot[w][1];
       total += s_tot[w][0];
       all_tasks += s_tot[w][1];
       most = max(most, s_tot[w][2]);
@@ -266,7 +273,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
     all_tasks = uniform(all_tasks);
     S = max(min_tiles, (total + G - 1) / G);
     each = (all_tasks + G - 1) / G;
-    whole = each == 1 && uniform(most) <= S + kSplitTiles;  // then s_pre counts tasks, not units
+    whole = each == 1 && uniform(most) <= S + slack;  // then s_pre counts tasks, not units
     if (DEAL > 1 && each > 1 && each <= DEAL && B <= THREADS) {  // s_ord: sequences by length; s_pre: tasks before each of them
       const int n = tid < B ? s_n[tid] : 0, of_seq = tid < B ? s_pre[tid] : 0;
       s_ids[tid] = of_seq;
@@ -291,28 +298,72 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
         atomicMax(&s_most, load);
       }
       __syncthreads();
-      whole = dealt = uniform(s_most) <= S + kSplitTiles;
+      whole = dealt = uniform(s_most) <= S + slack;
       if (!dealt && tid < B) s_pre[tid] = of_seq;  // per is 1
     }
-    if (!dealt)
+    // Equal ranges end inside tasks and begin others, each change of which costs a range a few tiles' time and a second
+    // record. Prefix tasks are few and long: each is cut into pieces of its own instead, where lengths of at most `slack`
+    // tiles more make no more pieces than ranges (64 sequences over one prefix of 8192 tokens: 46 us with equal ranges, 37).
+    if (PART == kPrefix && !whole && B <= 64) {
+      const int length = S + min(lane, slack);
+      const float inv = 1.f / (float)length;
+      float ranges = 0.f;
+      for (int b = 0; b < B; ++b)  // at least the pieces of each task: the quotient is never rounded below them
+        ranges += (float)s_pre[b] * truncf((float)(s_n[b] + length - 1) * inv * 1.000001f + 0.001f);
+      const uint64_t fits = __ballot(ranges <= (float)G);
+      if (fits) cut = __shfl(length, __builtin_ctzll(fits), kWave);
+      cut = uniform(cut);
+      __syncthreads();  // s_pre is read above
+    }
+    if (PART == kPrefix && cut > 0) {  // s_pre: ranges before
+      run = 0;
+      for (int b = b0; b < b1; ++b) run += s_pre[b] * ((s_n[b] + cut - 1) / cut);
+      const int upto = wave_scan(run, plus);  // B is 64 at most: one wave's
+      run = upto - run;
       for (int b = b0; b < b1; ++b) {
-        const int of_seq = s_pre[b];
-        s_pre[b] = whole ? run_tasks : run;
-        run += s_n[b] * of_seq;
-        run_tasks += of_seq;
+        const int of_seq = s_pre[b] * ((s_n[b] + cut - 1) / cut);
+        s_pre[b] = run;
+        run += of_seq;
       }
-    if (tid == 0) s_pre[B] = whole ? all_tasks : total;
+      if (tid == min(B, THREADS) - 1) s_pre[B] = run;
+    } else {
+      if (!dealt)
+        for (int b = b0; b < b1; ++b) {
+          const int of_seq = s_pre[b];
+          s_pre[b] = whole ? run_tasks : run;
+          run += s_n[b] * of_seq;
+          run_tasks += of_seq;
+        }
+      if (tid == 0) s_pre[B] = whole ? all_tasks : total;
+    }
     __syncthreads();
   }
-  int u0 = 0, n_w;
-  if (whole) {
-    if (tid < each) {
-      const int k = deal(r, tid), i = k < all_tasks ? find(k) : 0, b = dealt ? s_ord[i] : i;
+  int u0 = 0, n_w, pieces = 0;
+  if (PART == kPrefix && cut > 0) {
+    if (r >= s_pre[B]) return;
+    const int b = find(r), n = s_n[b];
+    pieces = uniform((n + cut - 1) / cut);
+    const int each_piece = (n + pieces - 1) / pieces, off = r - s_pre[b], task = off / pieces;
+    tile0 = uniform((off - task * pieces) * each_piece);
+    n_w = uniform(min(n - tile0, each_piece));
+    whole = true;
+    each = 1;
+    if (tid == 0) {
+      s_list[0][0] = b;
+      s_list[0][1] = task;
+      s_list[0][2] = n_w;
+      s_list[0][3] = task / max(1, (seqs.rows[b] * group + QT - 1) / QT);
+    }
+    __syncthreads();
+    if (n_w <= 0) return;
+  } else if (whole) {
+    if (at_list < each) {
+      const int k = deal(r, at_list), i = k < all_tasks ? find(k) : 0, b = dealt ? s_ord[i] : i;
       const int rows = PART == kPrefix ? seqs.rows[b] : draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring).n;
-      s_list[tid][0] = b;
-      s_list[tid][1] = k - s_pre[i];
-      s_list[tid][2] = k < all_tasks ? s_n[b] : 0;
-      s_list[tid][3] = (k - s_pre[i]) / max(1, (rows * group + QT - 1) / QT);
+      s_list[at_list][0] = b;
+      s_list[at_list][1] = k - s_pre[i];
+      s_list[at_list][2] = k < all_tasks ? s_n[b] : 0;
+      s_list[at_list][3] = (k - s_pre[i]) / max(1, (rows * group + QT - 1) / QT);
     }
     __syncthreads();
     n_w = 0;
@@ -337,6 +388,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
         while (i + 1 < each && off >= s_list[i][2]) off -= s_list[i++][2];
       b = s_list[i][0];
       head = s_list[i][3];
+      if (PART == kPrefix) off += tile0;
     } else {
       b = find(u0 + t);
       const int n = s_n[b];
@@ -356,7 +408,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   // for a register would drain the tiles in flight.
   int page_cur, head_cur, head_nxt;
   bool has_nxt;
-  int *const ids = s_ids + wave * 64;
+  int *const ids = s_ids + of_block * 64;
   auto fetch_window = [&](int t0) {
     const int64_t e = entry(t0, head_nxt);
     has_nxt = e >= 0;
@@ -410,11 +462,16 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   auto issue = [&](int age) {
     ok_bits |= ok_next << (2 * age);
     uint8_t *const dst = slots + islot * Shape::kTileBytes;
-#pragma unroll
-    for (int i = 0; i < LPT; ++i)
-      __builtin_amdgcn_global_load_lds((const void *)((chunk_p1[i] ? base1 : base0) + chunk_off[i]),
-                                       (__attribute__((address_space(3))) void *)(dst + (wave * LPT + i) * 1024), 16, 0,
-                                       STREAM ? 2 : 0);  // 2: nt
+#define ODS_TILE_LOADS(aux)                                                                                            \
+  _Pragma("unroll") for (int i = 0; i < LPT; ++i)                                                                      \
+      __builtin_amdgcn_global_load_lds((const void *)((chunk_p1[i] ? base1 : base0) + chunk_off[i]),                   \
+                                       (__attribute__((address_space(3))) void *)(dst + (wave * LPT + i) * 1024), 16, 0, aux)
+    if (PART == kTail && past) {
+      ODS_TILE_LOADS(2);  // nt
+    } else {
+      ODS_TILE_LOADS(STREAM ? 2 : 0);
+    }
+#undef ODS_TILE_LOADS
     islot = islot + 1 == NS ? 0 : islot + 1;
   };
 
@@ -485,7 +542,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   // Output or record of the task's piece [seg_first, last tile so far]; `whole`: the piece is all of the task.
   auto close_task = [&](bool whole) {
     const int cols = seq.n * group;
-    const int rec = 2 * block + (first_piece ? 0 : 1);
+    const int rec = 2 * r + (first_piece ? 0 : 1);
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       float sum = l[cb];
@@ -510,17 +567,17 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
           *(u32x2 *)(dst + nb * 16) = w;
         }
       } else {
-        float *dst = out.rec_acc + ((int64_t)rec * RS + at) * D + rq * 4;
+        float *dst = out.rec_acc + ((int64_t)rec * QT + at) * D + rq * 4;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(dst + nb * 16) = acc[cb][nb];
-        if (rq == 0) out.rec_ml[(int64_t)rec * RS + at] = make_float2(m[cb], sum);
+        if (rq == 0) out.rec_ml[(int64_t)rec * QT + at] = make_float2(m[cb], sum);
       }
     }
   };
 
   // The task that began in this range lies in `pieces` ranges. By one thread.
   auto describe = [&](int pieces) {
-    const int rec = 2 * block + (first_piece ? 0 : 1);
+    const int rec = 2 * r + (first_piece ? 0 : 1);
     if (PART == kPrefix)
       out.prefix[((int64_t)head * a.rows + seq.r0) * group + qt * QT] = make_int2(pieces, rec);
     else
@@ -668,7 +725,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   if (whole) {
     cb_seq = uniform(s_list[0][0]);
     ct = uniform(s_list[0][1]);
-    tile = 0;
+    tile = tile0;
     load_seq();
   } else {
     cb_seq = uniform(find(u0));
@@ -746,17 +803,26 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
       first_keys();
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) vf[nb] = value(at_slot(slot), nb);
+      if (EARLY) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        find_pages();
+        ok_bits >>= 2;
+        issue(NS - 1);
+      }
       scores(std::false_type(), nullptr);
     }
   };
   auto to_softmax = [&](auto edge, int t0, bool ok0, bool ok1) {
-    find_pages();
-    if (QW > 1) issue(NS - 1);
-    ok_bits >>= 2;
+    if (!EARLY) {
+      find_pages();
+      if (QW > 1) issue(NS - 1);
+      ok_bits >>= 2;
+    }
     if (busy) softmax(edge, t0, ok0, ok1);
     if (QW == 1) {
       values(std::false_type(), nullptr);
-      issue(NS - 1);
+      if (!EARLY) issue(NS - 1);
     } else {
       meet(Soft(), true);
     }
@@ -786,8 +852,8 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
       if (QW > 1) values(std::false_type(), nullptr);
       close_task(seg_first == 0);
       if (PART == kWhole) {
-        if (by_task && tid == 0 && seg_first == 0) desc[task_id()].pieces = 1;
-      } else if (tid == 0 && seg_first == 0) {
+        if (by_task && lead && seg_first == 0) desc[task_id()].pieces = 1;
+      } else if (lead && seg_first == 0) {
         describe(1);
       }
       first_piece = false;
@@ -816,9 +882,9 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   if (tile > 0) {  // the range ends inside a task
     close_task(false);
-    if (tid == 0 && seg_first == 0) {  // ... that began in it: this range names the records to join
+    if (lead && seg_first == 0) {  // ... that began in it: this range names the records to join
       const int begin = uniform(s_pre[cb_seq]) + ct * c_n, end = begin + c_n;
-      describe((end - 1) / S - r + 1);
+      describe(pieces > 0 ? pieces : (end - 1) / S - r + 1);
     }
   }
 }
@@ -833,8 +899,9 @@ __global__ __launch_bounds__(64 * QW) __attribute__((amdgpu_waves_per_eu(2))) vo
   seqs.pre = smem;  // units before, first tile, tiles of a sequence
   seqs.first = smem + a.B + 1;
   seqs.n = seqs.first + a.B;
-  tree_work<D, NQ, QW, STREAM, kWhole, NQ * QW>(a, seqs, (uint8_t *)smem + ((3 * a.B + 1) * 4 + 15) / 16 * 16, blockIdx.x, gridDim.x,
-                                                blockIdx.x, min_tiles, max_qt, by_task, no_cut, scale_log2, out);
+  tree_work<D, NQ, QW, TreeShape<D, NQ, QW>::kSlots, STREAM, kWhole, 1>(a, seqs, (uint8_t *)smem + ((3 * a.B + 1) * 4 + 15) / 16 * 16,
+                                                                        blockIdx.x, gridDim.x, min_tiles, kSplitTiles, max_qt, by_task, no_cut,
+                                                                        scale_log2, out);
 }
 
 // Joins the records of tasks that lie in several ranges: o[d] = sum_i

@@ -172,8 +172,8 @@ def test_sliding_window_layers_read_their_own_windows():
 def test_many_groups_and_batches_of_several_launches():
     say("many")
     rng = np.random.default_rng(9)
-    for B, size in ((2048, 2), (4096, 4), (4095, 5)):
-        groups = [(size, 32)] * (B // size)
+    for B, size in ((1024, 2), (4096, 9), (1500, 3)):
+        groups = [(size, 32)] * (B // size)  # the last sequences may be in no group
         ctx = 32 + rng.integers(0, 20, B)
         c = Shared(groups, ctx, rng.integers(0, 3, B), n_q=2, n_kv=1, hd=64, seed=B, max_rows=2).device()
         got = c.attend()
@@ -183,7 +183,7 @@ def test_many_groups_and_batches_of_several_launches():
         # step of each, and of the probabilities
         d, most = (got.float() - plain.float()).abs(), float(c.pool.abs().max())
         assert (d <= 2 * 2.0 ** -8 * (plain.float().abs().maximum(got.float().abs()) + 33 / 32 * most)).all()
-    sub = Shared([(3, 32)] * 700, 32 + rng.integers(0, 9, 2100), [1] * 2100, n_q=2, n_kv=1, hd=64, seed=3)
+    sub = Shared([(4, 32)] * 512, 32 + rng.integers(0, 9, 2048), [1] * 2048, n_q=2, n_kv=1, hd=64, seed=3)
     sub.device()
     sub.check(sub.attend())
 
