@@ -604,7 +604,7 @@ ods_status ods_pages_shared(const int32_t *table, int32_t rows, int32_t max_page
  *   path_len, next_token  device int32 [batch]; 0 and -1 for a sequence without rows
  *   ws               at least ods_verify_workspace_bytes() bytes
  * Arrays of this struct need the alignment of their values only, ws 16 bytes. */
-#define ODS_VERIFY_MAX_VOCAB (1 << 24)
+#define ODS_VERIFY_MAX_VOCAB (1 << 20)
 typedef enum { ODS_PROBS_F32 = 0, ODS_PROBS_BF16 = 1 } ods_probs;
 
 typedef struct {

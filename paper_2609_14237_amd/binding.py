@@ -23,7 +23,7 @@ ODS_ROPE_PLAIN, ODS_ROPE_LINEAR, ODS_ROPE_BASE, ODS_ROPE_ROTATIONS, ODS_ROPE_IND
 DRAFT_MAX_ROWS = 256  # ODS_DRAFT_MAX_ROWS
 ROPE_AXES = 8  # ODS_ROPE_AXES
 SHARED_GROUPS = 512  # ODS_SHARED_GROUPS
-VERIFY_MAX_VOCAB = 1 << 24  # ODS_VERIFY_MAX_VOCAB
+VERIFY_MAX_VOCAB = 1 << 20  # ODS_VERIFY_MAX_VOCAB
 ODS_PROBS_F32, ODS_PROBS_BF16 = 0, 1
 
 BUFFERS = ("resid", "xn", "qkv", "o", "hn", "gu", "act", "logits", "topk_w", "topk_ids", "perm",

@@ -75,7 +75,8 @@ template <typename T, bool DRAWN>
 struct Rest {
   const T *p, *q;
   int k, vocab;
-  const double *z;
+  const double *z;  // LDS or global
+  const int32_t *gone;
   // Values [e, e + N); uniform k.
   template <int N>
   __device__ __forceinline__ void load(int e, double (&w)[N]) const {
@@ -90,7 +91,6 @@ struct Rest {
 #pragma unroll
     for (int i = 0; i < N; ++i) w[i] = a[i];
     if (!DRAWN) {
-      const int32_t *gone = (const int32_t *)z;
       for (int j = 0; j < k; ++j) {
         const int at = gone[j] - e;
 #pragma unroll
@@ -104,13 +104,14 @@ struct Rest {
 constexpr int kPer = kVerifyChunk / kWave;  // values of a lane in a chunk
 
 template <typename T, bool DRAWN>
-__device__ __forceinline__ Rest<T, DRAWN> rest_of(const VerifyArgs &a, int row, int k, const double *z) {
+__device__ __forceinline__ Rest<T, DRAWN> rest_of(const VerifyArgs &a, int row, int k, const double *z, const int32_t *gone) {
   Rest<T, DRAWN> r;
   r.p = (const T *)a.target + (int64_t)row * a.target_stride;
   r.q = DRAWN ? (const T *)a.proposal + (int64_t)row * a.proposal_stride : nullptr;
   r.k = k;
   r.vocab = a.vocab;
   r.z = z;
+  r.gone = gone;
   return r;
 }
 
@@ -129,17 +130,19 @@ __device__ __forceinline__ double chunk_sum(const Rest<T, DRAWN> &r, int chunk) 
   return wave_sum_f64(sum);
 }
 
-// One block per sequence. Bound by latency: a row's token and parent, their probabilities, then the tests one after the
-// other. Only a second test of drawn siblings needs the sum over the vocabulary of what the first one left.
-template <typename T, bool DRAWN>
-__global__ __launch_bounds__(256) void verify_walk_kernel(const VerifyArgs a) {
-  constexpr int M = ODS_DRAFT_MAX_ROWS;
-  __shared__ int s_token[M], s_gone_of[4][M];  // refused tokens and sums: a copy for each wave, none waits for another
+// One block per sequence, whose first wave walks: a row's token, parent and probabilities are fetched for all rows at once, a
+// test is a few operations. Bound by latency, 3 us of which are these fetches. Only a second test of drawn siblings needs the
+// sum over the vocabulary of what the first one left; the whole block makes it (200 trees of up to 10 rows, 50257 tokens:
+// with 256 threads 60 us, with 1024 22).
+template <typename T, bool DRAWN, int THREADS>
+__global__ __launch_bounds__(THREADS) void verify_walk_kernel(const VerifyArgs a) {
+  constexpr int M = ODS_DRAFT_MAX_ROWS, WAVES = THREADS / kWave;
+  __shared__ int s_token[M], s_gone[M];
   __shared__ float s_p[M], s_q[M], s_u[M];
-  __shared__ double s_z_of[4][M], s_sum[4];
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int *const s_gone = s_gone_of[wave];
-  double *const s_z = s_z_of[wave];
+  __shared__ double s_z[M], s_sum[WAVES];
+  __shared__ int s_cur, s_k, s_more;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int first = a.row_off[b], last = a.row_off[b + 1];
   const int n = first < 0 || first >= a.rows || last <= first ? 0 : min(min(last, a.rows) - first, a.max_rows);
   int32_t *path = a.path + (int64_t)b * a.path_cols;
@@ -149,91 +152,106 @@ __global__ __launch_bounds__(256) void verify_walk_kernel(const VerifyArgs a) {
       a.next_token[b] = -1;
       a.head[b].row = -1;
     }
-    for (int i = tid; i < a.path_cols; i += 256) path[i] = -1;
+    for (int i = tid; i < a.path_cols; i += THREADS) path[i] = -1;
     return;
   }
-  const T *target = (const T *)a.target + (int64_t)first * a.target_stride;
-  const T *proposal = DRAWN ? (const T *)a.proposal + (int64_t)first * a.proposal_stride : nullptr;
   int of[M / kWave];  // parents of rows lane, lane + 64, ...; -1: passed over
+  if (wave == 0) {
 #pragma unroll
-  for (int i = 0; i < M / kWave; ++i) {
-    const int j = i * kWave + lane;
-    of[i] = -1;
-    if (j == 0 || j >= n) continue;
-    const int up = a.parent[first + j], x = a.tokens[first + j];
-    if (up < 0 || up >= j || x < 0 || x >= a.vocab) continue;
-    of[i] = up;
-    if (wave != i % 4) continue;
-    s_token[j] = x;
-    s_u[j] = a.accept_u[first + j];
-    s_p[j] = prob(target + up * a.target_stride, x);
-    if (DRAWN) s_q[j] = prob(proposal + up * a.proposal_stride, x);
+    for (int i = 0; i < M / kWave; ++i) {
+      const int j = i * kWave + lane;
+      of[i] = -1;
+      if (j == 0 || j >= n) continue;
+      const int up = a.parent[first + j], x = a.tokens[first + j];
+      if (up < 0 || up >= j || x < 0 || x >= a.vocab) continue;
+      of[i] = up;
+      s_token[j] = x;
+      s_u[j] = a.accept_u[first + j];
+      s_p[j] = prob((const T *)a.target + (int64_t)(first + up) * a.target_stride, x);
+      if (DRAWN) s_q[j] = prob((const T *)a.proposal + (int64_t)(first + up) * a.proposal_stride, x);
+    }
   }
   __syncthreads();
-  // Every thread takes every step.
+  // The walk, as far as it goes without a sum: every lane of the first wave takes every step.
   int cur = 0, len = 1, k = 0, at = 0;
   double z = 1.0;
   bool stale = false;  // z is not yet the sum of what is left
   if (tid == 0) path[0] = 0;
-  while (len < a.path_cols) {
-    int j = M;  // the next child of cur behind `at`
+  for (;;) {
+    if (wave == 0) {
+      bool more = false;
+      while (len < a.path_cols) {
+        int j = M;  // the next child of cur behind `at`
 #pragma unroll
-    for (int i = M / kWave - 1; i >= 0; --i) {
-      const uint64_t m = __ballot(of[i] == cur && i * kWave + lane > at);
-      if (m) j = i * kWave + __builtin_ctzll(m);
-    }
-    if (j == M) break;
-    at = j;
-    const int x = s_token[j];
-    if (DRAWN && stale) {
-      const auto r = rest_of<T, DRAWN>(a, first + cur, k, s_z);
-      double sum = 0.0;
-      for (int e = tid * 8; e < a.vocab; e += 256 * 8) {
-        double w[8];
-        r.load(e, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += w[i];
+        for (int i = M / kWave - 1; i >= 0; --i) {
+          const uint64_t m = __ballot(of[i] == cur && i * kWave + lane > at);
+          if (m) j = i * kWave + __builtin_ctzll(m);
+        }
+        if (j == M) break;
+        if (DRAWN && stale) {
+          more = true;
+          break;
+        }
+        at = j;
+        const int x = s_token[j];
+        double w = s_p[j], least = z * (double)s_u[j];
+        if (DRAWN) {
+          for (int i = 0; i < k; ++i) w = fmax(w - s_z[i] * (double)s_q[j], 0.0);
+          least *= (double)s_q[j];
+        } else {
+          for (int i = 0; i < k; ++i)
+            if (s_gone[i] == x) w = 0.0;
+        }
+        if (w > 0.0 && least < w) {
+          if (lane == 0) path[len] = j;
+          cur = j;
+          ++len;
+          k = 0;
+          z = 1.0;
+          stale = false;
+        } else if (DRAWN) {
+          s_z[k++] = z;
+          stale = true;
+        } else {
+          s_gone[k++] = x;
+          z -= w;
+        }
       }
-      sum = wave_sum_f64(sum);
-      __syncthreads();
-      if (lane == 0) s_sum[wave] = sum;
-      __syncthreads();
-      z = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
-      stale = false;
+      if (lane == 0) {
+        s_cur = cur;
+        s_k = k;
+        s_more = more;
+      }
     }
-    double w = s_p[j], least = z * (double)s_u[j];
-    if (DRAWN) {
-      w = left_of(s_p[j], s_q[j], s_z, k);
-      least *= (double)s_q[j];
-    } else {
-      for (int i = 0; i < k; ++i)
-        if (s_gone[i] == x) w = 0.0;
+    __syncthreads();
+    if (!DRAWN || !s_more) break;
+    const auto r = rest_of<T, DRAWN>(a, first + s_cur, s_k, s_z, s_gone);
+    double mine = 0.0;
+#pragma unroll 2
+    for (int e = tid * 8; e < a.vocab; e += THREADS * 8) {
+      double w[8];
+      r.load(e, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mine += w[i];
     }
-    if (w > 0.0 && least < w) {
-      if (tid == 0) path[len] = j;
-      cur = j;
-      ++len;
-      k = 0;
-      z = 1.0;
-      stale = false;
-    } else if (DRAWN) {
-      s_z[k++] = z;
-      stale = true;
-    } else {
-      s_gone[k++] = x;
-      z -= w;
+    mine = wave_sum_f64(mine);
+    if (lane == 0) s_sum[wave] = mine;
+    __syncthreads();
+    z = 0.0;
+    for (int w = 0; w < WAVES; ++w) z += s_sum[w];
+    stale = false;
+  }
+  if (wave == 0) {
+    for (int i = len + lane; i < a.path_cols; i += kWave) path[i] = -1;
+    if (lane == 0) {
+      a.path_len[b] = len;
+      a.head[b].row = first + cur;
+      a.head[b].k = k;
     }
   }
-  __syncthreads();
-  for (int i = len + tid; i < a.path_cols; i += 256) path[i] = -1;
-  for (int i = tid; i < k; i += 256) {
+  for (int i = tid; i < s_k; i += THREADS) {
     if (DRAWN) a.list[(int64_t)b * M + i] = s_z[i];
     else ((int32_t *)(a.list + (int64_t)b * M))[i] = s_gone[i];
-  }
-  if (tid == 0) {
-    a.path_len[b] = len;
-    a.head[b].row = first + cur;
-    a.head[b].k = k;
   }
 }
 
@@ -243,7 +261,8 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs a) {
   const int b = blockIdx.y, chunk = blockIdx.x * 4 + (threadIdx.x >> 6);
   const VerifyHead h = a.head[b];
   if (h.row < 0 || chunk >= a.chunks) return;
-  const double sum = chunk_sum(rest_of<T, DRAWN>(a, h.row, h.k, a.list + (int64_t)b * ODS_DRAFT_MAX_ROWS), chunk);
+  const double *list = a.list + (int64_t)b * ODS_DRAFT_MAX_ROWS;
+  const double sum = chunk_sum(rest_of<T, DRAWN>(a, h.row, h.k, list, (const int32_t *)list), chunk);
   if ((threadIdx.x & 63) == 0) a.sums[(int64_t)b * a.chunks + chunk] = sum;
 }
 
@@ -274,7 +293,7 @@ __global__ __launch_bounds__(64) void verify_pick_kernel(const VerifyArgs a) {
   double mine = of_lane();
   if (!__any(mine > 0.0) && h.k > 0) {  // nothing is left: the target itself
     h.k = 0;
-    const auto r = rest_of<T, DRAWN>(a, h.row, 0, nullptr);
+    const auto r = rest_of<T, DRAWN>(a, h.row, 0, nullptr, nullptr);
     for (int c = 0; c < a.chunks; ++c) {
       const double s = chunk_sum(r, c);
       if (lane == 0) sums[c] = s;
@@ -309,7 +328,8 @@ __global__ __launch_bounds__(64) void verify_pick_kernel(const VerifyArgs a) {
     chunk = __shfl(any, 63 - __builtin_clzll(__ballot(any >= 0)), kWave);
     before = INFINITY;  // its last token
   }
-  const auto r = rest_of<T, DRAWN>(a, h.row, h.k, a.list + (int64_t)b * ODS_DRAFT_MAX_ROWS);
+  const double *list = a.list + (int64_t)b * ODS_DRAFT_MAX_ROWS;
+  const auto r = rest_of<T, DRAWN>(a, h.row, h.k, list, (const int32_t *)list);
   const int e0 = chunk * kVerifyChunk + lane * kPer;
   double w[kPer], sum = 0.0;
   r.load(e0, w);
@@ -334,7 +354,8 @@ __global__ __launch_bounds__(64) void verify_pick_kernel(const VerifyArgs a) {
 
 template <typename T, bool DRAWN>
 hipError_t go_verify(const VerifyArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((verify_walk_kernel<T, DRAWN>), dim3(a.B), dim3(256), 0, s, a);
+  constexpr int WALK = DRAWN ? 1024 : 64;
+  hipLaunchKernelGGL((verify_walk_kernel<T, DRAWN, WALK>), dim3(a.B), dim3(WALK), 0, s, a);
   hipLaunchKernelGGL((verify_sums_kernel<T, DRAWN>), dim3((a.chunks + 3) / 4, a.B), dim3(256), 0, s, a);
   hipLaunchKernelGGL((verify_pick_kernel<T, DRAWN>), dim3(a.B), dim3(64), 0, s, a);
   return hipGetLastError();

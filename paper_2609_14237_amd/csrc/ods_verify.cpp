@@ -1,8 +1,6 @@
-// Host side of the verification of drafted tokens: argument checks, workspace.
-// Plain C++, free of HIP calls.
+// Host side of the verification of drafted tokens: argument checks,
+// workspace. Plain C++, free of HIP calls.
 #include "plan.hpp"
-
-using namespace ods;
 
 namespace ods {
 
@@ -58,6 +56,7 @@ ods_status check_verify(int batch, const ods_draft *draft, const ods_verify *v) 
 extern "C" {
 
 size_t ods_verify_workspace_bytes(int32_t batch, int32_t vocab) {
+  using namespace ods;
   if (batch < 0 || batch > kMaxAttnBatch || vocab < 1 || vocab > ODS_VERIFY_MAX_VOCAB) return 0;
   const size_t bytes = verify_ws(batch, vocab).bytes;
   return bytes > 16 ? bytes : 16;

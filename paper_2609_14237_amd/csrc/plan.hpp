@@ -276,11 +276,12 @@ ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, con
 // Every check ods_run_draft makes before it enqueues anything.
 ods_status validate_draft(const ods_block *blk, int op_begin, int op_end, const ods_batch *batch, const ods_draft *draft,
                           const ods_state *st, int cus);
-// Arguments of ods_draft_verify, and where its workspace's parts are.
+// Arguments of ods_draft_verify, and where its workspace's parts are (bytes): per sequence 16 bytes, ODS_DRAFT_MAX_ROWS
+// doubles, a double for every chunk of the vocabulary.
 ods_status check_verify(int batch, const ods_draft *draft, const ods_verify *v);
 constexpr int kVerifyChunk = 1024;  // values of the vocabulary whose sum is kept
 struct VerifyWs {
-  size_t head, list, sums, bytes;  // offsets: per sequence 16 bytes, ODS_DRAFT_MAX_ROWS doubles, chunks doubles
+  size_t head, list, sums, bytes;
   int chunks;
 };
 VerifyWs verify_ws(int batch, int vocab);

@@ -262,7 +262,7 @@ def rope(r: Rope, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor | None =
         n_q = heads if norm is None or norm.n_q is None else norm.n_q
         if norm is not None and (norm.head_dim != r.c.head_dim or not 0 <= n_q <= heads or (n_q < heads and norm.gain_k is None)):
             raise ValueError(f"rope: a norm of heads of {norm.head_dim}, {n_q} with gain_q, for {heads} of {r.c.head_dim}")
-        on = _devices(x, y, pos, r.freqs, r.axis) + (norm.devices if norm is not None else ())
+        on = (x.get_device(), y.get_device(), pos.get_device(), r.freqs.get_device(), *(norm.devices if norm is not None else ()))
         _b._check(_b.ods_head_rows(r.c, None if norm is None else norm.c, _ptr(r.axis), r.axes, x.data_ptr(), xs, y.data_ptr(),
                                    ys, rows, n_q, heads - n_q, pos.data_ptr(), _stream_of("rope", stream, *on)),
                   "ods_head_rows")
@@ -591,8 +591,8 @@ class KvPages:
 
 class DraftVerifier:
     """Accepted paths of drafted tokens and the tokens after them (ods_draft_verify), for batches of up to `batch`
-    sequences: `path` [batch, path_cols], `path_len` [batch] (what kv_accept takes) and `next` [batch], int32, with the
-    workspace of a vocabulary. A run writes the rows of its batch; runs on one verifier are ordered by the caller."""
+    sequences over up to `vocab` tokens: `path` [batch, path_cols], `path_len` [batch] (what kv_accept takes) and `next`
+    [batch], int32, with a workspace. A run writes the rows of its batch; runs on one verifier are ordered by the caller."""
 
     DTYPES = {torch.float32: _b.ODS_PROBS_F32, torch.bfloat16: _b.ODS_PROBS_BF16}
 
@@ -605,13 +605,42 @@ class DraftVerifier:
         self.path_len = torch.zeros(batch, dtype=torch.int32, device=device)
         self.next = torch.full((batch,), -1, dtype=torch.int32, device=device)
         self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self._device = self.ws.get_device()
+        self.c = ods_verify()
+        self.c.path_cols, self.c.path, self.c.path_len = path_cols, _ptr(self.path), _ptr(self.path_len)
+        self.c.next_token, self.c.ws, self.c.ws_bytes = _ptr(self.next), _ptr(self.ws), nbytes
 
     def run(self, draft: DeviceDraft, tokens: torch.Tensor, parent: torch.Tensor, target: torch.Tensor,
             accept_u: torch.Tensor, next_u: torch.Tensor, proposal: torch.Tensor | None = None,
             stream: int | None = None) -> None:
         """tokens, parent int32 [rows]; target and proposal [rows, vocab] probabilities, fp32 or bf16, rows at any stride
         (proposal None: the tokens are guesses); accept_u [rows] and next_u [batch of this call] fp32 in [0, 1)."""
-        rows, B = draft.rows, draft.row_off.shape[0] - 1
+        c, B, rows = self.c, draft.row_off.shape[0] - 1, draft.c.rows
+        vocab = target.shape[1] if target.dim() == 2 else 0
+        # one condition for what is right, reasons afterwards: a call of a few microseconds is host work first
+        if not (B <= self.batch and 1 <= vocab <= self.vocab and target.dtype in self.DTYPES
+                and tokens.shape == parent.shape == accept_u.shape == (rows,) and next_u.shape == (B,)
+                and tokens.dtype == parent.dtype == torch.int32 and accept_u.dtype == next_u.dtype == torch.float32
+                and tokens.is_contiguous() and parent.is_contiguous() and accept_u.is_contiguous() and next_u.is_contiguous()
+                and target.shape == (rows, vocab) and (target.stride(1) == 1 or vocab == 1)
+                and (proposal is None or (proposal.shape == target.shape and proposal.dtype == target.dtype
+                                          and (proposal.stride(1) == 1 or vocab == 1)))):
+            self._refuse(rows, B, tokens, parent, target, accept_u, next_u, proposal)
+        # the stride of a single row means nothing
+        c.vocab, c.dtype, c.target = vocab, self.DTYPES[target.dtype], target.data_ptr()
+        c.target_stride = target.stride(0) if rows > 1 else vocab
+        if proposal is None:
+            c.proposal, c.proposal_stride = None, 0
+        else:
+            c.proposal, c.proposal_stride = proposal.data_ptr(), proposal.stride(0) if rows > 1 else vocab
+        c.tokens, c.parent = tokens.data_ptr(), parent.data_ptr()
+        c.accept_u, c.next_u = accept_u.data_ptr(), next_u.data_ptr()
+        stream = _stream_of("DraftVerifier", stream, self._device, draft.row_off.get_device(), tokens.get_device(), parent.get_device(),
+                            target.get_device(), accept_u.get_device(), next_u.get_device(),
+                            self._device if proposal is None else proposal.get_device())
+        _b._check(_b.ods_draft_verify(B, draft.c, c, stream), "ods_draft_verify")
+
+    def _refuse(self, rows, B, tokens, parent, target, accept_u, next_u, proposal):
         if B > self.batch:
             raise ValueError(f"DraftVerifier: {B} sequences, made for {self.batch}")
         for name, t, dtype, shape in (("tokens", tokens, torch.int32, (rows,)), ("parent", parent, torch.int32, (rows,)),
@@ -626,12 +655,4 @@ class DraftVerifier:
                                  f"{t.dtype} {tuple(t.shape)}")
             if t.stride(1) != 1 and t.shape[1] > 1:
                 raise ValueError(f"DraftVerifier: the values of a row of {name} must be contiguous")
-        vocab = target.shape[1]
-        if not 1 <= vocab <= self.vocab:
-            raise ValueError(f"DraftVerifier: {vocab} tokens, made for {self.vocab}")
-        stride = lambda t: 0 if t is None else max(t.stride(0), vocab) if rows <= 1 else t.stride(0)  # noqa: E731
-        v = ods_verify(vocab, self.DTYPES[target.dtype], _ptr(target), stride(target), _ptr(proposal), stride(proposal),
-                       _ptr(tokens), _ptr(parent), _ptr(accept_u), _ptr(next_u), self.path_cols, _ptr(self.path),
-                       _ptr(self.path_len), _ptr(self.next), _ptr(self.ws), self.ws.numel())
-        on = _devices(draft.row_off, tokens, parent, target, proposal, accept_u, next_u, self.ws)
-        _b._check(_b.ods_draft_verify(B, draft.c, v, _stream_of("DraftVerifier", stream, *on)), "ods_draft_verify")
+        raise ValueError(f"DraftVerifier: {target.shape[1]} tokens, made for {self.vocab}")

@@ -191,6 +191,14 @@ def test_what_is_no_probability_counts_as_zero():
         c.check()
 
 
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("vocab", [128000, 300007])
+def test_large_vocabularies(vocab, drawn):
+    say("large vocabulary", vocab, drawn)
+    for seed in range(3):
+        Case([4, 9], vocab, 3, drawn, seed=seed).check()
+
+
 def test_large_batches_and_a_verifier_for_more():
     say("batch")
     rng = np.random.default_rng(1)

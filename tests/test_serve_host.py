@@ -176,7 +176,7 @@ def test_python_side_refusals():
     for norm in ([], [R.HeadNorm(z(128, dt=bf), z(128, dt=bf))]):
         with pytest.raises(ValueError):
             R.run_draft(blk, 2, 5, batch, R.DeviceDraft(z(3), z(8), z(8, dt=torch.int64), max_rows=64, norm=norm), R.ods_state())
-    for args in ((0, 4, 0), (4, 0, 100), (4, 257, 100), (4097, 4, 100)):
+    for args in ((-1, 4, 5), (4097, 4, 100), (0, 4, 0), (4, 0, 100), (4, 257, 100), (4, 4, B.VERIFY_MAX_VOCAB + 1)):
         with pytest.raises(ValueError):
             R.DraftVerifier(*args, device="cpu")
     v, d = R.DraftVerifier(2, 4, 100, device="cpu"), R.DeviceDraft(z(3), z(8), z(8, dt=torch.int64), max_rows=4)
