@@ -36,11 +36,10 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
       const HeadTurn p{heads, a.n_q, D, rdim, a.freqs ? a.interleaved : 0, a.gain_q, a.gain_k, a.eps};
       auto here = [&](int) { return row; };
       auto go = [](int) { return true; };
-      turns();
       const HeadKind kind = head_kind(rdim, p.interleaved);
-      if (kind == kHalves) turn_heads<kHalves>(p, 1, here, here, go, cs, sn, exchange);
-      if (kind == kPairs) turn_heads<kPairs>(p, 1, here, here, go, cs, sn, exchange);
-      if (kind == kAny) turn_heads<kAny>(p, 1, here, here, go, cs, sn, exchange);
+      if (kind == kHalves) turn_heads<kHalves, 2>(p, 1, 256, here, here, go, cs, sn, exchange, turns);
+      if (kind == kPairs) turn_heads<kPairs, 2>(p, 1, 256, here, here, go, cs, sn, exchange, turns);
+      if (kind == kAny) turn_heads<kAny, 2>(p, 1, 256, here, here, go, cs, sn, exchange, turns);
     } else if (wide && a.interleaved) {
       turn_row<true>(row, row, heads, D, rdim, cs, sn, turns);
     } else if (wide) {

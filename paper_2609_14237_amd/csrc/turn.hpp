@@ -1,5 +1,7 @@
 // Turning the heads of one row, by the 256 threads of a block.
 #pragma once
+#include <type_traits>
+
 #include "common.hpp"
 
 namespace ods {
@@ -127,32 +129,64 @@ __host__ __device__ inline int head_lanes_log2(int items) {
   return log;
 }
 
-// Heads of `rows` rows by the 256 threads of a block; src(r) and dst(r) are a row's first value (they may be the same), go(r)
-// whether it is done at all. Row r's cosines start at cs + r * rdim / 2. exchange: 2048 floats of LDS, kAny only.
-template <int KIND, typename Src, typename Dst, typename Go>
-__device__ __forceinline__ void turn_heads(const HeadTurn &p, int rows, Src src, Dst dst, Go go, const float *cs, const float *sn,
-                                           float *exchange) {
-  constexpr int U = 2;  // items of a thread in flight
+// Sum over groups of 1 << log neighbouring lanes, in every lane of the group: partners within rows of sixteen lanes by the
+// data path of the vector unit, the two rows of 32 lanes by a shuffle.
+__device__ __forceinline__ float lanes_sum(float v, int log) {
+  auto with = [](float x, float y) { return x + y; };
+  auto moved = [](float x, auto ctrl) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  if (log > 0) v = with(v, moved(v, std::integral_constant<int, 0xb1>()));   // lane ^ 1
+  if (log > 1) v = with(v, moved(v, std::integral_constant<int, 0x4e>()));   // lane ^ 2
+  if (log > 2) v = with(v, moved(v, std::integral_constant<int, 0x141>()));  // 7 - lane of eight: the other four, alike by now
+  if (log > 3) v = with(v, moved(v, std::integral_constant<int, 0x140>()));  // 15 - lane of sixteen
+  if (log > 4) v = with(v, __shfl_xor(v, 16, kWave));
+  return v;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // one conversion for both
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
+}
+
+// Heads of `rows` rows by the NT threads of a block, U items of each in flight; src(r) and dst(r) are a row's first value
+// (they may be the same). A thread's first loads are made before `turns`, which fills cs and sn (row r's cosines start at
+// cs + r * rdim / 2) and what go(r), whether row r is done at all, looks at: its sines come under them. exchange: 8 NT floats
+// of LDS, kAny only.
+template <int KIND, int U, typename Src, typename Dst, typename Go, typename Turns>
+__device__ __forceinline__ void turn_heads(const HeadTurn &p, int rows, int NT, Src src, Dst dst, Go go, const float *cs,
+                                           const float *sn, float *exchange, Turns turns) {
   const int np = p.rdim / 2, turned = np / 8, items = head_items((HeadKind)KIND, p.D, p.rdim);
   const int log = head_lanes_log2(items), lanes = 1 << log, total = rows * p.heads << log;
-  const float inv_d = 1.f / (float)p.D;
-  for (int t0 = 0; t0 < total; t0 += 256 * U) {
-    u32x4 a[U], b[U];
+  const float inv_d = 1.f / (float)p.D, inv_heads = 1.f / (float)p.heads;
+  for (int t0 = 0; t0 < total; t0 += NT * U) {
+    u32x4 a[U], b[U], ga[U], gb[U];
     int row[U], head[U], at[U];  // at: first dim of the item, -1: none
     bool pair[U];                // kHalves: the item has mates
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int t = t0 + u * 256 + (int)threadIdx.x, h = min(t >> log, rows * p.heads - 1), i = t & (lanes - 1);
-      row[u] = h / p.heads;
+      const int t = t0 + u * NT + (int)threadIdx.x, h = min(t >> log, rows * p.heads - 1), i = t & (lanes - 1);
+      row[u] = rows == 1 ? 0 : (int)(((float)h + 0.5f) * inv_heads);  // h / heads, exact: eight rows of less than 2^13 heads (one
+                                                                      // row of more)
       head[u] = h - row[u] * p.heads;
       pair[u] = KIND == kHalves && i < turned;
-      at[u] = t >= total || i >= items || !go(row[u]) ? -1 : KIND != kHalves || i < turned ? i * 8 : p.rdim + (i - turned) * 8;
+      at[u] = t >= total || i >= items ? -1 : KIND != kHalves || i < turned ? i * 8 : p.rdim + (i - turned) * 8;
       a[u] = b[u] = u32x4{0u, 0u, 0u, 0u};
       if (at[u] < 0) continue;
       const uint16_t *x = src(row[u]) + head[u] * p.D + at[u];
       a[u] = *(const u32x4 *)x;
       if (pair[u]) b[u] = *(const u32x4 *)(x + np);
     }
+    if (p.gain_q || p.gain_k) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint16_t *g = (head[u] < p.n_q ? p.gain_q : p.gain_k) + max(at[u], 0);
+        ga[u] = *(const u32x4 *)g;
+        gb[u] = pair[u] ? *(const u32x4 *)(g + np) : ga[u];
+      }
+    }
+    if (t0 == 0) turns();
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float v[8], w[8];  // the item's values, and their mates (kHalves)
@@ -166,26 +200,30 @@ __device__ __forceinline__ void turn_heads(const HeadTurn &p, int rows, Src src,
       if (p.gain_q || p.gain_k) {
         float sum = sumsq8(a[u]);
         if (KIND == kHalves) sum += sumsq8(b[u]);
-        for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor(sum, o, kWave);
-        const float inv = rsqrtf(sum * inv_d + p.eps);
-        const uint16_t *g = (head[u] < p.n_q ? p.gain_q : p.gain_k) + max(at[u], 0);
-        const u32x4 ga = *(const u32x4 *)g;
-        const u32x4 gb = pair[u] ? *(const u32x4 *)(g + np) : ga;
+        const float inv = rsqrtf(lanes_sum(sum, log) * inv_d + p.eps);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          v[2 * k] *= inv * bf_lo(ga[k]);
-          v[2 * k + 1] *= inv * bf_hi(ga[k]);
-          w[2 * k] *= inv * bf_lo(gb[k]);
-          w[2 * k + 1] *= inv * bf_hi(gb[k]);
+          v[2 * k] *= inv * bf_lo(ga[u][k]);
+          v[2 * k + 1] *= inv * bf_hi(ga[u][k]);
+          if (KIND != kHalves) continue;
+          w[2 * k] *= inv * bf_lo(gb[u][k]);
+          w[2 * k + 1] *= inv * bf_hi(gb[u][k]);
         }
       }
       const float *c = cs + row[u] * np, *s = sn + row[u] * np;
       if (KIND == kHalves && pair[u]) {
+        float cv[8], sv[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) turn2(v[k], w[k], c[at[u] + k], s[at[u] + k]);
+        for (int k = 0; k < 8; k += 4) {
+          *(f32x4 *)(cv + k) = *(const f32x4 *)(c + at[u] + k);
+          *(f32x4 *)(sv + k) = *(const f32x4 *)(s + at[u] + k);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) turn2(v[k], w[k], cv[k], sv[k]);
       } else if (KIND == kPairs && at[u] >= 0 && at[u] < p.rdim) {
+        const f32x4 cv = *(const f32x4 *)(c + at[u] / 2), sv = *(const f32x4 *)(s + at[u] / 2);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) turn2(v[2 * k], v[2 * k + 1], c[at[u] / 2 + k], s[at[u] / 2 + k]);
+        for (int k = 0; k < 4; ++k) turn2(v[2 * k], v[2 * k + 1], cv[k], sv[k]);
       } else if (KIND == kAny) {
         float *mine = exchange + threadIdx.x * 8;
         *(f32x4 *)mine = f32x4{v[0], v[1], v[2], v[3]};
@@ -207,10 +245,10 @@ __device__ __forceinline__ void turn_heads(const HeadTurn &p, int rows, Src src,
         asm volatile("" ::: "memory");
         __builtin_amdgcn_wave_barrier();
       }
-      if (at[u] < 0) continue;
+      if (at[u] < 0 || !go(row[u])) continue;
       uint16_t *y = dst(row[u]) + head[u] * p.D + at[u];
-      *(u32x4 *)y = u32x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
-      if (pair[u]) *(u32x4 *)(y + np) = u32x4{pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7])};
+      *(u32x4 *)y = u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+      if (pair[u]) *(u32x4 *)(y + np) = u32x4{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]), pack_bf16(w[4], w[5]), pack_bf16(w[6], w[7])};
     }
   }
 }

@@ -148,6 +148,16 @@ def test_empty_calls_refusals_and_another_stream():
     assert torch.equal(got, want)
 
 
+def test_more_heads_than_a_block_divides():
+    """Rows of 2^13 heads and more, several rows, odd counts of them around the blocks'."""
+    say("wide rows")
+    for heads, rows in ((8191, 3), (8192, 3), (9001, 2), (5, 2049), (3, 4100), (40, 2050)):
+        full, pos, gq, gk = make(rows, heads, 0, 8, heads, 3000)
+        y, bound = S.heads(f64(full), pos, [0] * 4, D.freqs(8, 1e4), 8, False, f64(gq), f64(gk), heads // 3, 1e-6)
+        check(R.rope(R.Rope(8), full, torch.from_numpy(pos[:, 0].copy()).cuda(), out=torch.empty_like(full),
+                     norm=R.HeadNorm(gq, gk, n_q=heads // 3)), y, bound)
+
+
 def test_captured_and_replayed():
     say("graph")
     full, pos, gq, gk = make(20, 6, 0, 128, 4, 4000)
