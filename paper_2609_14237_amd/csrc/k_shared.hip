@@ -38,13 +38,20 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
   t.key = t.n + B;
   uint8_t *const slots = (uint8_t *)smem + ((5 * N + 4 * B + 3) * 4 + 15) / 16 * 16;
   __shared__ int s_sums[KW][4];
+  __shared__ float s_units[KW];
 
   // Groups, as far as their sequences are this launch's; the rows and tokens of the sequences.
+  // Whatever the arrays hold, the tasks counted are those of disjoint groups of no more rows than there are: offsets that
+  // descend, or rows that overlap so that their tiles pass what the launch was checked for, share nothing.
+  auto here = [&](int off) { return (int)min(max((int64_t)off - a.base, (int64_t)0), (int64_t)B); };
+  bool descends = false;
+  float tiles = 0.f;
   for (int g = tid; g <= N; g += THREADS) {
-    const int s0 = min(max(a.shared.group_off[g] - a.base, 0), B);
+    const int s0 = here(a.shared.group_off[g]);
     p.first[g] = s0;
     if (g == N) break;
-    const int s1 = min(max(a.shared.group_off[g + 1] - a.base, s0), B);
+    descends = descends || a.shared.group_off[g] > a.shared.group_off[g + 1];
+    const int s1 = max(here(a.shared.group_off[g + 1]), s0);
     // Whole tiles, fewer tokens than the table holds, and none in a group of one.
     const int tokens = s1 - s0 < 2 ? 0 : max(0, min(a.shared.tokens[g], a.cols * kPage - 1)) / kTile;
     const int r0 = a.row_off[s0], e = a.row_off[s1];
@@ -53,7 +60,10 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
     p.rows[g] = rows;
     p.n[g] = rows > 0 ? tokens : 0;
     p.pre[g] = p.n[g] > 0 ? a.n_kv * ((rows * group + QTP - 1) / QTP) : 0;
+    tiles += (float)p.n[g] * (float)p.pre[g];
   }
+  tiles = wave_sum(tiles);
+  if ((tid & 63) == 0) s_units[tid >> 6] = tiles;
   for (int b = tid; b < B; b += THREADS) {
     const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
     t.pre[b] = s.n;
@@ -61,7 +71,13 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
     t.n[b] = s.end;
     t.key[b] = s.r0;
   }
-  __syncthreads();
+  const bool none = __syncthreads_or(descends);
+  tiles = 0.f;
+  for (int w = 0; w < KW; ++w) tiles += s_units[w];
+  if (none || tiles > 1.07e9f) {  // 2^30
+    for (int g = tid; g < N; g += THREADS) p.n[g] = p.pre[g] = 0;
+    __syncthreads();
+  }
   int sums[4] = {0, 0, 0, 0};  // units and tasks of prefixes, of tails
   for (int b = tid; b < B; b += THREADS) {
     const int rows = t.pre[b], ctx = t.first[b], end = t.n[b], r0 = t.key[b];
@@ -121,7 +137,7 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
 // One wave per column of a tail task: the pieces of its prefix task, then its own. Bound by latency where there are few
 // columns (the two descriptors, then all records at once), by memory where there are many.
 template <int D>
-__global__ __launch_bounds__(256) void shared_join_kernel(const DraftArgs a, const int qtp, const int qtt, const TreeOut prefix_out,
+__global__ __launch_bounds__(256) void shared_join_kernel(const DraftArgs a, const int qtp, const int qtt, const int ranges, const TreeOut prefix_out,
                                                           const TreeOut tail_out) {
   constexpr int LPR = D / 4, RPW = kWave / LPR, PRE = 4;  // lanes per record, records a wave reads at once, trips in flight
   const int lane = threadIdx.x & 63, at = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -133,6 +149,8 @@ __global__ __launch_bounds__(256) void shared_join_kernel(const DraftArgs a, con
   const int64_t to = (int64_t)row * a.n_q + head * group + col % group;
   const int rel = e.key < 0 ? 0 : e.r0 * group + col - e.key, first = rel / qtp * qtp;
   const int2 p = e.key < 0 ? make_int2(0, 0) : prefix_out.prefix[(int64_t)head * a.rows * group + e.key + first];
+  // Records of the launch, whatever was left where a group's rows are not ascending.
+  if (p.x < 0 || p.y < 0 || (int64_t)(p.y | 1) + 2 * ((int64_t)p.x - 1) >= 2 * ranges) return;
   const int pieces = p.x + e.pieces;
   const int d = (lane % LPR) * 4, sub = lane / LPR;
   float M = kNoScore, sum = 0.f;
@@ -215,7 +233,7 @@ hipError_t go_shared(DraftArgs a, const SharedPlan &plan, void *ws, hipStream_t 
                        plan.max_qt, scale, out[0], out[1]);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     hipLaunchKernelGGL(shared_join_kernel<D>, dim3(a.B * a.n_kv * plan.max_qt, (columns + 3) / 4), dim3(256), 0, s, a, plan.qtp, plan.qtt,
-                       out[0], out[1]);
+                       plan.grid, out[0], out[1]);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     a.row_off += a.B;
     a.ctx_lens += a.B;

@@ -143,7 +143,8 @@ ods_status ods_pages_release(ods_pages *p, int32_t *row, int32_t max_pages) {
 ods_status ods_pages_shared(const int32_t *table, int32_t rows, int32_t max_pages, const int32_t *tokens,
                             int32_t *group_off, int32_t *group_tokens, int32_t *n_groups) {
   const char *who = "ods_pages_shared";
-  if (!table || !tokens || !group_off || !group_tokens || !n_groups) return set_error(ODS_EINVAL, "%s: null pointer", who);
+  if (!group_off || !group_tokens || !n_groups || (rows > 0 && (!table || !tokens)))
+    return set_error(ODS_EINVAL, "%s: null pointer", who);
   if (rows < 0 || max_pages < 1) return set_error(ODS_EINVAL, "%s: rows %d, max_pages %d", who, rows, max_pages);
   for (int32_t r = 0; r < rows; ++r)
     if (tokens[r] < 0 || pages_of(tokens[r]) > max_pages)

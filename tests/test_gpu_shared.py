@@ -160,6 +160,26 @@ def test_claims_that_pass_the_table_or_are_negative():
         c.check(c.attend())
 
 
+def test_offsets_that_do_not_ascend_share_nothing():
+    """Device arrays that break their contract are computed without a prefix (offsets that descend, or outside the batch), or
+    at least stay inside the buffers (rows that do not ascend)."""
+    say("offsets")
+    ctx = [200 + 7 * b for b in range(8)]
+    for off in ([0, 8, 0, 8, 0, 8], [5, 4, 3, 2, 1, 0], [-2 ** 31, 2 ** 31 - 1, -1, 3, 9, 8], [8, 8, 8, 2 ** 31 - 1, 9, 0]):
+        c = Shared([(8, 192)], ctx, [3] * 8, n_q=8, n_kv=2, hd=64, seed=14)
+        c.group_off, c.tokens = np.array(off, np.int64).astype(np.int32), np.full(5, 192, np.int32)
+        c.device()
+        c.check(c.attend())
+    for off in ([-7, 3, 3, 8], [0, 4, 2 ** 31 - 1, 2 ** 31 - 1], [-2 ** 31, -2 ** 31, 0, 100]):   # clipped to the batch
+        c = Shared([(8, 192)], ctx, [3] * 8, n_q=8, n_kv=2, hd=64, seed=15)
+        c.group_off, c.tokens = np.array(off, np.int64).astype(np.int32), np.full(3, 192, np.int32)
+        c.device()
+        c.check(c.attend())
+    c = Shared([(4, 192), (4, 192)], ctx, [3] * 8, n_q=8, n_kv=2, hd=64, seed=16).device()
+    c.draft.row_off.copy_(cuda(np.array([0, 24, 3, 24, 9, 12, 24, 18, 24], np.int32)))
+    c.attend()   # no more than that it ends
+
+
 def test_sliding_window_layers_read_their_own_windows():
     say("window")
     c = Shared([(4, 320)], [330, 350, 320, 400], [3, 2, 1, 5], n_q=4, n_kv=2, hd=64, window=50, seed=8).device()

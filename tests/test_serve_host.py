@@ -1,6 +1,9 @@
 """Host-side checks, without a GPU, of normalised heads, shared prefixes and the verification of drafted tokens: every
 refusal (all return before anything is enqueued), groups found in page tables, workspace sizes."""
 import ctypes as C
+import os
+import shutil
+import subprocess
 from dataclasses import replace
 
 import numpy as np
@@ -12,7 +15,7 @@ import workloads as W
 
 B = pytest.importorskip("paper_2609_14237_amd.binding")
 from paper_2609_14237_amd import runtime as R  # noqa: E402
-from test_draft_host import CFG, FAKE, fake_batch, fake_block, fake_state, rope_struct  # noqa: E402
+from test_draft_host import CFG, CXX, FAKE, ROOT, fake_batch, fake_block, fake_state, rope_struct  # noqa: E402
 
 FAR = FAKE + (1 << 20)
 
@@ -214,3 +217,18 @@ def test_the_reference_keeps_the_targets_distribution():
                 w = np.maximum(p - q, 0)
                 got += q[x] / n * w / w.sum()
     np.testing.assert_allclose(got, p, atol=1.0 / n)
+
+
+@pytest.mark.skipif(shutil.which(CXX) is None, reason="no host compiler")
+def test_host_parts_under_the_sanitizers(tmp_path):
+    src, exe = os.path.join(ROOT, "paper_2609_14237_amd", "csrc"), tmp_path / "serve_check"
+    cmd = [CXX, "-std=c++17", "-g", "-O1", "-fno-omit-frame-pointer", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+           "-D__HIP_PLATFORM_AMD__", "-I", "/opt/rocm/include", "-I", os.path.join(ROOT, "include"),
+           *(os.path.join(src, f) for f in ("ods_host.cpp", "ods_draft.cpp", "ods_pages.cpp", "ods_verify.cpp")),
+           os.path.join(ROOT, "tests", "host", "serve_check.cpp"), "-o", str(exe)]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-4000:]
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=600,
+                       env=dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1"))
+    assert r.returncode == 0, (r.stdout + r.stderr)[-4000:]
+    assert "serve_check OK" in r.stdout
