@@ -19,7 +19,7 @@ inline size_t shared_meta_bytes(int groups, int B) { return ((5 * (size_t)groups
 // are one wave's each: with few columns a tile is a chain of latencies, and such chains side by side reach the memory's rate.
 template <int D, int NQP, int NQT, int WT, int KW>
 __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) void shared_attention_kernel(
-    const DraftArgs a, const SharedCost cost, const int max_qt, const float scale_log2, const TreeOut prefix_out, const TreeOut tail_out) {
+    const DraftArgs a, const SharedCost cost, const float scale_log2, const TreeOut prefix_out, const TreeOut tail_out) {
   constexpr int THREADS = 64 * KW, QTP = NQP * KW, QTT = NQT * WT, RPB = KW / WT;  // RPB: tail ranges of a workgroup
   constexpr int TILE = TreeShape<D, NQP, KW>::kTileBytes, NS = TreeShape<D, NQP, KW>::kSlots;
   extern __shared__ __align__(16) int smem[];
@@ -113,8 +113,7 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
   const int G = gridDim.x, r = blockIdx.x;
   for (int b = r; b < B; b += G) {  // what no range writes: zeros of sequences left alone, tasks that are none
     zero_left_alone(a, b, THREADS);
-    for (int i = tid; i < a.n_kv * max_qt; i += THREADS)
-      if (t.n[b] == 0 || i % max_qt >= t.pre[b] / a.n_kv) tail_out.desc[(int64_t)b * a.n_kv * max_qt + i].pieces = 0;
+    if (t.n[b] == 0 && tid < a.n_kv) tail_out.desc[(int64_t)b * a.n_kv + tid].pieces = 0;
   }
   const float of_p = (float)sums[0] * cost.prefix_tile + (float)sums[1] * cost.prefix_task;
   const float of_t = (float)sums[2] * cost.tail_tile + (float)sums[3] * cost.tail_task;
@@ -126,10 +125,9 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
     constexpr int NT = NS / RPB > 0 ? NS / RPB : 1;
     static_assert(NT * RPB * TILE <= NS * TILE, "tiles of the tail ranges");
     const int of_wave = RPB > 1 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
-    // Tails that are read once and are more than the last-level cache holds (256 MB) go past the caches, where prefixes are to
-    // stay.
-    const bool past = max_qt == 1 && (float)sums[2] * (float)TILE > 256e6f;
-    tree_work<D, NQT, WT, NT, false, kTail, RPB>(a, t, slots, (r - split) * RPB + of_wave, (G - split) * RPB, cost.tail_least, cost.tail_slack, max_qt, 1, 0,
+    // Tails that are more than the last-level cache holds (256 MB) go past the caches, where prefixes are to stay.
+    const bool past = (float)sums[2] * (float)TILE > 256e6f;
+    tree_work<D, NQT, WT, NT, false, kTail, RPB>(a, t, slots, (r - split) * RPB + of_wave, (G - split) * RPB, cost.tail_least, cost.tail_slack, 1, 1, 0,
                                                   scale_log2, tail_out, past);
   }
 }
@@ -230,9 +228,9 @@ hipError_t go_shared(DraftArgs a, const SharedPlan &plan, void *ws, hipStream_t 
     a.B = B - b0 < kSharedBatch ? B - b0 : kSharedBatch;
     a.base = b0;
     hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * KW), tiles + shared_meta_bytes(a.shared.n_groups, a.B), s, a, plan.cost,
-                       plan.max_qt, scale, out[0], out[1]);
+                       scale, out[0], out[1]);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(shared_join_kernel<D>, dim3(a.B * a.n_kv * plan.max_qt, (columns + 3) / 4), dim3(256), 0, s, a, plan.qtp, plan.qtt,
+    hipLaunchKernelGGL(shared_join_kernel<D>, dim3(a.B * a.n_kv, (columns + 3) / 4), dim3(256), 0, s, a, plan.qtp, plan.qtt,
                        plan.grid, out[0], out[1]);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     a.row_off += a.B;
@@ -250,13 +248,10 @@ hipError_t launch_shared_attention(const DraftArgs &a, const SharedPlan &plan, v
     if (plan.waves == 8) switch (plan.qtt) {
         case 16: return go_shared<D, 32, 16, 1, 8>(a, plan, ws, s);
         case 32: return go_shared<D, 32, 32, 1, 8>(a, plan, ws, s);
-        case 128: return go_shared<D, 32, 16, 8, 8>(a, plan, ws, s);
-        case 256: return go_shared<D, 32, 32, 8, 8>(a, plan, ws, s);
       }
     else switch (plan.qtt) {
         case 16: return plan.qtp == 64 ? go_shared<D, 16, 16, 1, 4>(a, plan, ws, s) : go_shared<D, 32, 16, 1, 4>(a, plan, ws, s);
         case 64: return go_shared<D, 32, 16, 4, 4>(a, plan, ws, s);
-        case 128: return go_shared<D, 32, 32, 4, 4>(a, plan, ws, s);
       }
     return hipErrorInvalidValue;
   };

@@ -178,7 +178,7 @@ DraftArgs draft_args(const ods_block *blk, int layer, const ods_batch *batch, co
     a.gain_q = (const uint16_t *)n.gain_q; a.gain_k = (const uint16_t *)n.gain_k; a.eps = n.eps;
   }
   a.batch = batch->batch;
-  if (takes_shared(c, draft)) a.shared = *draft->shared;
+  if (takes_shared(c, batch, draft)) a.shared = *draft->shared;
   return a;
 }
 
@@ -381,7 +381,7 @@ ods_status ods_run_draft(const ods_block *blk, int32_t op_begin, int32_t op_end,
     const DraftArgs a = draft_args(blk, op.layer, batch, draft, st);
     const ods_layer_cfg &c = blk->layers[op.layer].cfg;
     const hipError_t e = !step.attn ? launch_draft_rope_append(a, step.rope, step.append, stream)
-                         : takes_shared(c, draft)
+                         : takes_shared(c, batch, draft)
                              ? launch_shared_attention(a, shared_plan(c, batch, draft, cus), st->ws, stream)
                              : launch_tree_attention(a, tree_plan(c, batch, draft, cus), st->ws, stream);
     const char *what = step.rope && step.append ? "rope+kv_append" : op_kind_name(op.kind);

@@ -200,6 +200,27 @@ size_t tree_ws_bytes(const TreePlan &p, int D) {
   return (size_t)p.grid * kTreeDescBytes + (size_t)2 * p.grid * p.qt * (D + 2) * sizeof(float);
 }
 
+namespace {
+
+constexpr int kSharedColumns = 32;                    // most query vectors of a KV head and sequence
+constexpr int64_t kSharedBytes = (int64_t)128 << 20;  // fewest of the tables' tokens
+
+bool spans_shared(const ods_layer_cfg &c, const ods_batch *batch) {
+  return (int64_t)batch->batch * batch->max_pages * ODS_PAGE_TOKENS >= kSharedBytes / ((int64_t)4 * c.n_kv * c.head_dim);
+}
+
+}  // namespace
+
+// Reading a prefix once saves what its sequences would read of it again: from memory where their tables span more than the
+// caches hold, else from these, which is no gain over a second kernel's start and records. With many columns a sequence the
+// products bound either way, and the records grow with them. 32 / 8 heads of 128, one group, tails of 256, us with and
+// without: a token each, 8 sequences over 2048 (76 MB) 20.5 and 18.5, 16 over 2048 (151 MB) 24.7 and 27.7, 8 over 8192
+// (277 MB) 29 and 48, 64 over 8192 43 and 208; 64 sequences of 24, 32, 48 and 64 columns over 8192 100 and 207, 130 and 209,
+// 179 and 211, 229 and 214; of 32 and 48 over 2048 68 and 64, 88 and 67. The host sees no contexts: tables count as if they were full.
+bool takes_shared(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft) {
+  return has_shared(c, draft) && (int64_t)draft->max_rows * (c.n_q / c.n_kv) <= kSharedColumns && spans_shared(c, batch);
+}
+
 SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus) {
   SharedPlan p;
   const int group = c.n_q / c.n_kv, groups = std::max(draft->shared->n_groups, 1);
@@ -212,23 +233,19 @@ SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods
   p.waves = mean >= 1024 ? 8 : 4;
   // Tails of 16 columns (32 with eight waves) are one wave's ranges; wider ones a workgroup's (seven groups, up to 32 columns,
   // four waves: 96 us, with ranges of a wave 98).
-  if (p.waves == 8)
-    p.qtt = nq <= 16 ? 16 : nq <= 32 ? 32 : nq <= 128 ? 128 : 256;
-  else
-    p.qtt = nq <= 16 ? 16 : nq <= 64 ? 64 : 128;
+  p.qtt = nq <= 16 ? 16 : p.waves == 4 ? 64 : 32;
   p.qtp = p.waves == 8 ? 256 : p.qtt == 16 && mean <= 64 ? 64 : 128;
-  p.max_qt = (int)((nq + p.qtt - 1) / p.qtt);
   const int64_t tiles = ((int64_t)batch->max_pages * ODS_PAGE_TOKENS + 31) / 32 + 1;
-  const int64_t tasks = c.n_kv * (columns / p.qtp + groups) + (int64_t)batch->batch * c.n_kv * p.max_qt;
+  const int64_t tasks = c.n_kv * (columns / p.qtp + groups) + (int64_t)batch->batch * c.n_kv;
   p.units_ok = tasks * tiles < (int64_t)1 << 30;
   p.grid = (int)std::max<int64_t>(2, std::min<int64_t>((int64_t)std::max(cus, 1) * (p.waves == 4 ? 2 : 1), tasks * tiles / 4));
   // Of a prefix tile, measured as what splits the grid best (64 sequences over 8192 tokens, us at 0.5, 0.75 and 0.9 of a
   // prefix tile for a tile of eight tail waves: 42, 38 and 42; seven groups, a tile of a whole workgroup at 0.7, 1.0 and 1.3:
   // 104, 103 and 96; eight waves, 128 sequences over 32768, at 0.3, 0.4 and 0.6: 377, 309 and 312).
-  const bool of_wave = p.qtt == 16 || (p.waves == 8 && p.qtt == 32);
+  const bool of_wave = p.qtt <= 32;
   p.cost.prefix_tile = 1.f;
   p.cost.prefix_task = 4.f;
-  p.cost.tail_tile = p.waves == 8 ? (of_wave ? 0.4f : 0.8f) : of_wave ? 0.75f : 1.3f;
+  p.cost.tail_tile = p.waves == 8 ? 0.4f : of_wave ? 0.75f : 1.3f;
   p.cost.tail_task = of_wave ? 0.3f : 1.f;
   // A prefix range leaves a record of up to 66 KB (8 sequences over 2000 tokens, at least 4, 8 and 16 tiles: 23.4, 20.6 and
   // 22.5 us), a tail range of a wave one of 8 KB (2 and 3 tiles: 20.0 and 19.1).
@@ -252,7 +269,7 @@ SharedWs shared_ws(const SharedPlan &p, int batch, int rows, int n_q, int n_kv, 
     w.state_ml[i] = take((size_t)rows * n_q * 2 * sizeof(float));
   }
   w.prefix = take((size_t)rows * n_q * 2 * sizeof(int32_t));
-  w.desc = take((size_t)batch * n_kv * p.max_qt * kTreeDescBytes);
+  w.desc = take((size_t)batch * n_kv * kTreeDescBytes);
   for (int i = 0; i < 2; ++i) {
     const size_t records = (size_t)2 * p.grid * (i == 0 ? p.qtp : p.qtt <= 32 ? p.waves * p.qtt : p.qtt);
     w.rec_ml[i] = take(records * 2 * sizeof(float));
@@ -277,7 +294,7 @@ size_t draft_ws_bytes(const ods_block *blk, int op_begin, int op_end, const ods_
     const OpRef op = op_at(blk, g);
     const ods_layer_cfg &c = blk->layers[op.layer].cfg;
     if (op.kind != K_ATTN_CORE) continue;
-    w = std::max(w, takes_shared(c, draft)
+    w = std::max(w, takes_shared(c, batch, draft)
                         ? shared_ws(shared_plan(c, batch, draft, cus), batch->batch, draft->rows, c.n_q, c.n_kv, c.head_dim).bytes
                         : tree_ws_bytes(tree_plan(c, batch, draft, cus), c.head_dim));
   }
@@ -300,13 +317,13 @@ size_t draft_ws_most(const ods_block *blk, const ods_batch *batch, const ods_dra
       if (qt / (c.n_q / c.n_kv) >= 1) take(std::min(draft->max_rows, qt / (c.n_q / c.n_kv)));
     take(draft->max_rows);
     w = std::max(w, records);
-    if (!takes_shared(c, draft)) continue;
-    // The most of every part: the widest tiles, and as many of the tails' as the narrowest would make.
+    if (!has_shared(c, draft) || !spans_shared(c, batch)) continue;  // as narrower trees may take it
+    // The most of every part: the widest tiles of all, and of the tails with ranges of a wave.
     SharedPlan p{};
-    p.grid = std::max(cus, 2);
     p.waves = 8;
-    p.qtp = p.qtt = 256;
-    p.max_qt = (int)(((int64_t)draft->max_rows * (c.n_q / c.n_kv) + 127) / 128);
+    p.grid = std::max(cus, 2);
+    p.qtp = 256;
+    p.qtt = 32;
     w = std::max(w, shared_ws(p, batch->batch, draft->rows, c.n_q, c.n_kv, c.head_dim).bytes);
   }
   return w;
@@ -337,7 +354,7 @@ ods_status check_draft_sizes(const ods_block *blk, int op_begin, int op_end, con
       return set_error(ODS_EUNSUPPORTED, "layer %d: draft rows * n_q exceeds 2^31", op.layer);
     if (op.kind == K_ATTN_CORE && !tree_plan(c, batch, draft, 1).units_ok)
       return set_error(ODS_EUNSUPPORTED, "layer %d: batch * n_kv * query tiles * window pages exceeds 2^30", op.layer);
-    if (op.kind == K_ATTN_CORE && takes_shared(c, draft) && !shared_plan(c, batch, draft, 1).units_ok)
+    if (op.kind == K_ATTN_CORE && takes_shared(c, batch, draft) && !shared_plan(c, batch, draft, 1).units_ok)
       return set_error(ODS_EUNSUPPORTED, "layer %d: n_kv * query tiles of groups and trees * pages exceeds 2^30", op.layer);
   }
   return ODS_OK;
@@ -382,7 +399,7 @@ ods_status validate_draft(const ods_block *blk, int op_begin, int op_end, const 
       if ((rc = check_ptr(draft->mask, who, "mask")) != ODS_OK || (rc = check_ptr(st->o, who, "o")) != ODS_OK ||
           (rc = check_ptr(st->ws, who, "ws")) != ODS_OK)
         return rc;
-      if (takes_shared(c, draft) && ((rc = check_ptr(draft->shared->group_off, who, "shared group_off")) != ODS_OK ||
+      if (has_shared(c, draft) && ((rc = check_ptr(draft->shared->group_off, who, "shared group_off")) != ODS_OK ||
                                      (rc = check_ptr(draft->shared->tokens, who, "shared tokens")) != ODS_OK))
         return rc;
       if (need == 0) need = draft_ws_bytes(blk, op_begin, op_end, batch, draft, cus);

@@ -235,17 +235,17 @@ struct SharedCost {
 };
 struct SharedPlan {
   int waves;     // of a workgroup: 4, two workgroups to a compute unit, or 8
-  int qtp, qtt;  // columns of the query tiles of prefixes (16 or 32 a wave) and of tails
-  int max_qt;    // query tiles of the longest tree
+  int qtp, qtt;  // columns of the query tiles of prefixes (16 or 32 a wave), and of tails, which have one each
   int grid;      // workgroups
   SharedCost cost;
   bool units_ok;
 };
 constexpr int kSharedBatch = 512;  // sequences of a launch: what LDS has room for beside the tiles and the groups
-// Whether a layer's attention takes the draft's groups.
-inline bool takes_shared(const ods_layer_cfg &c, const ods_draft *draft) {
+// Whether a layer's attention could read shared prefixes once, and whether it does.
+inline bool has_shared(const ods_layer_cfg &c, const ods_draft *draft) {
   return draft->shared && draft->shared->n_groups > 0 && c.window == 0;
 }
+bool takes_shared(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft);
 SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft, int cus);
 // Where the workspace's parts are, in bytes.
 struct SharedWs {

@@ -26,6 +26,7 @@ static void *const kFake = (void *)0x100000;
 
 // Plans of every shape: the kernels that launch them exist, parts of the workspace follow each other and fit.
 static void shared_plans() {
+  int taken = 0;
   for (int hd : {64, 128})
     for (int n_kv : {1, 2, 8})
       for (int group : {1, 3, 4, 16})
@@ -54,20 +55,27 @@ static void shared_plans() {
                 d.row_off = d.depth = (int32_t *)kFake;
                 d.mask = (uint64_t *)kFake;
                 d.shared = &shared;
-                CHECK(takes_shared(L.cfg, &d));
+                const size_t need = draft_ws_bytes(&blk, 4, 5, &b, &d, 256);
+                CHECK(draft_ws_most(&blk, &b, &d, 256) >= need);
+                const bool takes = takes_shared(L.cfg, &b, &d);
+                CHECK(takes == (max_rows * group <= 32 && (int64_t)batch * pages * 16 * n_kv * hd * 4 >= 128 << 20));
+                taken += takes;
+                if (!takes) {
+                  d.shared = nullptr;
+                  CHECK(!takes_shared(L.cfg, &b, &d) && draft_ws_bytes(&blk, 4, 5, &b, &d, 256) == need);
+                  continue;
+                }
                 const SharedPlan p = shared_plan(L.cfg, &b, &d, 256);
                 if (!p.units_ok) continue;
                 CHECK(p.waves == 4 || p.waves == 8);
                 CHECK(p.waves == 8 ? p.qtp == 256 : p.qtp == 128 || (p.qtp == 64 && p.qtt == 16));
-                CHECK(p.qtt == 16 || (p.waves == 8 ? p.qtt == 32 || p.qtt == 128 || p.qtt == 256 : p.qtt == 64 || p.qtt == 128));
-                CHECK((int64_t)p.max_qt * p.qtt >= (int64_t)max_rows * group && p.grid >= 2 && p.grid <= 512);
-                CHECK(p.max_qt == 1 || p.qtt == 32 * p.waves);
+                CHECK(p.qtt == 16 || p.qtt == (p.waves == 8 ? 32 : 64));
+                CHECK(p.qtt >= max_rows * group && p.grid >= 2 && p.grid <= 512);
                 const SharedWs w = shared_ws(p, batch, d.rows, n_kv * group, n_kv, hd);
                 const size_t at[] = {w.state[0], w.state_ml[0], w.state[1], w.state_ml[1], w.prefix, w.desc,
                                      w.rec_ml[0], w.rec_acc[0], w.rec_ml[1], w.rec_acc[1], w.bytes};
                 for (size_t i = 0; i + 1 < sizeof(at) / sizeof(at[0]); ++i) CHECK(at[i] < at[i + 1] && at[i] % 16 == 0);
-                const size_t need = draft_ws_bytes(&blk, 4, 5, &b, &d, 256);
-                CHECK(need >= w.bytes && draft_ws_most(&blk, &b, &d, 256) >= need);
+                CHECK(need >= w.bytes);
                 ods_state st;
                 memset(&st, 0, sizeof(st));
                 st.qkv = st.o = st.ws = kFake;
@@ -76,6 +84,7 @@ static void shared_plans() {
                 st.ws_bytes = need - 1;
                 CHECK(validate_draft(&blk, 4, 5, &b, &d, &st, 256) == ODS_ENOMEM);
               }
+  CHECK(taken > 100);
 }
 
 // Groups of random tables against what they promise.

@@ -63,7 +63,9 @@ def test_fork_draft_verify_keep(axes):
             k.resize(b, int(k.tokens[b]) + n)
         copies()
         off = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
-        batch = R.DeviceBatch(cuda(ctx), cuda(k.table[seqs]))
+        table = np.full((len(seqs), 4096 if shared else k.table.shape[1]), -1, np.int32)  # groups are taken by tables that span 128 MB
+        table[:, :k.table.shape[1]] = k.table[seqs]
+        batch = R.DeviceBatch(cuda(ctx), cuda(table))
         draft = R.DeviceDraft(cuda(off), cuda(np.asarray(depth, np.int32)), cuda(D.mask_words(sets, max_rows)), max_rows=max_rows,
                               rope=rope, norm=norm, shared=shared)
         state = R.DeviceState(block, batch, fill=float("nan"), draft=draft)

@@ -18,6 +18,7 @@ from paper_2609_14237_amd import runtime as R  # noqa: E402
 from test_gpu_tree import Case  # noqa: E402
 
 PAGE = 16
+SPAN = 128 << 20
 
 
 def say(*a):
@@ -41,11 +42,19 @@ class Shared(Case):
             self.table[b:b + g[0], :g[1] // PAGE] = self.table[b, :g[1] // PAGE]
             b += g[0]
 
-    def device(self, rope=None, shared=True):
+    def device(self, rope=None, shared=True, more=False):
+        """Groups are taken where the tables span 128 MB: of more columns, or (`more`) of more sequences, which are left alone."""
         super().device(rope)
         self.prefix = R.SharedPrefix(cuda(self.group_off), cuda(self.tokens))
         if shared:
-            self.draft = R.DeviceDraft(cuda(self.off), cuda(self.depth), cuda(D.mask_words(self.sets, self.max_rows)),
+            B, cols = self.table.shape
+            least = SPAN // (PAGE * self.n_kv * self.hd * 4)
+            wide = np.full((max(B, -(-least // cols)), cols) if more else (B, max(cols, -(-least // B))), -1, np.int32)
+            wide[:B, :cols] = self.table
+            ctx, off = np.full(len(wide), -1, np.int32), np.full(len(wide) + 1, self.off[-1], np.int32)
+            ctx[:B], off[:B] = self.ctx, self.off[:B]
+            self.batch = R.DeviceBatch(cuda(ctx), cuda(wide), ring_table=None)
+            self.draft = R.DeviceDraft(cuda(off), cuda(self.depth), cuda(D.mask_words(self.sets, self.max_rows)),
                                        max_rows=self.max_rows, rope=rope, shared=self.prefix)
             self.state = R.DeviceState(self.block, self.batch, fill=float("nan"), draft=self.draft)
             self.state.view("qkv", *self.qkv.shape).copy_(self.qkv)
@@ -77,12 +86,22 @@ def test_prefixes_around_pages_and_tiles(prefix, hd):
     c.check(c.attend())
 
 
-@pytest.mark.parametrize("n", [1, 2, 5, 16, 33, 64])
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 8, 9, 16, 32, 33, 64])
 @pytest.mark.parametrize("group,hd", [(1, 64), (4, 128), (16, 64)])
 def test_trees_of_every_width(n, group, hd):
     say("width", n, group, hd)
     ctx = [200, 233, 192, 700, 64, 70, 80, 81]
     c = Shared([(4, 192), (4, 64)], ctx, [n] * 8, n_q=2 * group, n_kv=2, hd=hd, seed=n).device()
+    c.check(c.attend())
+
+
+@pytest.mark.parametrize("n_q,n_kv,hd,n", [(16, 1, 64, 2), (8, 2, 64, 5), (16, 1, 128, 1), (8, 2, 128, 8), (3, 3, 128, 32)])
+def test_groups_of_a_thousand_columns(n_q, n_kv, hd, n):
+    say("columns", n_q, n_kv, hd, n)
+    members = 80
+    ctx = 160 + np.arange(members) * 3
+    rows = [n - b % 2 for b in range(members)] if n > 1 else [1] * members
+    c = Shared([(members, 160)], ctx, rows, n_q=n_q, n_kv=n_kv, hd=hd, seed=n, max_rows=n).device()
     c.check(c.attend())
 
 
@@ -92,7 +111,7 @@ def test_ragged_groups_with_everything_in_them():
     say("ragged")
     ctx = [40, 400, 401, 415, -1, 390, 100, 3, 64, 0, 1000, 1200, 1024, 77, 9]
     rows = [3, 2, 0, 12, 2, 5, 4, 1, 6, 3, 1, 8, 2, 1, 4]
-    c = Shared([(0, 0), (7, 384), (2, 0), (1, 0), (3, 992)], ctx, rows, n_q=8, n_kv=2, hd=128, seed=1, max_rows=9, pad=6)
+    c = Shared([(0, 0), (7, 384), (2, 0), (1, 0), (3, 992)], ctx, rows, n_q=8, n_kv=2, hd=128, seed=1, max_rows=8, pad=6)
     c.group_off = np.array([1, 1, 8, 10, 10, 13], np.int32)   # sequences 0, 13 and 14 in no group
     c.tokens = np.array([50, 384, 0, 64, 992], np.int32)
     for a, e, k in ((1, 8, 384), (10, 13, 992)):
@@ -103,6 +122,7 @@ def test_ragged_groups_with_everything_in_them():
 
 @pytest.mark.parametrize("max_rows", [65, 128, 256])
 def test_masks_of_several_words(max_rows):
+    """More columns than groups are taken for."""
     say("words", max_rows)
     c = Shared([(3, 320)], [320, 340, 700], [max_rows, 66, 1], n_q=4, n_kv=2, hd=64, seed=max_rows, max_rows=max_rows).device()
     c.check(c.attend())
@@ -110,7 +130,7 @@ def test_masks_of_several_words(max_rows):
 
 def test_long_prefixes_cut_into_many_ranges():
     say("long")
-    for members, rows, n_q, n_kv, hd in ((2, 1, 4, 1, 64), (40, 2, 32, 8, 128), (6, 20, 16, 1, 128)):
+    for members, rows, n_q, n_kv, hd in ((2, 1, 4, 1, 64), (40, 2, 32, 8, 128), (6, 2, 16, 1, 128)):
         ctx = 9000 + np.arange(members) * 37
         c = Shared([(members, 8992)], ctx, [rows] * members, n_q=n_q, n_kv=n_kv, hd=hd, seed=members).device()
         c.check(c.attend())
@@ -142,22 +162,23 @@ def test_hidden_rows_and_what_is_not_finite():
 def test_pages_outside_the_pool_and_tables_that_end():
     say("bad pages")
     ctx = [200, 210, 230, 256, 250]
-    c = Shared([(4, 192), (1, 0)], ctx, [2, 20, 1, 9, 16], n_q=4, n_kv=2, hd=64, seed=5)
+    c = Shared([(4, 192), (1, 0)], ctx, [2, 16, 1, 9, 16], n_q=4, n_kv=2, hd=64, seed=5)
     c.table[:4, 3], c.table[:4, 4], c.table[1, 12] = -1, c.P + 5, -7
     c.table = c.table[:, :16].copy()                # 256 tokens: what does not fit is neither written nor attended
-    c.device()
+    c.device(more=True)
     c.check(c.attend())
     c = Shared([(3, 64)], [64, 64, 64], [4, 1, 2], n_q=4, n_kv=2, hd=128, seed=6)
     c.table = c.table[:, :4].copy()                 # a prefix as wide as the table: its last tile is each one's own
-    c.device()
+    c.device(more=True)
     c.check(c.attend())
 
 
 def test_claims_that_pass_the_table_or_are_negative():
     say("claims")
     for claim in (-5, 2 ** 31 - 1, 10_000):
-        c = Shared([(3, 160, claim)], [170, 180, 176], [2, 1, 3], n_q=4, n_kv=2, hd=64, seed=7).device()
-        c.check(c.attend())
+        for more in (False, True):
+            c = Shared([(3, 160, claim)], [170, 180, 176], [2, 1, 3], n_q=4, n_kv=2, hd=64, seed=7).device(more=more)
+            c.check(c.attend())
 
 
 def test_offsets_that_do_not_ascend_share_nothing():
@@ -272,7 +293,7 @@ def test_a_state_for_the_widest_serves_narrower_drafts():
     wide = Shared([(6, 640)], [640 + 9 * i for i in range(6)], [32] * 6, n_q=16, n_kv=2, hd=128, seed=13).device()
     wide.check(wide.attend())
     state = wide.state
-    for n in (1, 2, 5, 16, 31):
+    for n in (1, 2, 3, 4, 5, 16, 31):
         c = Shared([(3, 640), (2, 0)], [650 + i for i in range(5)], [n] * 5, n_q=16, n_kv=2, hd=128, seed=n).device()
         assert c.state.ws_bytes <= state.ws_bytes
         state.view("qkv", *c.qkv.shape).copy_(c.qkv)

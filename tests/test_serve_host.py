@@ -64,10 +64,11 @@ def test_norms_and_groups_of_drafted_rows_are_refused():
     assert run(4, 5, draft(rows=5000, max_rows=1, shared=B.ods_shared(4096, FAKE, FAKE)), fake_batch(batch=4096)) == B.ODS_EUNSUPPORTED
     # n_kv * query tiles of 2^20 rows * pages of a table this wide: the kernel's unit index
     wide = fake_block([replace(CFG, n_q=32, n_kv=2)])
-    assert B.ods_run_draft(wide.c, 4, 5, fake_batch(max_pages=1 << 14), draft(rows=1 << 20, max_rows=256, shared=B.ods_shared(1, FAKE, FAKE)),
+    assert B.ods_run_draft(wide.c, 4, 5, fake_batch(max_pages=1 << 14), draft(rows=1 << 20, max_rows=2, shared=B.ods_shared(1, FAKE, FAKE)),
                            fake_state(), None) == B.ODS_EUNSUPPORTED
-    need = B.ods_draft_workspace_bytes(blk.c, fake_batch(), draft(shared=B.ods_shared(1, FAKE, FAKE)))
-    assert need > B.ods_draft_workspace_bytes(blk.c, fake_batch(), draft())
+    long, one = fake_batch(max_pages=1 << 14), B.ods_shared(1, FAKE, FAKE)
+    assert B.ods_draft_workspace_bytes(blk.c, long, draft(shared=one)) > B.ods_draft_workspace_bytes(blk.c, long, draft())
+    assert B.ods_draft_workspace_bytes(blk.c, fake_batch(), draft(shared=one)) == B.ods_draft_workspace_bytes(blk.c, fake_batch(), draft())
     assert run(4, 5, draft(shared=B.ods_shared(1, FAKE, FAKE)), st=fake_state(ws_bytes=8 * 4 * 66 * 4)) == B.ODS_ENOMEM
     assert B.ods_draft_workspace_bytes(blk.c, fake_batch(), draft(shared=B.ods_shared(3, FAKE, FAKE))) == 0
     # nothing to do
