@@ -228,7 +228,8 @@ SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods
   // The host knows no group's rows: the mean group's decide. Workgroups of eight waves have a compute unit to themselves and
   // share each K/V byte among 256 columns, which is fastest where the prefixes' products are nearly all there is (128
   // sequences of 4 rows, 4096 columns, over 32768 tokens: 309 us, with four waves 379). Two of four waves overlap the products
-  // of one with the loads of the other (64 sequences over 8192 tokens, 256 columns: 38 us, with eight waves 42).
+  // of one with the loads of the other (64 sequences over 8192 tokens, 256 columns, read from the caches: 38 us, with eight
+  // waves 42).
   const int64_t mean = columns / groups;
   p.waves = mean >= 1024 ? 8 : 4;
   // Tails of 16 columns (32 with eight waves) are one wave's ranges; wider ones a workgroup's (seven groups, up to 32 columns,
@@ -239,9 +240,9 @@ SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods
   const int64_t tasks = c.n_kv * (columns / p.qtp + groups) + (int64_t)batch->batch * c.n_kv;
   p.units_ok = tasks * tiles < (int64_t)1 << 30;
   p.grid = (int)std::max<int64_t>(2, std::min<int64_t>((int64_t)std::max(cus, 1) * (p.waves == 4 ? 2 : 1), tasks * tiles / 4));
-  // Of a prefix tile, measured as what splits the grid best (64 sequences over 8192 tokens, us at 0.5, 0.75 and 0.9 of a
-  // prefix tile for a tile of eight tail waves: 42, 38 and 42; seven groups, a tile of a whole workgroup at 0.7, 1.0 and 1.3:
-  // 104, 103 and 96; eight waves, 128 sequences over 32768, at 0.3, 0.4 and 0.6: 377, 309 and 312).
+  // Of a prefix tile, measured as what splits the grid best, tokens read from the caches (64 sequences over 8192 tokens, us at
+  // 0.5, 0.75 and 0.9 of a prefix tile for a tile of eight tail waves: 42, 38 and 42; seven groups, a tile of a whole workgroup
+  // at 0.7, 1.0 and 1.3: 104, 103 and 96; eight waves, 128 sequences over 32768, at 0.3, 0.4 and 0.6: 377, 309 and 312).
   const bool of_wave = p.qtt <= 32;
   p.cost.prefix_tile = 1.f;
   p.cost.prefix_task = 4.f;

@@ -290,8 +290,9 @@ class SharedPrefix:
 class DeviceDraft:
     """ods_draft: drafted rows of a batch. row_off [B + 1] and depth [rows] int32, mask [rows, ceil(max_rows / 64)]
     int64 (bit patterns; a 1-D tensor is one word per row). `rope`: None for the layers' own, or one Rope per layer
-    (of one with sections every axis is at the row's position, as in text). `norm`: None, or one HeadNorm per layer, of whose gains the layer's q and k heads take one each. `shared`: None, or the
-    prefixes that groups of the batch's sequences share."""
+    (of one with sections every axis is at the row's position, as in text). `norm`: None, or one HeadNorm per layer, of
+    whose gains the layer's q and k heads take one each. `shared`: None, or the prefixes that groups of the batch's
+    sequences share, read once where the tables are large and the trees narrow enough for that to pay (ods_shared)."""
 
     def __init__(self, row_off: torch.Tensor, depth: torch.Tensor, mask: torch.Tensor, max_rows: int, rope=None, norm=None,
                  shared: SharedPrefix | None = None):
