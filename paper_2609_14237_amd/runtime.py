@@ -623,9 +623,9 @@ class DraftVerifier:
                 and tokens.shape == parent.shape == accept_u.shape == (rows,) and next_u.shape == (B,)
                 and tokens.dtype == parent.dtype == torch.int32 and accept_u.dtype == next_u.dtype == torch.float32
                 and tokens.is_contiguous() and parent.is_contiguous() and accept_u.is_contiguous() and next_u.is_contiguous()
-                and target.shape == (rows, vocab) and (target.stride(1) == 1 or vocab == 1)
+                and target.shape == (rows, vocab) and (target.stride(1) == 1 or vocab == 1 or rows == 0)
                 and (proposal is None or (proposal.shape == target.shape and proposal.dtype == target.dtype
-                                          and (proposal.stride(1) == 1 or vocab == 1)))):
+                                          and (proposal.stride(1) == 1 or vocab == 1 or rows == 0)))):
             self._refuse(rows, B, tokens, parent, target, accept_u, next_u, proposal)
         # the stride of a single row means nothing
         c.vocab, c.dtype, c.target = vocab, self.DTYPES[target.dtype], target.data_ptr()
@@ -654,6 +654,6 @@ class DraftVerifier:
             if t.dtype not in self.DTYPES or t.dtype != target.dtype or t.dim() != 2 or t.shape != target.shape or t.shape[0] != rows:
                 raise ValueError(f"DraftVerifier: {name} is fp32 or bf16 [{rows}, vocab], target and proposal alike, got "
                                  f"{t.dtype} {tuple(t.shape)}")
-            if t.stride(1) != 1 and t.shape[1] > 1:
+            if t.stride(1) != 1 and t.numel() > t.shape[0]:
                 raise ValueError(f"DraftVerifier: the values of a row of {name} must be contiguous")
         raise ValueError(f"DraftVerifier: {target.shape[1]} tokens, made for {self.vocab}")

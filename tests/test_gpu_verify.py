@@ -207,6 +207,22 @@ def test_large_batches_and_a_verifier_for_more():
     Case(rng.integers(1, 7, 100).tolist(), 50, 3, False, seed=13, max_rows=6).check(v)
 
 
+def test_no_rows_and_no_sequences():
+    say("empty")
+    for drawn in (False, True):
+        v = R.DraftVerifier(5, 4, 40)
+        v.path.fill_(-9), v.path_len.fill_(-9), v.next.fill_(-9)
+        c = Case([0, 0, 0], 40, 1, drawn, seed=16, path_cols=4)
+        v.run(c.draft(), *c.args(), proposal=c.proposal)
+        torch.cuda.synchronize()
+        assert (v.path[:3] == -1).all() and (v.path_len[:3] == 0).all() and (v.next[:3] == -1).all()
+        assert (v.path[3:] == -9).all() and (v.path_len[3:] == -9).all() and (v.next[3:] == -9).all()
+    c.off, c.v, before = c.off[:1], c.v[:0], v.path.clone()
+    v.run(c.draft(), *c.args(), proposal=c.proposal)
+    torch.cuda.synchronize()
+    assert torch.equal(v.path, before)
+
+
 def test_tokens_come_from_the_target():
     """4096 times the same row: its next token, drafted or not, is distributed as the target says. The count of a token of
     probability p is within 5 of its deviations sqrt(n p (1 - p)) of n p (one in a million falls outside)."""
