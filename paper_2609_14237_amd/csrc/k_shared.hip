@@ -93,7 +93,7 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
     t.first[b] = covered ? first : 0;
     t.key[b] = covered ? p.r0[g] * group : -1;
     t.n[b] = end == 0 ? 0 : (end - 1) / kTile + 1 - t.first[b];
-    t.pre[b] = end == 0 ? 0 : a.n_kv * ((rows * group + QTT - 1) / QTT);
+    t.pre[b] = end == 0 ? 0 : a.n_kv;
     sums[2] += t.n[b] * t.pre[b];
     sums[3] += t.pre[b];
   }
@@ -113,7 +113,8 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
   const int G = gridDim.x, r = blockIdx.x;
   for (int b = r; b < B; b += G) {  // what no range writes: zeros of sequences left alone, tasks that are none
     zero_left_alone(a, b, THREADS);
-    if (t.n[b] == 0 && tid < a.n_kv) tail_out.desc[(int64_t)b * a.n_kv + tid].pieces = 0;
+    if (t.n[b] != 0) continue;
+    for (int i = tid; i < a.n_kv; i += THREADS) tail_out.desc[(int64_t)b * a.n_kv + i].pieces = 0;
   }
   const float of_p = (float)sums[0] * cost.prefix_tile + (float)sums[1] * cost.prefix_task;
   const float of_t = (float)sums[2] * cost.tail_tile + (float)sums[3] * cost.tail_task;
@@ -250,7 +251,7 @@ hipError_t launch_shared_attention(const DraftArgs &a, const SharedPlan &plan, v
         case 32: return go_shared<D, 32, 32, 1, 8>(a, plan, ws, s);
       }
     else switch (plan.qtt) {
-        case 16: return plan.qtp == 64 ? go_shared<D, 16, 16, 1, 4>(a, plan, ws, s) : go_shared<D, 32, 16, 1, 4>(a, plan, ws, s);
+        case 16: return go_shared<D, 32, 16, 1, 4>(a, plan, ws, s);
         case 64: return go_shared<D, 32, 16, 4, 4>(a, plan, ws, s);
       }
     return hipErrorInvalidValue;

@@ -214,8 +214,8 @@ bool spans_shared(const ods_layer_cfg &c, const ods_batch *batch) {
 // Reading a prefix once saves what its sequences would read of it again: from memory where their tables span more than the
 // caches hold, else from these, which is no gain over a second kernel's start and records. With many columns a sequence the
 // products bound either way, and the records grow with them. 32 / 8 heads of 128, one group, tails of 256, us with and
-// without: a token each, 8 sequences over 2048 (76 MB) 20.5 and 18.5, 16 over 2048 (151 MB) 24.7 and 27.7, 8 over 8192
-// (277 MB) 29 and 48, 64 over 8192 43 and 208; 64 sequences of 24, 32, 48 and 64 columns over 8192 100 and 207, 130 and 209,
+// without: a token each, 8 sequences over 2048 (76 MB) 20.5 and 18.5, 16 over 2048 (151 MB) 26 and 28, 8 over 8192
+// (277 MB) 28 and 48, 64 over 8192 43 and 208; 64 sequences of 24, 32, 48 and 64 columns over 8192 100 and 207, 130 and 209,
 // 179 and 211, 229 and 214; of 32 and 48 over 2048 68 and 64, 88 and 67. The host sees no contexts: tables count as if they were full.
 bool takes_shared(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft) {
   return has_shared(c, draft) && (int64_t)draft->max_rows * (c.n_q / c.n_kv) <= kSharedColumns && spans_shared(c, batch);
@@ -235,22 +235,24 @@ SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods
   // Tails of 16 columns (32 with eight waves) are one wave's ranges; wider ones a workgroup's (seven groups, up to 32 columns,
   // four waves: 96 us, with ranges of a wave 98).
   p.qtt = nq <= 16 ? 16 : p.waves == 4 ? 64 : 32;
-  p.qtp = p.waves == 8 ? 256 : p.qtt == 16 && mean <= 64 ? 64 : 128;
+  p.qtp = 32 * p.waves;
   const int64_t tiles = ((int64_t)batch->max_pages * ODS_PAGE_TOKENS + 31) / 32 + 1;
   const int64_t tasks = c.n_kv * (columns / p.qtp + groups) + (int64_t)batch->batch * c.n_kv;
   p.units_ok = tasks * tiles < (int64_t)1 << 30;
   p.grid = (int)std::max<int64_t>(2, std::min<int64_t>((int64_t)std::max(cus, 1) * (p.waves == 4 ? 2 : 1), tasks * tiles / 4));
-  // Of a prefix tile, measured as what splits the grid best, tokens read from the caches (64 sequences over 8192 tokens, us at
-  // 0.5, 0.75 and 0.9 of a prefix tile for a tile of eight tail waves: 42, 38 and 42; seven groups, a tile of a whole workgroup
-  // at 0.7, 1.0 and 1.3: 104, 103 and 96; eight waves, 128 sequences over 32768, at 0.3, 0.4 and 0.6: 377, 309 and 312).
+  // Of a prefix tile, measured as what splits the grid best (us, tokens from memory): tails of a wave at 0.5, 0.75, 1.0 and
+  // 1.3, 64 sequences over 8192 tokens 47, 45, 46 and 45, 4 over 32768 tokens 52.5, 49.2, 48.2 and 48.1; tails of four waves,
+  // seven groups, 114, 107, 110 and 106 (1.6: 110); eight waves, 128 sequences over 32768, at 0.3, 0.4, 0.6 and 1.0: 377, 309,
+  // 312 and 318.
   const bool of_wave = p.qtt <= 32;
   p.cost.prefix_tile = 1.f;
   p.cost.prefix_task = 4.f;
-  p.cost.tail_tile = p.waves == 8 ? 0.4f : of_wave ? 0.75f : 1.3f;
+  p.cost.tail_tile = p.waves == 8 ? 0.4f : 1.3f;
   p.cost.tail_task = of_wave ? 0.3f : 1.f;
-  // A prefix range leaves a record of up to 66 KB (8 sequences over 2000 tokens, at least 4, 8 and 16 tiles: 23.4, 20.6 and
-  // 22.5 us), a tail range of a wave one of 8 KB (2 and 3 tiles: 20.0 and 19.1).
-  p.cost.prefix_least = 8;
+  // A prefix range leaves a record of up to 66 KB (at least 4, 8, 16 and 24 tiles: 8 sequences over 8192 tokens 32, 29, 25 and
+  // 27 us, 16 over 16384 38, 38, 35 and 34), a tail range of a wave one of 8 KB (2, 3 and 6 tiles: 16 sequences over 2048
+  // tokens 24, 23 and 27 us).
+  p.cost.prefix_least = 16;
   p.cost.tail_least = of_wave ? 3 : 4;
   p.cost.prefix_slack = 6;
   p.cost.tail_slack = of_wave ? 1 : 8;

@@ -235,7 +235,7 @@ struct SharedCost {
 };
 struct SharedPlan {
   int waves;     // of a workgroup: 4, two workgroups to a compute unit, or 8
-  int qtp, qtt;  // columns of the query tiles of prefixes (16 or 32 a wave), and of tails, which have one each
+  int qtp, qtt;  // columns of the query tiles of prefixes (32 a wave), and of tails, which have one each
   int grid;      // workgroups
   SharedCost cost;
   bool units_ok;

@@ -186,8 +186,9 @@ struct TreeShape {
 };
 
 // Range r of G of a launch's tasks, by QW waves. The sequences of kPrefix and kTail are known already, seqs.pre holding the
-// tasks of each. Ranges are whole tasks where the longest is at most `slack` tiles more than an even share. WPB > 1: a workgroup is that many waves of one range each (QW is 1), with tiles of their own.
-// K and V go past the caches with STREAM (kTail: with `past`).
+// tasks of each. Ranges are whole tasks where the longest is at most `slack` tiles more than an even share. WPB > 1: a
+// workgroup is that many waves of one range each (QW is 1), with tiles of their own. K and V go past the caches with STREAM
+// (kTail: with `past`).
 template <int D, int NQ, int QW, int NS, bool STREAM, TreePart PART, int WPB>
 __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &seqs, uint8_t *const all_slots, const int r, const int G,
                                           const int min_tiles, const int slack, const int max_qt, const int by_task, const int no_cut,
@@ -746,8 +747,8 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   // after its last use) and softmax, which also fetches a tile.
   //  - Softmax of tile t fetches into the slot of tile t - 1, whose last reads were made in products t - 1.
   //  - Two or four waves meet once a tile, after its softmax; where a compute unit runs two workgroups, the other fills the
-  //    gaps. Products of tile t read its keys first, so one tile fewer has to have landed (24 rows x 64 sequences: 123 us with the keys
-  //    read a tile ahead, 112).
+  //    gaps. Products of tile t read its keys first, so one tile fewer has to have landed (24 rows x 64 sequences: 123 us with
+  //    the keys read a tile ahead, 112).
   //  - Eight waves have a compute unit to themselves. Their products read the next tile's keys, so that the reads run under
   //    the products: everyone's loads of t + 1 have landed before products t. The two waves of a SIMD run half a tile apart
   //    and all meet after either phase: while one is at its products the other is at its softmax. In step they queue for

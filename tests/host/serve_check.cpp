@@ -68,7 +68,7 @@ static void shared_plans() {
                 const SharedPlan p = shared_plan(L.cfg, &b, &d, 256);
                 if (!p.units_ok) continue;
                 CHECK(p.waves == 4 || p.waves == 8);
-                CHECK(p.waves == 8 ? p.qtp == 256 : p.qtp == 128 || (p.qtp == 64 && p.qtt == 16));
+                CHECK(p.qtp == 32 * p.waves);
                 CHECK(p.qtt == 16 || p.qtt == (p.waves == 8 ? 32 : 64));
                 CHECK(p.qtt >= max_rows * group && p.grid >= 2 && p.grid <= 512);
                 const SharedWs w = shared_ws(p, batch, d.rows, n_kv * group, n_kv, hd);

@@ -250,6 +250,18 @@ def test_captured_graph_whose_groups_change():
     g.close()
 
 
+def test_sequences_that_end_between_calls():
+    """What an earlier call left in the workspace is not joined for sequences that are left alone now, of any KV head."""
+    say("left alone")
+    c = Shared([(3, 96)], [100, 130, 96], [2, 1, 2], n_q=300, n_kv=300, hd=64, seed=17).device()
+    c.check(c.attend())
+    c.ctx[1] = -1
+    c.batch.ctx_lens.copy_(cuda(c.ctx))
+    got = c.attend()
+    c.check(got)
+    assert (got[2] == 0).all()
+
+
 def test_the_same_twice_and_on_another_stream():
     say("stream")
     c = Shared([(40, 2000)], 2000 + np.arange(40) * 11, [2] * 40, n_q=32, n_kv=8, hd=128, seed=11).device()
