@@ -133,28 +133,32 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
   }
 }
 
-// One wave per column of a tail task: the pieces of its prefix task, then its own. Bound by latency where there are few
-// columns (the two descriptors, then all records at once), by memory where there are many.
-template <int D>
+// JOIN waves per column of a tail task, which take turns at the pieces of its prefix task and then its own. Bound by latency
+// where there are few columns (the two descriptors, then all records at once), by memory where there are many.
+template <int D, int JOIN>
 __global__ __launch_bounds__(256) void shared_join_kernel(const DraftArgs a, const int qtp, const int qtt, const int ranges, const TreeOut prefix_out,
                                                           const TreeOut tail_out) {
   constexpr int LPR = D / 4, RPW = kWave / LPR, PRE = 4;  // lanes per record, records a wave reads at once, trips in flight
-  const int lane = threadIdx.x & 63, at = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ float s_m[4], s_l[4];
+  __shared__ f32x4 s_v[4][LPR];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave % JOIN;
+  const int at = blockIdx.y * (4 / JOIN) + wave / JOIN;
   const int group = a.n_q / a.n_kv;
   const TreeDesc e = tail_out.desc[blockIdx.x];
   const int col = e.col0 + at;
-  if (e.pieces == 0 || at >= qtt || col >= e.cols || (e.pieces == 1 && e.key < 0)) return;
+  const bool live = !(e.pieces == 0 || at >= qtt || col >= e.cols || (e.pieces == 1 && e.key < 0));
   const int row = e.r0 + col / group, head = e.head;
   const int64_t to = (int64_t)row * a.n_q + head * group + col % group;
   const int rel = e.key < 0 ? 0 : e.r0 * group + col - e.key, first = rel / qtp * qtp;
-  const int2 p = e.key < 0 ? make_int2(0, 0) : prefix_out.prefix[(int64_t)head * a.rows * group + e.key + first];
+  const int2 p = !live || e.key < 0 ? make_int2(0, 0) : prefix_out.prefix[(int64_t)head * a.rows * group + e.key + first];
   // Records of the launch, whatever was left where a group's rows are not ascending.
-  if (p.x < 0 || p.y < 0 || (int64_t)(p.y | 1) + 2 * ((int64_t)p.x - 1) >= 2 * ranges) return;
-  const int pieces = p.x + e.pieces;
+  const bool none = !live || p.x < 0 || p.y < 0 || (int64_t)(p.y | 1) + 2 * ((int64_t)p.x - 1) >= 2 * ranges;
+  if (JOIN == 1 && none) return;
+  const int pieces = none ? 0 : p.x + e.pieces;
   const int d = (lane % LPR) * 4, sub = lane / LPR;
   float M = kNoScore, sum = 0.f;
   f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int i0 = 0; i0 < pieces; i0 += PRE * RPW) {
+  for (int i0 = part * PRE * RPW; i0 < pieces; i0 += JOIN * PRE * RPW) {
     f32x4 x[PRE];
     float2 ml[PRE];
 #pragma unroll
@@ -194,7 +198,21 @@ __global__ __launch_bounds__(256) void shared_join_kernel(const DraftArgs a, con
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] += __shfl_xor(v[i], o, kWave);
   }
-  if (lane >= LPR) return;
+  if (JOIN > 1) {
+    if (lane == 0) s_m[wave] = top, s_l[wave] = l;
+    if (lane < LPR) s_v[wave][lane] = v;
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int i = 1; i < JOIN; ++i) {
+      const float other = s_m[wave + i], both = fmaxf(top, other);
+      const float x = __builtin_amdgcn_exp2f(top - both), y = __builtin_amdgcn_exp2f(other - both);
+      l = l * x + s_l[wave + i] * y;
+      v = v * x + s_v[wave + i][lane % LPR] * y;
+      top = both;
+    }
+  }
+  if ((JOIN > 1 && none) || lane >= LPR) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   u32x2 out;
   out[0] = pack_pair(v[0] * inv, v[1] * inv);
@@ -225,14 +243,18 @@ hipError_t go_shared(DraftArgs a, const SharedPlan &plan, void *ws, hipStream_t 
   }
   const float scale = (float)(1.4426950408889634 / sqrt((double)D));
   const int B = a.B, most = a.max_rows * (a.n_q / a.n_kv), columns = most < plan.qtt ? most : plan.qtt;
+  // Four waves a column where one each is fewer than the chip runs at once (64 tokens over 8192, 2048 columns: 45.2 us with one,
+  // 43.9; 4 over 32768: 49.5, 40.2), one where they are more than enough (4096 columns: 56, 58; seven groups: 107, 119).
+  const int waves = (int64_t)a.rows * a.n_q <= 2048 ? 4 : 1;
+  const auto join = waves == 4 ? shared_join_kernel<D, 4> : shared_join_kernel<D, 1>;
   for (int b0 = 0; b0 < B; b0 += kSharedBatch) {  // a group on both sides of a border is two, each of which reads the prefix
     a.B = B - b0 < kSharedBatch ? B - b0 : kSharedBatch;
     a.base = b0;
     hipLaunchKernelGGL(kern, dim3(plan.grid), dim3(64 * KW), tiles + shared_meta_bytes(a.shared.n_groups, a.B), s, a, plan.cost,
                        scale, out[0], out[1]);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(shared_join_kernel<D>, dim3(a.B * a.n_kv, (columns + 3) / 4), dim3(256), 0, s, a, plan.qtp, plan.qtt,
-                       plan.grid, out[0], out[1]);
+    hipLaunchKernelGGL(join, dim3(a.B * a.n_kv, (columns * waves + 3) / 4), dim3(256), 0, s, a, plan.qtp, plan.qtt, plan.grid, out[0],
+                       out[1]);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     a.row_off += a.B;
     a.ctx_lens += a.B;
