@@ -225,6 +225,7 @@ hipError_t go_shared(DraftArgs a, const SharedPlan &plan, void *ws, hipStream_t 
   using Shape = TreeShape<D, NQP, KW>;
   static std::atomic<uint64_t> lds_set{0};  // devices whose LDS limit is raised
   if (plan.waves != KW || plan.qtp != NQP * KW || plan.qtt != NQT * WT) return hipErrorInvalidValue;  // what the workspace is cut for
+  if (a.max_rows * (a.n_q / a.n_kv) > NQT * WT || a.max_rows > 32) return hipErrorInvalidValue;  // one query tile, masks of 32 bits
   const size_t tiles = (size_t)Shape::kSlots * Shape::kTileBytes;
   const auto kern = shared_attention_kernel<D, NQP, NQT, WT, KW>;
   if (hipError_t e = ensure_lds_limit((const void *)kern, tiles + shared_meta_bytes(ODS_SHARED_GROUPS, kSharedBatch), lds_set); e != hipSuccess)

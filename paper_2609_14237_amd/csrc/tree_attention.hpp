@@ -202,6 +202,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   constexpr int DEAL = PART == kWhole && NQ == 16 ? 4 : 1;  // most whole tasks of a range; wider waves have no registers left for a list
   const int B = seqs.count, group = a.n_q / a.n_kv;
   int *const s_pre = seqs.pre, *const s_first = seqs.first, *const s_n = seqs.n;
+  const int window = PART == kWhole ? a.window : 0, ring = PART == kWhole ? a.ring : 0;  // groups are of full attention
   TreeDesc *const desc = out.desc;
   __shared__ int s_tot[QW * WPB][3], s_ids[THREADS], s_ord[DEAL > 1 ? THREADS : 1], s_lists[WPB][DEAL][4], s_most;
 
@@ -246,8 +247,8 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
     for (int b = b0; b < b1; ++b) {
       int first, n, of_seq;
       if (PART == kWhole) {
-        const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
-        tiles_of(s, a.window, first, n);
+        const DraftSeq s = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, ring);
+        tiles_of(s, window, first, n);
         s_first[b] = first;
         s_n[b] = n;
         of_seq = n == 0 ? 0 : a.n_kv * ((s.n * group + QT - 1) / QT);
@@ -363,7 +364,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   } else if (whole) {
     if (at_list < each) {
       const int k = deal(r, at_list), i = k < all_tasks ? find(k) : 0, b = dealt ? s_ord[i] : i;
-      const int rows = PART == kPrefix ? 0 : draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring).n;
+      const int rows = PART == kPrefix ? 0 : draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, ring).n;
       s_list[at_list][0] = b;
       s_list[at_list][1] = k - s_pre[i];
       s_list[at_list][2] = k < all_tasks ? s_n[b] : 0;
@@ -403,8 +404,8 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
       else if (max_qt > 1) head /= (s_pre[b + 1] - s_pre[b]) / (n * a.n_kv);
     }
     const int lp = 2 * ((PART == kPrefix ? 0 : s_first[b]) + off) + (lane & 1);
-    if (a.ring <= 0 && lp >= a.cols) return -1;
-    return (int64_t)(PART == kPrefix ? s_first[b] : b) * a.cols + (a.ring > 0 ? lp % a.ring : lp);
+    if (ring <= 0 && lp >= a.cols) return -1;
+    return (int64_t)(PART == kPrefix ? s_first[b] : b) * a.cols + (ring > 0 ? lp % ring : lp);
   };
   constexpr int64_t blk = (int64_t)kPage * D;
   int it = 0, islot = 0;   // next unit to fetch, and its slot
@@ -493,7 +494,8 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   f32x4 s[CB][2];
   float m[CB], l[CB];
   int col_lo[CB];                     // first visible token of this lane's columns
-  uint64_t col_mask[CB];              // their rows' masks, or, where those are of several words, the rows themselves
+  // Their rows' masks, or, where those are of several words, the rows themselves; groups have 32 columns a sequence at most.
+  std::conditional_t<PART == kWhole, uint64_t, uint32_t> col_mask[CB];
 
   auto task_id = [&]() { return ((int64_t)cb_seq * a.n_kv + head) * max_qt + qt; };
   auto load_seq = [&]() {
@@ -505,7 +507,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
       seq.ctx = seq.end = seq.cap = c_n * kTile;
     } else {
       c_first = uniform(s_first[cb_seq]);
-      const DraftSeq s = draft_seq((ConstInts)a.row_off, (ConstInts)a.ctx_lens, cb_seq, a.rows, a.max_rows, a.cols, a.ring);
+      const DraftSeq s = draft_seq((ConstInts)a.row_off, (ConstInts)a.ctx_lens, cb_seq, a.rows, a.max_rows, a.cols, ring);
       seq.r0 = uniform(s.r0);
       seq.n = uniform(s.n);
       seq.ctx = uniform(s.ctx);
@@ -529,8 +531,8 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
       const uint16_t *src = a.qkv + (seq.r0 + j) * row_elems + (head * group + c - j * group) * D + rq * 8;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) q[cb][kk] = *(const u32x4 *)(src + kk * 32);
-      col_mask[cb] = PART == kPrefix ? 0 : a.max_rows <= 64 ? a.mask[seq.r0 + j] : (uint64_t)(seq.r0 + j);
-      col_lo[cb] = a.window > 0 ? max(0, seq.ctx + clamp_depth(a.depth[seq.r0 + j], a.max_rows) - a.window + 1) : 0;
+      col_mask[cb] = PART == kPrefix ? 0 : PART == kTail || a.max_rows <= 64 ? a.mask[seq.r0 + j] : (uint64_t)(seq.r0 + j);
+      col_lo[cb] = window > 0 ? max(0, seq.ctx + clamp_depth(a.depth[seq.r0 + j], a.max_rows) - window + 1) : 0;
       m[cb] = kNoScore;
       l[cb] = 0.f;
 #pragma unroll
@@ -554,16 +556,12 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
       sum += __shfl_xor(sum, 16, kWave);
       sum += __shfl_xor(sum, 32, kWave);
       const int at = col0 + cb * 16 + hl, c = qt * QT + at;
-      if (c >= cols) continue;
-      const int j = row_of(c);
-      if (whole && (PART == kPrefix || (PART == kTail && c_key >= 0))) {
-        const int64_t to = (int64_t)(seq.r0 + j) * a.n_q + head * group + c - j * group;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(out.state_acc + to * D + nb * 16 + rq * 4) = acc[cb][nb];
-        if (rq == 0) out.state_ml[to] = make_float2(m[cb], sum);
-      } else if (whole) {
+      const int j = row_of(min(c, cols - 1));
+      const int64_t to = (int64_t)(seq.r0 + j) * a.n_q + head * group + c - j * group, at_rec = (int64_t)rec * QT + at;
+      const bool mine = c < cols, state = whole && (PART == kPrefix || (PART == kTail && c_key >= 0));
+      if (mine && whole && !state) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        uint16_t *dst = a.o + ((int64_t)(seq.r0 + j) * a.n_q + head * group + c - j * group) * D + rq * 4;
+        uint16_t *dst = a.o + to * D + rq * 4;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           u32x2 w;
@@ -571,12 +569,13 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
           w[1] = pack_pair(acc[cb][nb][2] * inv, acc[cb][nb][3] * inv);
           *(u32x2 *)(dst + nb * 16) = w;
         }
-      } else {
-        float *dst = out.rec_acc + ((int64_t)rec * QT + at) * D + rq * 4;
+      }
+      if (mine && (state || !whole)) {
+        float *dst = (state ? out.state_acc + to * D : out.rec_acc + at_rec * D) + rq * 4;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) *(f32x4 *)(dst + nb * 16) = acc[cb][nb];
-        if (rq == 0) out.rec_ml[(int64_t)rec * QT + at] = make_float2(m[cb], sum);
       }
+      if (mine && (state || !whole) && rq == 0) *(state ? out.state_ml + to : out.rec_ml + at_rec) = make_float2(m[cb], sum);
     }
   };
 
@@ -627,12 +626,13 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
         const int j0 = t0 - seq.ctx;  // drafted token of the tile's first slot (below 0: cached ones come first)
-        uint32_t v = PART == kPrefix ? 0u : words == 1 ? (j0 < 0 ? (j0 > -32 ? (uint32_t)(col_mask[cb] << -j0) : 0u)
-                                          : j0 < 64 ? (uint32_t)(col_mask[cb] >> j0) : 0u)
+        constexpr int BITS = 8 * sizeof(col_mask[0]);
+        uint32_t v = PART == kPrefix ? 0u : PART == kTail || words == 1 ? (j0 < 0 ? (j0 > -32 ? (uint32_t)(col_mask[cb] << -j0) : 0u)
+                                          : j0 < BITS ? (uint32_t)(col_mask[cb] >> j0) : 0u)
                                 : mask_window(a.mask + (int64_t)col_mask[cb] * words, words, j0);
         v &= bits_between(-j0, seq.end - t0);
         v = v >> (rq * 8) & 0xffu;
-        if (a.window > 0 && a.window < a.max_rows) {  // not the drafted tokens `window` positions or more before the row
+        if (window > 0 && window < a.max_rows) {  // not the drafted tokens `window` positions or more before the row
           int depth[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) depth[i] = v >> i & 1 ? a.depth[seq.r0 + j0 + rq * 8 + i] : 0;
@@ -762,7 +762,9 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   //    have landed when anyone's products t end.
   //  - One wave alone has no barrier; it reads a tile when it starts on it.
   constexpr bool PING = QW == 8;
-  constexpr bool AHEAD = QW == 8;  // keys are read a tile ahead
+  // Keys are read a tile ahead. Not where prefixes and tails are one kernel: it has no registers left for them, and what is
+  // spilled to memory there has been read back by the lanes of an inner branch alone (128 x 4 rows over 32768: 300 us, 312).
+  constexpr bool AHEAD = QW == 8 && PART == kWhole;
   int slot = 0;
   auto next_slot = [](int x) { return x + 1 == NS ? 0 : x + 1; };
   auto at_slot = [&](int x) { return (const uint8_t *)(slots + x * Shape::kTileBytes); };
@@ -839,7 +841,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
     if ((it & 31) == 0) next_window();
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): what is pending here is not waited for in every product phase below
     // Tiles that need no mask, up to the next page window: all of it cached tokens that every row sees, pages in the pool.
-    const int lo_most = a.window > 0 ? seq.ctx + a.max_rows - a.window : 0;
+    const int lo_most = window > 0 ? seq.ctx + a.max_rows - window : 0;
     const int full_end = min(seq.ctx, seq.cap) / kTile - c_first, full_begin = (max(lo_most, 0) + kTile - 1) / kTile - c_first;
     const int run = tile < full_begin ? 0 : min(min(n_w - t, full_end - tile), 32 - (it & 31));
     int done = 0;

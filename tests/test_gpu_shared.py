@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import draft_ref as D
+import workloads as W
 
 pytestmark = pytest.mark.gpu
 
@@ -134,6 +135,50 @@ def test_long_prefixes_cut_into_many_ranges():
         ctx = 9000 + np.arange(members) * 37
         c = Shared([(members, 8992)], ctx, [rows] * members, n_q=n_q, n_kv=n_kv, hd=hd, seed=members).device()
         c.check(c.attend())
+
+
+@pytest.mark.parametrize("hd,n,tail", [(128, 4, 700), (128, 2, 700), (64, 4, 1400)])
+def test_long_ranges_of_whole_tails(hd, n, tail):
+    """Ranges of one wave that pass several tails and more than 32 tiles, beside a prefix long enough to leave them few
+    compute units. The definition is computed on the GPU in 64 bits."""
+    say("long tails", hd, n, tail)
+    B, g, prefix = 128, 8, 65536
+    rng = np.random.default_rng(hd + n)
+    ctx = prefix + rng.integers(tail // 3, tail, B)
+    own = -(-(ctx + n) // PAGE) - prefix // PAGE
+    P = prefix // PAGE + int(own.sum())
+    ids, at = rng.permutation(P).astype(np.int32), prefix // PAGE
+    table = np.full((B, prefix // PAGE + int(own.max())), -1, np.int32)
+    table[:, :prefix // PAGE] = ids[:prefix // PAGE]
+    for b, k in enumerate(own):
+        table[b, prefix // PAGE:prefix // PAGE + k] = ids[at:at + k]
+        at += k
+    gen = torch.Generator(device="cuda").manual_seed(hd)
+    pool = torch.randn((P, 2, 1, PAGE * hd), generator=gen, device="cuda").to(torch.bfloat16)
+    qkv = torch.randn((B * n, (g + 2) * hd), generator=gen, device="cuda").to(torch.bfloat16)
+    block = R.DeviceBlock([W.LayerCfg(hidden=256, n_q=g, n_kv=1, head_dim=hd, ffn=512)], [{}], [pool], P)
+    batch = R.DeviceBatch(cuda(ctx.astype(np.int32)), cuda(table))
+    draft = R.DeviceDraft(cuda(np.arange(B + 1, dtype=np.int32) * n), cuda(np.tile(np.arange(n, dtype=np.int32), B)),
+                          cuda(np.tile((2 << np.arange(n)) - 1, B).astype(np.int64)), max_rows=n,
+                          shared=R.SharedPrefix(cuda(np.array([0, B], np.int32)), cuda(np.array([prefix], np.int32))))
+    state = R.DeviceState(block, batch, fill=float("nan"), draft=draft)
+    state.view("qkv", *qkv.shape).copy_(qkv)
+    R.run_draft(block, 4, 5, batch, draft, state)
+    torch.cuda.synchronize()
+    got = state.view("o", B * n, g * hd).double().cpu().numpy().reshape(B, n, g, hd)
+    for b in range(B):
+        last = int(ctx[b]) + n
+        pages = pool[torch.from_numpy(table[b, :-(-last // PAGE)].astype(np.int64)).cuda()].double()
+        k = pages[:, 0, 0].reshape(-1, hd)[:last]
+        v = pages[:, 1, 0].view(-1, hd, PAGE).transpose(1, 2).reshape(-1, hd)[:last]
+        s = qkv[b * n:(b + 1) * n, :g * hd].double().reshape(n * g, hd) @ k.T / hd ** 0.5
+        s = s.view(n, g, last)
+        for j in range(n):
+            s[j, :, int(ctx[b]) + j + 1:] = -float("inf")   # a chain: rows see those before them
+        p = torch.softmax(s, dim=2).view(n * g, last)
+        o, mag = ((p @ x).cpu().numpy().reshape(n, g, hd) for x in (v, v.abs()))
+        off = np.abs(got[b] - o) - D.tree_bound(o, mag)
+        assert (off <= 0).all(), f"sequence {b}: off by {off.max()} more than the bound"
 
 
 def test_hidden_rows_and_what_is_not_finite():
