@@ -437,14 +437,15 @@ ods_status ods_head_rows(const ods_rope *rope, const ods_head_norm *norm, const 
  * sequences group_off[g] .. group_off[g + 1] - 1 of the batch, whose page tables
  * name the same pages for their first tokens[g] tokens. In full-attention layers
  * attn_core then reads those pages once for all drafted rows of the group, by
- * the first sequence's table, and each sequence's other tokens by its own. What
- * it computes is the same attention. It does so where that pays, by the sizes the
- * host sees: up to 32 query vectors of a KV head and sequence (max_rows * n_q /
- * n_kv), and tables that span 128 MB of keys and values or more (batch *
- * max_pages); elsewhere each sequence is read by itself. So are sequences in no
- * group, groups of one, and sequences of fewer cached tokens than their group
- * shares; what is shared is rounded down to 32 tokens. Sliding-window layers
- * read each sequence's own window.
+ * the table of the first sequence that has rows and them all cached, and each
+ * sequence's other tokens by its own. What it computes is the same attention. It
+ * does so where that pays, by the sizes the host sees: up to 32 query vectors of
+ * a KV head and sequence (max_rows * n_q / n_kv), and tables that span 128 MB of
+ * keys and values or more (batch * max_pages); elsewhere each sequence is read by
+ * itself. So are sequences in no group, groups of one, and sequences of fewer
+ * cached tokens than their group shares, whatever their tables hold; what is
+ * shared is rounded down to 32 tokens. Sliding-window layers read each sequence's
+ * own window.
  *   n_groups   0 .. batch, at most ODS_SHARED_GROUPS
  *   group_off  device [n_groups + 1], ascending, in 0 .. batch
  *   tokens     device [n_groups] */

@@ -12,8 +12,8 @@ namespace {
 // tail task. Prefix tasks are bound by the matrix units (their columns are the rows of a whole group), tail tasks by memory
 // (few columns a byte). Both are ranges of one grid, so that the two kinds share compute units: the ranges are split
 // between them by their expected times, which every workgroup works out from the same metadata.
-// LDS: five integers of a group, four of a sequence, three to end lists.
-inline size_t shared_meta_bytes(int groups, int B) { return ((5 * (size_t)groups + 4 * (size_t)B + 4) * 4 + 15) / 16 * 16; }
+// LDS: six integers of a group, four of a sequence, three to end lists.
+inline size_t shared_meta_bytes(int groups, int B) { return ((6 * (size_t)groups + 4 * (size_t)B + 3) * 4 + 15) / 16 * 16; }
 
 // A workgroup has KW waves. Prefix ranges are one workgroup's work; tail ranges of up to 32 columns (WT: waves of a range)
 // are one wave's each: with few columns a tile is a chain of latencies, and such chains side by side reach the memory's rate.
@@ -26,8 +26,9 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
   const int N = a.shared.n_groups, B = a.B, group = a.n_q / a.n_kv, tid = threadIdx.x;
   TreeSeqs p{}, t{};
   p.count = N;
-  p.first = smem;             // [N + 1]: a group's first sequence, in this launch's numbers
-  p.pre = p.first + N + 1;
+  int *const bound = smem;    // [N + 1]: a group's first sequence, in this launch's numbers
+  p.first = bound + N + 1;    // the sequence by whose table its prefix is read
+  p.pre = p.first + N;
   p.n = p.pre + N + 1;
   p.r0 = p.n + N;
   p.rows = p.r0 + N;
@@ -36,7 +37,7 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
   t.first = t.pre + B + 1;
   t.n = t.first + B;
   t.key = t.n + B;
-  uint8_t *const slots = (uint8_t *)smem + ((5 * N + 4 * B + 3) * 4 + 15) / 16 * 16;
+  uint8_t *const slots = (uint8_t *)smem + ((6 * N + 4 * B + 3) * 4 + 15) / 16 * 16;
   __shared__ int s_sums[KW][4];
   __shared__ float s_units[KW];
 
@@ -48,8 +49,9 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
   float tiles = 0.f;
   for (int g = tid; g <= N; g += THREADS) {
     const int s0 = here(a.shared.group_off[g]);
-    p.first[g] = s0;
+    bound[g] = s0;
     if (g == N) break;
+    p.first[g] = B;
     descends = descends || a.shared.group_off[g] > a.shared.group_off[g + 1];
     const int s1 = max(here(a.shared.group_off[g + 1]), s0);
     // Whole tiles, fewer tokens than the table holds, and none in a group of one.
@@ -84,12 +86,14 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
     int g = 0, hi = N;  // the last group that begins at b or before
     while (hi - g > 1) {
       const int mid = (g + hi) >> 1;
-      if (p.first[mid] <= b) g = mid; else hi = mid;
+      if (bound[mid] <= b) g = mid; else hi = mid;
     }
     // Its group's tiles cover a sequence that has them all cached, tokens of its own behind them, and its rows among theirs.
+    // They are read by the table of the first such one: others (left alone, released, shorter) may name no pages there.
     const int first = p.n[g];
-    const bool covered = first > 0 && b >= p.first[g] && b < p.first[g + 1] && ctx >= first * kTile && end > first * kTile &&
+    const bool covered = first > 0 && b >= bound[g] && b < bound[g + 1] && ctx >= first * kTile && end > first * kTile &&
                          r0 >= p.r0[g] && r0 + rows <= p.r0[g] + p.rows[g];
+    if (covered) atomicMin(&p.first[g], b);
     t.first[b] = covered ? first : 0;
     t.key[b] = covered ? p.r0[g] * group : -1;
     t.n[b] = end == 0 ? 0 : (end - 1) / kTile + 1 - t.first[b];
@@ -97,7 +101,9 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
     sums[2] += t.n[b] * t.pre[b];
     sums[3] += t.pre[b];
   }
+  __syncthreads();
   for (int g = tid; g < N; g += THREADS) {
+    if (p.first[g] == B) p.n[g] = p.pre[g] = 0;  // covers none
     sums[0] += p.n[g] * p.pre[g];
     sums[1] += p.pre[g];
   }
