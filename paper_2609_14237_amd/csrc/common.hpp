@@ -30,6 +30,14 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int kWave = 64;
 constexpr int kPage = 16;
 
+// x, as if it were made here: what follows from it is not worked out ahead of the loop around it, to be kept in registers that
+// the loop needs.
+template <typename T>
+__device__ __forceinline__ T made_here(T x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // bf16 bits -> fp32 (exact).
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }

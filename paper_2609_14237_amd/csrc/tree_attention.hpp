@@ -123,10 +123,11 @@ __device__ __forceinline__ int wave_scan(int x, Op op) {
   return op(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
 }
 
-// The two bf16 halves of a dword as weights of what is not finite: 1 for +inf, 64 for -inf, 4096 for NaN, else 0.
-__device__ __forceinline__ uint32_t nonfinite_weight(uint32_t w) {
-  auto of = [](uint32_t h) {
-    return (h & 0x7f80u) != 0x7f80u ? 0u : (h & 0x7fu) ? 0x4580u : (h & 0x8000u) ? 0x4280u : 0x3f80u;
+// The two bf16 halves of a dword as weights of what is not finite: 1 for +inf, 64 for -inf, 4096 for NaN, else 0. one: 1 in
+// bf16, of which 64 and 4096 are other exponents.
+__device__ __forceinline__ uint32_t nonfinite_weight(uint32_t w, uint32_t one) {
+  auto of = [=](uint32_t h) {
+    return (h & 0x7f80u) != 0x7f80u ? 0u : (h & 0x7fu) ? one + 0x600u : (h & 0x8000u) ? one + 0x300u : one;
   };
   return of(w & 0xffffu) | of(w >> 16) << 16;
 }
@@ -550,6 +551,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   auto close_task = [&](bool whole) {
     const int cols = seq.n * group;
     const int rec = 2 * r + (first_piece ? 0 : 1);
+    const int hl = made_here(lane) & 15, rq = made_here(lane) >> 4;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       float sum = l[cb];
@@ -622,6 +624,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
     constexpr bool EDGE = decltype(edge)::value;
     uint32_t vis[CB];  // of this lane's eight tokens
     if (EDGE) {
+      const int rq = made_here(lane) >> 4;
       const int words = (a.max_rows + 63) / 64, seen_end = min(seq.ctx, seq.cap);
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
@@ -695,21 +698,25 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
     if (__any(!(nan[0] + nan[1] + nan[2] + nan[3] == 0.f))) {
       // Rare. What is not finite leaves the product and is added to the columns that see it: how many +inf, -inf and NaN
       // of each dim they see, 32 at most of each, as one product: weights 1, 64 and 4096 times the column's visible tokens.
+      const uint32_t one = made_here(0x3f80u);
+      const float not_a_number = made_here(NAN);
       u32x4 see[CB];
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          see[cb][i] = (vis[cb] >> (2 * i) & 1 ? 0x3f80u : 0u) | (vis[cb] >> (2 * i) & 2 ? 0x3f800000u : 0u);
+          see[cb][i] = (vis[cb] >> (2 * i) & 1 ? one : 0u) | (vis[cb] >> (2 * i) & 2 ? one << 16 : 0u);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         u32x4 v = vf[nb];
+        const f32x4 of = mfma_16x16x32(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, u32x4{0u, 0u, 0u, 0u}), f32x4{0.f, 0.f, 0.f, 0.f});
+        if (!__any(!(of[0] + of[1] + of[2] + of[3] == 0.f))) continue;  // these dims are finite
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           uint32_t w = v[i];
           drop_nonfinite(w);
           vf[nb][i] = w;
-          v[i] = nonfinite_weight(v[i]);
+          v[i] = nonfinite_weight(v[i], one);
         }
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb) {
@@ -719,7 +726,7 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
             const int c = (int)n[d];
             if (c & 63) acc[cb][nb][d] += INFINITY;
             if (c & (63 << 6)) acc[cb][nb][d] -= INFINITY;
-            if (c >> 12) acc[cb][nb][d] = NAN;
+            if (c >> 12) acc[cb][nb][d] = not_a_number;
           }
         }
         __builtin_amdgcn_sched_barrier(0);
