@@ -37,7 +37,7 @@ def test_others_are_built(tmp_path, monkeypatch):
     assert os.path.exists(build._compile("k_tree.hip"))
 
 
-@pytest.mark.parametrize("name", sorted(s for s in build.SOURCES if s.endswith(".hip") and s != "k_gemm.hip"))
+@pytest.mark.parametrize("name", sorted(s for s in build.SOURCES if s.endswith(".hip")))
 def test_spills_are_refused(name, tmp_path, monkeypatch):
     monkeypatch.setattr(build, "CSRC", str(tmp_path))
     monkeypatch.setattr(build, "BUILD_DIR", str(tmp_path))
