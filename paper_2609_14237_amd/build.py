@@ -33,8 +33,9 @@ EXTRA = {"k_gemm_stream.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _compile(src: str) -> str:
-    """Object of a HIP source. Kernels must fit the vector registers: the compiler has read a spilled register back in the
-    lanes of an inner branch only, where the others went on with what had taken its place."""
+    """Object of a HIP source, and beside it what its kernels hold (.usage). Kernels must fit the vector registers: the
+    compiler has read a spilled register back in the lanes of an inner branch only, where the others went on with what had
+    taken its place."""
     obj = os.path.join(BUILD_DIR, os.path.basename(src) + ".o")
     cmd = [HIPCC, *FLAGS, *EXTRA.get(src, []), "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj,
            "-Rpass-analysis=kernel-resource-usage"]
@@ -44,6 +45,8 @@ def _compile(src: str) -> str:
     spills = set(re.findall(r"VGPRs Spill: (\d+)", r.stderr))
     if src.endswith(".hip") and spills != {"0"}:
         raise RuntimeError(f"{src}: a kernel spills vector registers:\n{r.stderr}")
+    with open(obj + ".usage", "w") as f:
+        f.write(r.stderr)
     return obj
 
 

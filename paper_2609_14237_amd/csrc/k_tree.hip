@@ -14,8 +14,9 @@ namespace {
 // its cache slot. One block per (sequence, drafted row); bound by memory (64
 // sequences of 64 rows, 40 heads turned, 8 of keys and of values appended: 24 us,
 // two bytes a load 28).
+template <bool NORM>
 __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int do_rope, int do_append) {
-  __shared__ __align__(16) float cs[128], sn[128], exchange[2048];
+  __shared__ __align__(16) float cs[128], sn[128], exchange[NORM ? 2048 : 4];
   const int b = blockIdx.x, j = blockIdx.y, D = a.D;
   const DraftSeq q = draft_seq(a.row_off, a.ctx_lens, b, a.rows, a.max_rows, a.cols, a.ring);
   if (j >= q.n || q.ctx < 0) return;
@@ -32,7 +33,7 @@ __global__ __launch_bounds__(256) void draft_rope_append_kernel(DraftArgs a, int
       });
     };
     const bool wide = turns_wide(rdim, a.interleaved);
-    if (a.gain_q) {
+    if constexpr (NORM) {
       const HeadTurn p{heads, a.n_q, D, rdim, a.freqs ? a.interleaved : 0, a.gain_q, a.gain_k, a.eps};
       auto here = [&](int) { return row; };
       auto go = [](int) { return true; };
@@ -112,7 +113,8 @@ hipError_t go_tree(DraftArgs a, const TreePlan &plan, void *ws, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_draft_rope_append(const DraftArgs &a, bool do_rope, bool do_append, hipStream_t s) {
-  hipLaunchKernelGGL(draft_rope_append_kernel, dim3(a.B, a.max_rows), dim3(256), 0, s, a, (int)do_rope, (int)do_append);
+  const auto kern = do_rope && a.gain_q ? draft_rope_append_kernel<true> : draft_rope_append_kernel<false>;
+  hipLaunchKernelGGL(kern, dim3(a.B, a.max_rows), dim3(256), 0, s, a, (int)do_rope, (int)do_append);
   return hipGetLastError();
 }
 

@@ -1,5 +1,7 @@
-"""The build refuses kernels that spill vector registers, of every source."""
+"""The build refuses kernels that spill vector registers, of every source; what a kernel holds that one form of a call does not
+need is not held for the others."""
 import os
+import re
 import shutil
 
 import pytest
@@ -44,3 +46,16 @@ def test_spills_are_refused(name, tmp_path, monkeypatch):
     (tmp_path / name).write_text(SPILLS)
     with pytest.raises(RuntimeError, match="spills"):
         build._compile(name)
+
+
+def test_rotations_without_a_norm_hold_nothing_for_one():
+    """LDS of the drafted rows' RoPE and append: a row's cosines and sines, and what the norm exchanges only where there is one."""
+    usage = os.path.join(build.BUILD_DIR, "k_tree.hip.o.usage")
+    if not os.path.exists(usage):
+        os.makedirs(build.BUILD_DIR, exist_ok=True)
+        build._compile("k_tree.hip")
+    held = {}
+    for part in re.split(r"Function Name: ", open(usage).read())[1:]:
+        if "draft_rope_append_kernel" in part.split()[0]:
+            held[part.split()[0]] = int(re.search(r"LDS Size \[bytes/block\]: (\d+)", part).group(1))
+    assert sorted(held.values()) == [2 * 128 * 4, 2 * 128 * 4 + 8 * 256 * 4]
