@@ -42,8 +42,8 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
   __shared__ float s_units[KW];
 
   // Groups, as far as their sequences are this launch's; the rows and tokens of the sequences.
-  // Whatever the arrays hold, the tasks counted are those of disjoint groups of no more rows than there are: offsets that
-  // descend, or rows that overlap so that their tiles pass what the launch was checked for, share nothing.
+  // Whatever the arrays hold, the tasks counted are those of disjoint groups of disjoint rows: where offsets of groups or of
+  // rows descend, nothing is shared.
   auto here = [&](int off) { return (int)min(max((int64_t)off - a.base, (int64_t)0), (int64_t)B); };
   bool descends = false;
   float tiles = 0.f;
@@ -72,6 +72,7 @@ __global__ __launch_bounds__(64 * KW) __attribute__((amdgpu_waves_per_eu(2))) vo
     t.first[b] = s.ctx;
     t.n[b] = s.end;
     t.key[b] = s.r0;
+    descends = descends || a.row_off[b] > a.row_off[b + 1];
   }
   const bool none = __syncthreads_or(descends);
   tiles = 0.f;

@@ -6,6 +6,8 @@ import numpy as np
 import pytest
 import torch
 
+import draft_ref as D
+
 pytestmark = pytest.mark.gpu
 
 if not torch.cuda.is_available():  # pragma: no cover
@@ -75,3 +77,42 @@ def test_first_members_without_the_prefix_on_both_sides_of_a_launch():
     c.table[:3] = c.table[512:515] = -1
     c.device()
     c.check(c.attend())
+
+
+def test_rows_that_descend_share_nothing():
+    """Offsets of rows that do not ascend, so that the rows of one group's sequences lie among those another group's offsets
+    span: every sequence that has rows of its own gets its own attention, and nothing else is written."""
+    say("rows")
+    ctx = [200 + 7 * b for b in range(8)]
+    for off in ([0, 3, 12, 24, 6, 9, 12, 0, 0], [6, 9, 0, 24, 3, 9, 24, 12, 15], [0, 3, 6, 9, 12, 15, 18, 21, 24]):
+        c = Shared([(2, 192), (2, 64), (2, 192), (2, 96)], ctx, [3] * 8, n_q=8, n_kv=2, hd=64, seed=22, pad=4)
+        c.device()
+        c.off = np.array(off, np.int32)
+        c.draft.row_off[:9].copy_(cuda(c.off))
+        c.draft.row_off[9:].fill_(int(c.off[-1]))
+        guard = 1 << 16
+        ws = torch.full((c.state.ws_bytes + 2 * guard,), 0x5a, dtype=torch.uint8, device="cuda")
+        c.state.c.ws = ws.data_ptr() + guard
+        c.check(c.attend())
+        assert (ws[:guard] == 0x5a).all() and (ws[guard + c.state.ws_bytes:] == 0x5a).all()
+
+
+@pytest.mark.parametrize("B,size,tokens", [(1500, 3, 64), (4096, 9, 32), (1100, 40, 96)])
+def test_groups_on_both_sides_of_a_launch(B, size, tokens):
+    """The sequences around every border between launches, and the last ones, against the definition."""
+    say("border", B, size)
+    rng = np.random.default_rng(B)
+    ctx, rows = tokens + rng.integers(0, 40, B), rng.integers(0, 3, B)
+    c = Shared([(size, tokens)] * (B // size), ctx, rows, n_q=4, n_kv=1, hd=64, seed=B, max_rows=2).device()
+    assert len(c.tokens) <= 512
+    got = c.attend().double().cpu().numpy().reshape(c.R, 4, 64)
+    pool = c.pool.double().numpy()
+    q = c.qkv[:, :256].double().numpy().reshape(c.R, 4, 64)
+    near = {b for at in [*range(512, B, 512), B] for b in range(at - size - 1, min(at + size + 1, B))}
+    for b in sorted(near):
+        a, e = int(c.off[b]), int(c.off[b + 1])
+        if a == e:
+            continue
+        o, mag, _ = D.tree_attention(q[a:e], pool, c.table[b:b + 1], c.ctx[b:b + 1], [0, e - a], c.depth[a:e], c.sets[a:e], 1)
+        off = np.abs(got[a:e] - o) - D.tree_bound(o, mag)
+        assert (off <= 0).all(), f"sequence {b}: off by {off.max()} more than the bound"
