@@ -566,6 +566,10 @@ ods_status ods_kv_accept(const ods_block *blk, int32_t layer_begin, int32_t laye
  * group_tokens [rows] (their first *n_groups + 1 and *n_groups entries): together
  * the groups hold all rows, those that share nothing in groups of 0 tokens, or as
  * many of the first rows as ODS_SHARED_GROUPS groups take.
+ * Where none shares 32 tokens, give ods_draft no groups: with groups of nothing
+ * attn_core still takes the way of shared prefixes, which is slower for a batch
+ * without them (64 sequences of 512 to 4096 tokens, one row each: 107 us instead
+ * of 100, eight rows 135 instead of 113).
  * ODS_EINVAL for null pointers, negative sizes or token counts past the table. */
 ods_status ods_pages_shared(const int32_t *table, int32_t rows, int32_t max_pages, const int32_t *tokens,
                             int32_t *group_off, int32_t *group_tokens, int32_t *n_groups);

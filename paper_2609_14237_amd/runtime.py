@@ -565,11 +565,14 @@ class KvPages:
 
     def shared(self) -> tuple:
         """Groups of adjacent rows that share leading pages: (group_off [groups + 1], tokens [groups]) int32 numpy, for
-        SharedPrefix (ods_pages_shared)."""
+        SharedPrefix (ods_pages_shared). No groups where none shares two pages, the least that attention reads once: each
+        sequence is then read by itself at its full speed."""
         rows = len(self.tokens)
         off, tokens = np.zeros(rows + 1, np.int32), np.zeros(max(rows, 1), np.int32)
         st, n = _b.ods_pages_shared(self.table, self.tokens, off, tokens)
         _b._check(st, "ods_pages_shared")
+        if n and tokens[:n].max() < 2 * _b.PAGE_TOKENS:
+            n = 0
         return off[:n + 1].copy(), tokens[:n].copy()
 
     def compact(self, max_pairs: int | None = None) -> int:
