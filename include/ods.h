@@ -445,7 +445,11 @@ ods_status ods_head_rows(const ods_rope *rope, const ods_head_norm *norm, const 
  * itself. So are sequences in no group, groups of one, and sequences of fewer
  * cached tokens than their group shares, whatever their tables hold; what is
  * shared is rounded down to 32 tokens. Sliding-window layers read each sequence's
- * own window.
+ * own window. A table as wide as the longest context passes the 128 MB whatever
+ * is in it: short contexts are then better given no groups. Sharing has one
+ * level, of sequences that are neighbours in the batch: of a prefix common to all
+ * and longer ones common to some, a group names one. n_kv * (query tiles of the
+ * groups + batch) * 32-token tiles of a table < 2^30 (ODS_EUNSUPPORTED otherwise).
  *   n_groups   0 .. batch, at most ODS_SHARED_GROUPS
  *   group_off  device [n_groups + 1], ascending, in 0 .. batch
  *   tokens     device [n_groups] */

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(const uint16_t *x, int64
 
 // `per` rows a block (kHeadRows at most). Bound by memory, and by what the block waits for before its first row: positions,
 // then frequencies, then fp64 angles. Several rows a block share that wait, and all but the first items of a thread are loaded
-// without it (8192 rows of 32 + 8 heads of 128, 168 MB: a row a block 42 us, four 40, 4.2 TB/s; a copy takes 33; 4097 rows of
+// without it (8192 rows of 32 + 8 heads of 128, 168 MB: a row a block 42 us, four 38, 4.4 TB/s; a copy takes 33; 4097 rows of
 // 36 heads, half of each turned: 33 and 20).
 constexpr int kHeadRows = 8, kHeadThreads = 512;
 template <int KIND>

@@ -111,7 +111,7 @@ struct DraftArgs {
 hipError_t launch_draft_rope_append(const DraftArgs &a, bool do_rope, bool do_append, hipStream_t s);
 // ws: tree_ws_bytes(plan, D).
 hipError_t launch_tree_attention(const DraftArgs &a, const TreePlan &plan, void *ws, hipStream_t s);
-// The same with shared prefixes. ws: shared_ws_bytes(plan, ...).
+// The same with shared prefixes. ws: shared_ws(plan, ...).bytes.
 hipError_t launch_shared_attention(const DraftArgs &a, const SharedPlan &plan, void *ws, hipStream_t s);
 
 // Pools of several layers, handed to one launch by value.

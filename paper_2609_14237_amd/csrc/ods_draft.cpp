@@ -216,7 +216,8 @@ bool spans_shared(const ods_layer_cfg &c, const ods_batch *batch) {
 // products bound either way, and the records grow with them. 32 / 8 heads of 128, one group, tails of 256, us with and
 // without: a token each, 8 sequences over 2048 (76 MB) 20.5 and 18.5, 16 over 2048 (151 MB) 26 and 28, 8 over 8192
 // (277 MB) 28 and 48, 64 over 8192 43 and 208; 64 sequences of 24, 32, 48 and 64 columns over 8192 100 and 207, 130 and 209,
-// 179 and 211, 229 and 214; of 32 and 48 over 2048 68 and 64, 88 and 67. The host sees no contexts: tables count as if they were full.
+// 179 and 211, 229 and 214; of 32 and 48 over 2048 68 and 64, 88 and 67. The host sees no contexts: tables count as if they were
+// full, and short contexts in wide tables pay the second kernel (two of 100 tokens: 15.5 us, each by itself 10.7).
 bool takes_shared(const ods_layer_cfg &c, const ods_batch *batch, const ods_draft *draft) {
   return has_shared(c, draft) && (int64_t)draft->max_rows * (c.n_q / c.n_kv) <= kSharedColumns && spans_shared(c, batch);
 }
@@ -227,9 +228,9 @@ SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods
   const int64_t columns = (int64_t)draft->rows * group, nq = (int64_t)draft->max_rows * group;
   // The host knows no group's rows: the mean group's decide. Workgroups of eight waves have a compute unit to themselves and
   // share each K/V byte among 256 columns, which is fastest where the prefixes' products are nearly all there is (128
-  // sequences of 4 rows, 4096 columns, over 32768 tokens: 309 us, with four waves 379). Two of four waves overlap the products
-  // of one with the loads of the other (64 sequences over 8192 tokens, 256 columns, read from the caches: 38 us, with eight
-  // waves 42).
+  // sequences of 4 rows, 4096 columns, over 32768 tokens: 309 us, with four waves 364; 64-wide heads 225 and 229). Two of four
+  // waves overlap the products of one with the loads of the other (4 sequences over 32768 tokens 40 us, with eight waves 54; 64
+  // over 8192 44 and 45; seven groups 105 and 120, of 64-wide heads 73 and 70).
   const int64_t mean = columns / groups;
   p.waves = mean >= 1024 ? 8 : 4;
   // Tails of 16 columns (32 with eight waves) are one wave's ranges; wider ones a workgroup's (seven groups, up to 32 columns,
@@ -242,8 +243,9 @@ SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods
   p.grid = (int)std::max<int64_t>(2, std::min<int64_t>((int64_t)std::max(cus, 1) * (p.waves == 4 ? 2 : 1), tasks * tiles / 4));
   // Of a prefix tile, measured as what splits the grid best (us, tokens from memory): tails of a wave at 0.5, 0.75, 1.0 and
   // 1.3, 64 sequences over 8192 tokens 47, 45, 46 and 45, 4 over 32768 tokens 52.5, 49.2, 48.2 and 48.1; tails of four waves,
-  // seven groups, 114, 107, 110 and 106 (1.6: 110); eight waves, 128 sequences over 32768, at 0.3, 0.4, 0.6 and 1.0: 377, 309,
-  // 312 and 318.
+  // seven groups, 114, 107, 110 and 106 (1.6: 110); eight waves, 128 sequences over 32768, at 0.3, 0.4, 0.6 and 1.0: 379, 309,
+  // 305 and 311, of 64-wide heads 221, 225, 230 and 242. What a task costs besides is nearly level: prefix_task 0 and 8 within 1%;
+  // tail_task 0 and 2: 64 over 8192 44.1 and 45.0 (64-wide 29 and 31), 128 over 32768 322 and 303.
   const bool of_wave = p.qtt <= 32;
   p.cost.prefix_tile = 1.f;
   p.cost.prefix_task = 4.f;
@@ -254,6 +256,8 @@ SharedPlan shared_plan(const ods_layer_cfg &c, const ods_batch *batch, const ods
   // tokens 24, 23 and 27 us).
   p.cost.prefix_least = 16;
   p.cost.tail_least = of_wave ? 3 : 4;
+  // Prefix tasks cut into pieces of their own and tails left whole, at 2 and 12, 0 and 24: no difference; tails of a wave at 4:
+  // 4 over 32768 43.5 us, at 1 40.
   p.cost.prefix_slack = 6;
   p.cost.tail_slack = of_wave ? 1 : 8;
   return p;

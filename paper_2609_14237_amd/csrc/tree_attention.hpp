@@ -769,8 +769,8 @@ __device__ __forceinline__ void tree_work(const DraftArgs &a, const TreeSeqs &se
   //    have landed when anyone's products t end.
   //  - One wave alone has no barrier; it reads a tile when it starts on it.
   constexpr bool PING = QW == 8;
-  // Keys are read a tile ahead. Not where prefixes and tails are one kernel: it has no registers left for them, and what is
-  // spilled to memory there has been read back by the lanes of an inner branch alone (128 x 4 rows over 32768: 300 us, 312).
+  // Keys are read a tile ahead. Not where prefixes and tails are one kernel, which spilled 32 registers with them when that was
+  // tried (128 x 4 rows over 32768: 300 us, without either 312), one of them read back by the lanes of an inner branch alone.
   constexpr bool AHEAD = QW == 8 && PART == kWhole;
   int slot = 0;
   auto next_slot = [](int x) { return x + 1 == NS ? 0 : x + 1; };

@@ -1,4 +1,5 @@
-// Turning the heads of one row, by the 256 threads of a block.
+// Turning the heads of a row, by the 256 threads of a block, and of several rows whose heads are normalised first, by up to 512
+// (turn_heads).
 #pragma once
 #include <type_traits>
 
