@@ -276,7 +276,8 @@ def rope(r: Rope, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor | None =
 class SharedPrefix:
     """Groups of a batch's sequences that share the pages of a prefix (ods_shared): group g is sequences
     group_off[g] .. group_off[g + 1] - 1, whose tables name the same pages for their first tokens[g] tokens. Device int32
-    [groups + 1] and [groups]; KvPages.shared() finds them. Both may be rewritten between calls; their lengths stay."""
+    [groups + 1] and [groups]; KvPages.shared() finds them. Both may be rewritten between calls, as this object's `group_off`
+    and `tokens` (copies of what was given, where that is not contiguous); their lengths stay."""
 
     def __init__(self, group_off: torch.Tensor, tokens: torch.Tensor):
         if group_off.dtype != torch.int32 or tokens.dtype != torch.int32 or tokens.dim() != 1 or group_off.shape != (len(tokens) + 1,):
